@@ -294,6 +294,88 @@ int rsa_linformer_backward(const rsa_desc *d, int32_t Kp, const void *dO, const 
 int rsa_linformer_project_bwd(const rsa_desc *d, int32_t Kp, const void *dXp, const void *X,
                               const void *E, void *dX, float *dE, void *stream);
 
+/*
+ * Rotation of queries and keys by position: pairs of a head's first R elements are turned by
+ * angle position * inv_freq[i], i = 0 .. R/2 - 1 (fp32, the caller's: any base or stretching),
+ *   y0 = x0 cos - x1 sin,  y1 = x1 cos + x0 sin;
+ * the pair is (x[i], x[i + R/2]), with `adjacent` (x[2i], x[2i+1]).  Elements from R on are copied.  R is
+ * even, 2 <= R <= A.  The position of a row is its token in the sequence: rows of Q as the
+ * descriptor's ranks own them (contiguous or zig-zag), rows of K, (B, Z, L, A), in token order.
+ * Angles are reduced in 64 bits (no position is too far); products and sums are fp32, one rounding
+ * per stored element.  Either mode, dtype and layout of the descriptor; causal, scale and
+ * RSA_DETERMINISTIC change nothing.  Q and Qr share q_stride, K and Kr kv_stride.  Q with
+ * Qr or K with Kr may be NULL: not rotated.  An output may be exactly its own input (in place) and
+ * must not overlap anything otherwise.  B * L must be below 2^31.
+ *  rsa_rotate_bwd: dQ, dK = the transposed rotation of dQr, dKr (the angles get no gradient).
+ */
+int rsa_rotate(const rsa_desc *d, int32_t R, int32_t adjacent, const float *inv_freq,
+               const void *Q, const void *K, void *Qr, void *Kr, void *stream);
+int rsa_rotate_bwd(const rsa_desc *d, int32_t R, int32_t adjacent, const float *inv_freq,
+                   const void *dQr, const void *dKr, void *dQ, void *dK, void *stream);
+
+/*
+ * Answering with a trained model: a paged cache of keys and values, and the attention of one new
+ * token per sequence to it.
+ *
+ * The cache is two pools of pages in HBM, Kc and Vc, each (pages, Zkv, page, A): page p holds, head by
+ * head, `page` consecutive tokens' rows.  Sequence b is the pages table[b][0 .. width), int32: its
+ * token in slot s lies in page table[b][s / page], place s % page.  A table entry outside
+ * [0, pages) is a page that is not held (a window that has moved on, or none yet): nothing is written
+ * there and its slots are not seen.  lengths[b], int32, counts the sequence's slots, those of the
+ * tokens that the call appends included; slots below 0 or behind the table do not exist.
+ * Tables and lengths are device memory that the kernels check, so a
+ * captured graph replays with new contents.  Key head h serves query heads [h Z/Zkv, (h+1) Z/Zkv).
+ * bf16 or fp32 (arithmetic as for rsa_forward in bf16; fp32 multiply-adds in fp32), A a
+ * multiple of 64 up to 256, any page size, B below 2^16.
+ */
+typedef struct {
+  int32_t B;          /* sequences of a call (rows of the table)               */
+  int32_t Z, Zkv, A;  /* query heads, key heads (Zkv divides Z), head size     */
+  int32_t page;       /* tokens of a page                                      */
+  int32_t pages;      /* pages of a pool                                       */
+  int32_t width;      /* entries of a row of the table                         */
+  int32_t dtype;      /* rsa_dtype of queries, keys, values, pools and results */
+  float scale;        /* 0 selects 1/sqrt(A)                                   */
+  uint32_t flags;     /* 0                                                     */
+  /* Strides in elements of the batch, head and token index: q_stride for Q and Qr, kv_stride for
+   * the new K and V, o_stride for O.  All three zero = dense (B, heads, tokens, A).
+   * Positive multiples of 16 bytes otherwise. */
+  int64_t q_stride[3], kv_stride[3], o_stride[3];
+} rsa_cache_desc;
+
+/* Appends up to T tokens to every sequence.  K, V: (B, Zkv, T, A).  Of sequence b the first counts[b]
+ * (NULL, or above T: T; below 0: 0) tokens are there; token t takes slot lengths[b] - counts[b] + t and
+ * position first[b] (NULL: 0; the position of slot 0, for one rank's share of a cache) + slot.
+ * K is rotated by position as in rsa_rotate (inv_freq NULL: not rotated, R ignored), V copied.
+ * Tokens whose slot is below 0, behind the table or on a page that is not held are not
+ * written.  Q, (B, Z, T, A), unless NULL, is rotated into Qr alike for every token that
+ * is there, whether its slot is held or not; rows of other tokens are left as they are.  Qr may be exactly Q.
+ * Outputs must not overlap inputs otherwise, nor each other.  Two tokens of a call on one slot leave
+ * the elements of either there. */
+int rsa_cache_append(const rsa_cache_desc *d, int32_t T, const void *Q, const void *K, const void *V,
+                     const int32_t *table, const int32_t *lengths, const int32_t *counts,
+                     const int32_t *first, int32_t R, int32_t adjacent, const float *inv_freq,
+                     void *Qr, void *Kc, void *Vc, void *stream);
+
+/* Attention of one query row per sequence and head, Q (B, Z, 1, A), to the slots of its sequence
+ * that are held: O (B, Z, 1, A) and LSE (B, Z, 1) fp32 as rsa_forward's.  A row that sees no key
+ * gets O = 0 and LSE = -inf.  Pool memory outside the seen slots does not reach a result, whatever it holds.
+ * The walk over the cache is divided among work-groups by what the lengths say, in a fixed
+ * order of sums for given lengths.  ws: rsa_cache_workspace_bytes(d) bytes (may be NULL if that is 0), of one call at a
+ * time; the kernels read nothing there that the call has not written. */
+size_t rsa_cache_workspace_bytes(const rsa_cache_desc *d);
+int rsa_cache_attend(const rsa_cache_desc *d, const void *Q, const void *Kc, const void *Vc,
+                     const int32_t *table, const int32_t *lengths, void *O, float *LSE, void *ws,
+                     size_t ws_bytes, void *stream);
+
+/* Joins the results of N shares of a cache (each of N ranks holds some of the tokens and attends
+ * to those): Op (N, B, Z, 1, A) and LSEp (N, B, Z, 1), dense, as rsa_cache_attend wrote
+ * them; LSE = log sum_n exp(LSEp_n), O = sum_n exp(LSEp_n - LSE) Op_n.  A share with LSEp = -inf counts nothing,
+ * whatever its Op holds; all of them: O = 0, LSE = -inf.  Outputs must not overlap inputs.
+ * Of the descriptor B, Z, A, dtype and o_stride are used; the whole has to be valid. */
+int rsa_cache_join(const rsa_cache_desc *d, int32_t N, const void *Op, const float *LSEp, void *O,
+                   float *LSE, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

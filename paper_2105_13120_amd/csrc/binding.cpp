@@ -14,6 +14,8 @@
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <array>
+
 #include "rsa.h"
 
 namespace {
@@ -24,21 +26,23 @@ struct Refused {};  // a Python error is set
 struct Call {
   PyObject *const *args;
   rsa_desc *d = nullptr;
+  const rsa_cache_desc *cd = nullptr;  // ... or this one, of the calls on the cache
   Py_buffer view{};
 
-  Call(PyObject *const *args_, Py_ssize_t n, Py_ssize_t want) : args(args_) {
+  Call(PyObject *const *args_, Py_ssize_t n, Py_ssize_t want, bool cache) : args(args_) {
     if (n != want) {
       PyErr_Format(PyExc_TypeError, "%zd arguments expected, %zd given", want, n);
       throw Refused{};
     }
     // the descriptor is a ctypes structure, which exports its memory
     if (PyObject_GetBuffer(args[0], &view, PyBUF_SIMPLE) != 0) throw Refused{};
-    if (view.len != (Py_ssize_t)sizeof(rsa_desc)) {
+    if (view.len != (Py_ssize_t)(cache ? sizeof(rsa_cache_desc) : sizeof(rsa_desc))) {
       PyErr_SetString(PyExc_TypeError, "not a descriptor");
       PyBuffer_Release(&view);
       throw Refused{};
     }
-    d = static_cast<rsa_desc *>(view.buf);
+    if (cache) cd = static_cast<const rsa_cache_desc *>(view.buf);
+    else d = static_cast<rsa_desc *>(view.buf);
   }
   ~Call() { PyBuffer_Release(&view); }
   Call(const Call &) = delete;
@@ -91,11 +95,11 @@ template <class F> PyObject *finish(F call, std::initializer_list<at::Tensor> re
   return status == RSA_OK ? wrapped(results) : PyLong_FromLong(status);
 }
 
-template <PyObject *(*F)(Call &)> struct Entry {
+template <PyObject *(*F)(Call &), bool CACHE> struct Entry {
   template <int N> static PyObject *call(PyObject *, PyObject *const *args, Py_ssize_t n) {
     HANDLE_TH_ERRORS
     try {
-      Call c(args, n, N);
+      Call c(args, n, N, CACHE);
       return F(c);
     } catch (Refused) {
       return nullptr;
@@ -250,8 +254,181 @@ PyObject *linformer_project_bwd(Call &c) {
     {dX, dE});
 }
 
-template <PyObject *(*F)(Call &), int N> PyMethodDef method(const char *name) {
-  return {name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&Entry<F>::template call<N>)), METH_FASTCALL, nullptr};
+// The calls below read tables, so that a wrong shape would reach memory that is not the tensor's: every tensor is held against
+// the descriptor.  Tensors on the CPU come last, so that this is the same without a GPU.
+[[noreturn]] void refuse(int i, const char *what) {
+  PyErr_Format(PyExc_ValueError, "argument %d: %s", i, what);
+  throw Refused{};
+}
+// st: strides of all indices but the last; zeros: dense; nullptr: any dense
+void check(int i, const at::Tensor &t, at::ScalarType type, at::IntArrayRef shape, const int64_t *st = nullptr) {
+  if (t.scalar_type() != type) refuse(i, "not of the descriptor's (or the expected) dtype");
+  if (t.sizes() != shape) refuse(i, "not of the descriptor's (or the other tensors') shape");
+  bool dense = true;
+  if (st)
+    for (size_t k = 0; k + 1 < shape.size(); ++k) dense = dense && st[k] == 0;
+  if (dense ? !t.is_contiguous() : t.stride(-1) != 1 && shape.back() != 1) refuse(i, "not laid out as the descriptor says");
+  if (!dense)
+    for (size_t k = 0; k + 1 < shape.size(); ++k)
+      if (shape[k] != 1 && t.stride((int64_t)k) != st[k]) refuse(i, "not laid out as the descriptor says");
+}
+// ... and that they are where the work is enqueued
+void check_device(const Call &c, int n) {
+  for (int i = 1; i < n; ++i)
+    if (THPVariable_Check(c.args[i])) {
+      const at::Tensor &t = c.tensor(i);
+      if (!t.is_cuda() || t.get_device() != c10::hip::getCurrentHIPStream().device_index()) {
+        PyErr_Format(PyExc_AssertionError, "argument %d: a tensor of the current GPU expected", i);
+        throw Refused{};
+      }
+    }
+}
+// a result laid out as an input is, which only an input without gaps can lend
+at::Tensor laid_out_as(int i, const at::Tensor &t, bool zero) {
+  if (!t.is_non_overlapping_and_dense()) refuse(i, "a result for an input with gaps has to be given");
+  return zero ? at::zeros_like(t) : at::empty_like(t);
+}
+at::ScalarType type_of(int32_t dtype) { return dtype == RSA_F32 ? at::kFloat : at::kBFloat16; }
+int32_t truth(const Call &c, int i) {
+  const int v = PyObject_IsTrue(c.args[i]);
+  if (v < 0) throw Refused{};
+  return v;
+}
+// R, from the frequencies
+int32_t check_frequencies(const Call &c, int i) {
+  const at::Tensor &t = c.tensor(i);
+  const int64_t n = t.dim() == 1 ? t.size(0) : 0;
+  if (n < 1 || n > 128) refuse(i, "frequencies of 1 to A / 2 pairs expected");
+  check(i, t, at::kFloat, {n});
+  return (int32_t)(2 * n);
+}
+
+// desc, inv_freq, Q, K, Qr, Kr, adjacent, back
+PyObject *rotate(Call &c) {
+  const rsa_desc &d = *c.d;
+  const int32_t R = check_frequencies(c, 1), adjacent = truth(c, 6), back = truth(c, 7);
+  at::Tensor in[2], out[2];
+  for (int i = 0; i < 2; ++i) {
+    if (!c.given(2 + i)) {
+      if (c.given(4 + i)) refuse(4 + i, "a result without its input");
+      continue;
+    }
+    const std::array<int64_t, 4> shape{d.B, d.Z, i ? d.L : rows_of(&d), d.A};
+    const int64_t *st = i ? d.kv_stride : d.q_stride;
+    in[i] = c.tensor(2 + i);
+    check(2 + i, in[i], type_of(d.dtype), shape, st);
+    out[i] = c.tensor_or(4 + i, [&] { return laid_out_as(2 + i, in[i], false); });
+    check(4 + i, out[i], type_of(d.dtype), shape, st);
+  }
+  check_device(c, 6);
+  const auto call = back ? rsa_rotate_bwd : rsa_rotate;
+  const float *freq = static_cast<const float *>(ptr(c.tensor(1)));
+  void *stream = c10::hip::getCurrentHIPStream().stream();
+  int status;
+  Py_BEGIN_ALLOW_THREADS
+  status = call(&d, R, adjacent, freq, ptr(in[0]), ptr(in[1]), ptr(out[0]), ptr(out[1]), stream);
+  Py_END_ALLOW_THREADS
+  if (status != RSA_OK) return PyLong_FromLong(status);
+  PyObject *r = PyTuple_New(2);
+  for (int i = 0; r && i < 2; ++i) {
+    PyObject *o = out[i].defined() ? THPVariable_Wrap(out[i]) : (Py_INCREF(Py_None), Py_None);
+    if (!o) { Py_DECREF(r); return nullptr; }
+    PyTuple_SET_ITEM(r, i, o);
+  }
+  return r;
+}
+
+const int32_t *int32s(const Call &c, int i, at::IntArrayRef shape) {
+  if (!c.given(i)) return nullptr;
+  check(i, c.tensor(i), at::kInt, shape);
+  return static_cast<const int32_t *>(ptr(c.tensor(i)));
+}
+void check_pools(const Call &c, int i) {
+  const rsa_cache_desc &d = *c.cd;
+  for (int k = i; k < i + 2; ++k) check(k, c.tensor(k), type_of(d.dtype), {d.pages, d.Zkv, d.page, d.A});
+}
+
+// desc, K, V, Kc, Vc, table, lengths, counts, first, inv_freq, adjacent, Q, Qr
+PyObject *cache_append(Call &c) {
+  const rsa_cache_desc &d = *c.cd;
+  const at::Tensor &K = c.tensor(1), &V = c.tensor(2), &Kc = c.tensor(3), &Vc = c.tensor(4);
+  if (K.dim() != 4 || K.size(2) < 1 || K.size(2) > INT32_MAX) refuse(1, "(B, Zkv, T, A) expected");
+  const int64_t T = K.size(2);
+  for (int i = 1; i < 3; ++i) check(i, c.tensor(i), type_of(d.dtype), {d.B, d.Zkv, T, d.A}, d.kv_stride);
+  check_pools(c, 3);
+  if (!c.given(5) || !c.given(6)) refuse(c.given(5) ? 6 : 5, "a tensor expected");
+  const int32_t *table = int32s(c, 5, {d.B, d.width}), *lengths = int32s(c, 6, {d.B}), *counts = int32s(c, 7, {d.B});
+  const int32_t *first = int32s(c, 8, {d.B}), R = c.given(9) ? check_frequencies(c, 9) : 0, adjacent = truth(c, 10);
+  const float *freq = c.given(9) ? static_cast<const float *>(ptr(c.tensor(9))) : nullptr;
+  at::Tensor Q, Qr;
+  if (c.given(11)) {
+    Q = c.tensor(11);
+    check(11, Q, type_of(d.dtype), {d.B, d.Z, T, d.A}, d.q_stride);
+    Qr = c.tensor_or(12, [&] { return laid_out_as(11, Q, counts != nullptr); });
+    check(12, Qr, type_of(d.dtype), {d.B, d.Z, T, d.A}, d.q_stride);
+  } else if (c.given(12)) {
+    refuse(12, "a result without its input");
+  }
+  check_device(c, 13);
+  const auto call = [&](void *st) {
+    return rsa_cache_append(&d, (int32_t)T, ptr(Q), ptr(K), ptr(V), table, lengths, counts, first, R, adjacent, freq, ptr(Qr), ptr(Kc),
+                            ptr(Vc), st); };
+  if (Q.defined()) return finish(call, {Qr});
+  PyObject *r = finish(call, {Kc});
+  if (!r || PyLong_Check(r)) return r;
+  Py_DECREF(r);
+  Py_RETURN_NONE;
+}
+
+// desc, Q, Kc, Vc, table, lengths, O, LSE, ws
+PyObject *cache_attend(Call &c) {
+  const rsa_cache_desc &d = *c.cd;
+  const at::Tensor &Q = c.tensor(1), &Kc = c.tensor(2), &Vc = c.tensor(3);
+  const std::array<int64_t, 4> shape{d.B, d.Z, 1, d.A};
+  check(1, Q, type_of(d.dtype), shape, d.q_stride);
+  check_pools(c, 2);
+  if (!c.given(4) || !c.given(5)) refuse(c.given(4) ? 5 : 4, "a tensor expected");
+  const int32_t *table = int32s(c, 4, {d.B, d.width}), *lengths = int32s(c, 5, {d.B});
+  const at::Tensor O = c.tensor_or(6, [&] { return at::empty(shape, Q.options()); });
+  check(6, O, type_of(d.dtype), shape, d.o_stride);
+  const at::Tensor LSE = c.tensor_or(7, [&] { return at::empty({d.B, d.Z, 1}, Q.options().dtype(at::kFloat)); });
+  check(7, LSE, at::kFloat, {d.B, d.Z, 1});
+  check_device(c, 9);
+  size_t n = 0;
+  at::Tensor ws;
+  if (c.given(8)) {
+    ws = c.tensor(8);
+    if (!ws.is_contiguous()) refuse(8, "a workspace without gaps expected");
+    n = ws.nbytes();
+  } else if ((n = rsa_cache_workspace_bytes(&d)) > 0) {
+    ws = bytes(n, Q);
+  }
+  return finish([&](void *st) {
+    return rsa_cache_attend(&d, ptr(Q), ptr(Kc), ptr(Vc), table, lengths, ptr(O), static_cast<float *>(ptr(LSE)), ptr(ws), n, st); },
+    {O, LSE});
+}
+
+// desc, Op, LSEp, O, LSE
+PyObject *cache_join(Call &c) {
+  const rsa_cache_desc &d = *c.cd;
+  const at::Tensor &Op = c.tensor(1), &LSEp = c.tensor(2);
+  if (Op.dim() != 5 || Op.size(0) < 1 || Op.size(0) > INT32_MAX) refuse(1, "(N, B, Z, 1, A) expected");
+  const int64_t N = Op.size(0);
+  check(1, Op, type_of(d.dtype), {N, d.B, d.Z, 1, d.A});
+  check(2, LSEp, at::kFloat, {N, d.B, d.Z, 1});
+  const std::array<int64_t, 4> shape{d.B, d.Z, 1, d.A};
+  const at::Tensor O = c.tensor_or(3, [&] { return at::empty(shape, Op.options()); });
+  check(3, O, type_of(d.dtype), shape, d.o_stride);
+  const at::Tensor LSE = c.tensor_or(4, [&] { return at::empty({d.B, d.Z, 1}, LSEp.options()); });
+  check(4, LSE, at::kFloat, {d.B, d.Z, 1});
+  check_device(c, 5);
+  return finish([&](void *st) {
+    return rsa_cache_join(&d, (int32_t)N, ptr(Op), static_cast<const float *>(ptr(LSEp)), ptr(O), static_cast<float *>(ptr(LSE)), st); },
+    {O, LSE});
+}
+
+template <PyObject *(*F)(Call &), int N, bool CACHE = false> PyMethodDef method(const char *name) {
+  return {name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&Entry<F, CACHE>::template call<N>)), METH_FASTCALL, nullptr};
 }
 
 }  // namespace
@@ -263,6 +440,8 @@ PyMODINIT_FUNC PyInit__binding(void) {
       method<out_proj, 4>("out_proj"), method<out_proj_bwd, 7>("out_proj_bwd"), method<qkv_proj_bwd, 9>("qkv_proj_bwd"),
       method<linformer_project, 5>("linformer_project"), method<linformer_forward, 6>("linformer_forward"),
       method<linformer_backward, 11>("linformer_backward"), method<linformer_project_bwd, 6>("linformer_project_bwd"),
+      method<rotate, 8>("rotate"), method<cache_append, 13, true>("cache_append"),
+      method<cache_attend, 9, true>("cache_attend"), method<cache_join, 5, true>("cache_join"),
       {nullptr, nullptr, 0, nullptr}};
   static PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, table, nullptr, nullptr, nullptr, nullptr};
   return PyModule_Create(&module);

@@ -1,6 +1,7 @@
 // C ABI of the RSA library: argument validation and dispatch (declared in rsa.h).
 #include <cmath>
 #include <cstring>
+#include <initializer_list>
 #include <mutex>
 
 #include "rsa_kernels.h"
@@ -105,13 +106,13 @@ int check_rank_chunk(const Dims &d, int n, int j) {
 
 extern "C" {
 
-int rsa_version(void) { return 110; }
+int rsa_version(void) { return 120; }
 
 const char *rsa_strerror(int status) {
   switch (status) {
     case RSA_OK: return "ok";
     case RSA_ERR_NULL: return "a required pointer is NULL";
-    case RSA_ERR_SHAPE: return "bad shape: sizes must be positive, L divisible by N, ranks within [0, N)";
+    case RSA_ERR_SHAPE: return "bad shape: sizes must be positive, L divisible by N, ranks within [0, N), Z by Zkv, 2 <= R <= A";
     case RSA_ERR_UNSUPPORTED:
       return "unsupported: need a head size of 64 or 128 (staged mode: a multiple of 64 up to 256), L/N "
              "divisible by 64, 16-byte aligned pointers, bf16 for the fused mode";
@@ -466,6 +467,117 @@ int rsa_linformer_project_bwd(const rsa_desc *d, int32_t Kp, const void *dXp, co
   char *dXr = static_cast<char *>(dX) + row0 * own.A * 2;
   float *dEr = dE + row0 * Kp;
   return hip_status(rsa::linformer_project_bwd(Zt, own.L, own.Lq, Kp, own.A, dXp, Xr, Er, dXr, dEr, st));
+}
+
+// ------------------------------------------------- rotation by position ----
+namespace {
+int rotate(const rsa_desc *d, int32_t R, int32_t adjacent, const float *inv_freq, bool back, const void *Q, const void *K,
+           void *Qr, void *Kr, void *stream) {
+  RSA_STEP_PROLOGUE(inv_freq && (Q || K) && !Q == !Qr && !K == !Kr, Q, K, Qr, Kr);
+  if (reinterpret_cast<uintptr_t>(inv_freq) & 3u) return RSA_ERR_UNSUPPORTED;
+  if (R < 2 || R > dm.A) return RSA_ERR_SHAPE;
+  if (R % 2 != 0 || (int64_t)dm.B * dm.L >= (1LL << 31)) return RSA_ERR_UNSUPPORTED;
+  return hip_status(rsa::rotate_rows(dm, d->dtype, R, adjacent != 0, inv_freq, back, Q, K, Qr, Kr, st));
+}
+}  // namespace
+
+int rsa_rotate(const rsa_desc *d, int32_t R, int32_t adjacent, const float *inv_freq, const void *Q, const void *K, void *Qr,
+               void *Kr, void *stream) {
+  return rotate(d, R, adjacent, inv_freq, false, Q, K, Qr, Kr, stream);
+}
+
+int rsa_rotate_bwd(const rsa_desc *d, int32_t R, int32_t adjacent, const float *inv_freq, const void *dQr, const void *dKr,
+                   void *dQ, void *dK, void *stream) {
+  return rotate(d, R, adjacent, inv_freq, true, dQr, dKr, dQ, dK, stream);
+}
+
+// ------------------------------------------- the cache of keys and values ----
+namespace {
+// tokens: of the call's new queries, keys and values per sequence
+int cache_validate(const rsa_cache_desc *d, int32_t tokens, rsa::CacheDims *out) {
+  if (!d) return RSA_ERR_NULL;
+  if (d->B < 1 || d->Z < 1 || d->Zkv < 1 || d->A < 1 || d->page < 1 || d->pages < 1 || d->width < 1 || tokens < 1) return RSA_ERR_SHAPE;
+  if (d->Z % d->Zkv != 0) return RSA_ERR_SHAPE;
+  if (d->A % 64 != 0 || d->A > 256) return RSA_ERR_UNSUPPORTED;
+  if ((d->dtype != RSA_F32 && d->dtype != RSA_BF16) || d->flags != 0) return RSA_ERR_UNSUPPORTED;
+  if (!(d->scale >= 0.0f) || !std::isfinite(d->scale)) return RSA_ERR_SHAPE;
+  // slots, rows of a pool, rows of queries and tokens of a call are counted in 32 bits
+  const int64_t most = 1LL << 31;
+  if (d->B > 65535 || (int64_t)d->B * d->Z > (1 << 24) || (int64_t)d->width * d->page >= most || (int64_t)d->B * tokens >= most ||
+      (int64_t)d->pages * d->Zkv > (2 * most - 1) / d->page)
+    return RSA_ERR_UNSUPPORTED;
+  out->B = d->B; out->Z = d->Z; out->Zkv = d->Zkv; out->A = d->A;
+  out->page = d->page; out->pages = d->pages; out->width = d->width; out->dtype = d->dtype;
+  out->scale = d->scale > 0.0f ? d->scale : 1.0f / std::sqrt((float)d->A);
+  const int64_t *in[3] = {d->q_stride, d->kv_stride, d->o_stride};
+  int64_t *st[3] = {out->qs, out->ks, out->os};
+  const int unit = d->dtype == RSA_BF16 ? 8 : 4;
+  for (int t = 0; t < 3; ++t) {
+    const int64_t heads = t == 1 ? d->Zkv : d->Z, rows = t == 2 ? 1 : tokens, dense[3] = {heads * rows * d->A, rows * d->A, d->A};
+    const bool zero = in[t][0] == 0 && in[t][1] == 0 && in[t][2] == 0;
+    for (int k = 0; k < 3; ++k) {
+      st[t][k] = zero ? dense[k] : in[t][k];
+      if (st[t][k] <= 0) return RSA_ERR_SHAPE;
+      if (st[t][k] % unit != 0 || st[t][k] > (1LL << 40)) return RSA_ERR_UNSUPPORTED;
+    }
+  }
+  return RSA_OK;
+}
+size_t pool_bytes(const rsa::CacheDims &d) {
+  return (size_t)d.pages * d.Zkv * d.page * d.A * (d.dtype == RSA_BF16 ? 2 : 4);
+}
+}  // namespace
+
+#define RSA_CACHE_PROLOGUE(tokens, ptr_ok, ...)                   \
+  rsa::CacheDims dm;                                              \
+  int rc = cache_validate(d, tokens, &dm);                        \
+  if (rc != RSA_OK) return rc;                                    \
+  if (!(ptr_ok)) return RSA_ERR_NULL;                             \
+  { const void *ps_[] = {__VA_ARGS__};                            \
+    for (const void *p_ : ps_) if (misaligned(p_)) return RSA_ERR_UNSUPPORTED; } \
+  hipStream_t st = static_cast<hipStream_t>(stream)
+
+namespace {
+bool words(std::initializer_list<const void *> ps) {  // whether all are aligned to 4 bytes
+  for (const void *p : ps)
+    if (reinterpret_cast<uintptr_t>(p) & 3u) return false;
+  return true;
+}
+}  // namespace
+
+int rsa_cache_append(const rsa_cache_desc *d, int32_t T, const void *Q, const void *K, const void *V, const int32_t *table,
+                     const int32_t *lengths, const int32_t *counts, const int32_t *first, int32_t R, int32_t adjacent,
+                     const float *inv_freq, void *Qr, void *Kc, void *Vc, void *stream) {
+  RSA_CACHE_PROLOGUE(T, K && V && table && lengths && Kc && Vc && !Q == !Qr, Q, K, V, Qr, Kc, Vc);
+  if (!words({table, lengths, counts, first, inv_freq})) return RSA_ERR_UNSUPPORTED;
+  if (!inv_freq) R = 0;
+  if (inv_freq && (R < 2 || R > dm.A)) return RSA_ERR_SHAPE;
+  if (R % 2 != 0 || rsa::overlap(Kc, pool_bytes(dm), Vc, pool_bytes(dm))) return RSA_ERR_UNSUPPORTED;
+  return hip_status(rsa::cache_append(dm, T, R, adjacent != 0, inv_freq, Q, K, V, table, lengths, counts, first, Qr, Kc, Vc, st));
+}
+
+size_t rsa_cache_workspace_bytes(const rsa_cache_desc *d) {
+  rsa::CacheDims dm;
+  return cache_validate(d, 1, &dm) == RSA_OK ? rsa::cache_workspace_bytes(dm) : 0;
+}
+
+int rsa_cache_attend(const rsa_cache_desc *d, const void *Q, const void *Kc, const void *Vc, const int32_t *table,
+                     const int32_t *lengths, void *O, float *LSE, void *ws, size_t ws_bytes, void *stream) {
+  RSA_CACHE_PROLOGUE(1, Q && Kc && Vc && table && lengths && O && LSE, Q, Kc, Vc, O, ws);
+  if (!words({table, lengths, LSE})) return RSA_ERR_UNSUPPORTED;
+  const size_t need = rsa::cache_workspace_bytes(dm);
+  if (need > 0 && (!ws || ws_bytes < need)) return RSA_ERR_WORKSPACE;
+  return hip_status(rsa::cache_attend(dm, Q, Kc, Vc, table, lengths, O, LSE, ws, st));
+}
+
+int rsa_cache_join(const rsa_cache_desc *d, int32_t N, const void *Op, const float *LSEp, void *O, float *LSE, void *stream) {
+  RSA_CACHE_PROLOGUE(1, Op && LSEp && O && LSE, Op, O);
+  if (!words({LSEp, LSE})) return RSA_ERR_UNSUPPORTED;
+  if (N < 1) return RSA_ERR_SHAPE;
+  const size_t rows = (size_t)dm.B * dm.Z, es = dm.dtype == RSA_BF16 ? 2 : 4;
+  if (rsa::overlap(LSE, rows * 4, LSEp, N * rows * 4) || rsa::overlap(LSE, rows * 4, Op, N * rows * dm.A * es))
+    return RSA_ERR_UNSUPPORTED;
+  return hip_status(rsa::cache_join(dm, N, Op, LSEp, O, LSE, st));
 }
 
 }  // extern "C"

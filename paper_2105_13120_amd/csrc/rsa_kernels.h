@@ -128,4 +128,23 @@ hipError_t linformer_project(int64_t Zt, int64_t L, int64_t rows, int64_t Kp, in
 hipError_t linformer_project_bwd(int64_t Zt, int64_t L, int64_t rows, int64_t Kp, int A, const void *dXp,
                                  const void *X, const void *E, void *dX, float *dE, hipStream_t st);
 
+// --- rotation by position (ring rows), bf16 and fp32; Q or K may be nullptr ---
+hipError_t rotate_rows(const Dims &d, int dtype, int R, int adjacent, const float *inv_freq, bool back, const void *Q,
+                       const void *K, void *Qr, void *Kr, hipStream_t st);
+
+// --- the paged cache of keys and values ---
+// Derived sizes of a validated rsa_cache_desc and call.
+struct CacheDims {
+  int B, Z, Zkv, A, page, pages, width, dtype;
+  float scale;
+  int64_t qs[3], ks[3], os[3];  // element strides of (batch, head, token) of queries, new keys and values, results
+};
+hipError_t cache_append(const CacheDims &d, int T, int R, int adjacent, const float *inv_freq, const void *Q, const void *K,
+                        const void *V, const int32_t *table, const int32_t *lengths, const int32_t *counts, const int32_t *first,
+                        void *Qr, void *Kc, void *Vc, hipStream_t st);
+size_t cache_workspace_bytes(const CacheDims &d);
+hipError_t cache_attend(const CacheDims &d, const void *Q, const void *Kc, const void *Vc, const int32_t *table,
+                        const int32_t *lengths, void *O, float *LSE, void *ws, hipStream_t st);
+hipError_t cache_join(const CacheDims &d, int N, const void *Op, const float *LSEp, void *O, float *LSE, hipStream_t st);
+
 }  // namespace rsa

@@ -26,6 +26,7 @@ EXPORTS = (
     "rsa_proj_workspace_bytes", "rsa_qkv_proj", "rsa_out_proj", "rsa_out_proj_bwd", "rsa_qkv_proj_bwd",
     "rsa_linformer_workspace_bytes", "rsa_linformer_project", "rsa_linformer_forward",
     "rsa_linformer_backward", "rsa_linformer_project_bwd",
+    "rsa_rotate", "rsa_rotate_bwd", "rsa_cache_append", "rsa_cache_workspace_bytes", "rsa_cache_attend", "rsa_cache_join",
 )
 
 
@@ -35,6 +36,16 @@ class RSADesc(ctypes.Structure):
         ("L", ctypes.c_int64), ("N", ctypes.c_int32),
         ("rank_begin", ctypes.c_int32), ("rank_end", ctypes.c_int32),
         ("causal", ctypes.c_int32), ("dtype", ctypes.c_int32),
+        ("scale", ctypes.c_float), ("flags", ctypes.c_uint32),
+        ("q_stride", ctypes.c_int64 * 3), ("kv_stride", ctypes.c_int64 * 3),
+        ("o_stride", ctypes.c_int64 * 3),
+    ]
+
+
+class CacheDesc(ctypes.Structure):
+    _fields_ = [
+        ("B", ctypes.c_int32), ("Z", ctypes.c_int32), ("Zkv", ctypes.c_int32), ("A", ctypes.c_int32),
+        ("page", ctypes.c_int32), ("pages", ctypes.c_int32), ("width", ctypes.c_int32), ("dtype", ctypes.c_int32),
         ("scale", ctypes.c_float), ("flags", ctypes.c_uint32),
         ("q_stride", ctypes.c_int64 * 3), ("kv_stride", ctypes.c_int64 * 3),
         ("o_stride", ctypes.c_int64 * 3),
@@ -96,6 +107,13 @@ def lib():
         L.rsa_linformer_forward.argtypes = [dp, i] + [vp] * 6
         L.rsa_linformer_backward.argtypes = [dp, i] + [vp] * 10 + [sz, vp]
         L.rsa_linformer_project_bwd.argtypes = [dp, i] + [vp] * 6
+        cp = ctypes.POINTER(CacheDesc)
+        L.rsa_rotate.argtypes = L.rsa_rotate_bwd.argtypes = [dp, i, i] + [vp] * 6
+        L.rsa_cache_append.argtypes = [cp, i] + [vp] * 7 + [i, i] + [vp] * 5
+        L.rsa_cache_workspace_bytes.argtypes = [cp]
+        L.rsa_cache_workspace_bytes.restype = sz
+        L.rsa_cache_attend.argtypes = [cp] + [vp] * 8 + [sz, vp]
+        L.rsa_cache_join.argtypes = [cp, i] + [vp] * 5
         _lib = L
     return _lib
 
@@ -314,3 +332,56 @@ def linformer_project_bwd(desc, dXp, X, E, dX=None, dE=None):
         new = torch.empty_like if (desc.rank_begin, desc.rank_end) == (0, desc.N) else torch.zeros_like
         dX, dE = _like(dX, X, new), _like(dE, E, new, dtype=torch.float32, memory_format=torch.contiguous_format)
     return _done(_native().linformer_project_bwd(desc, dXp, X, E, dX, dE))
+
+
+# ---- rotation of queries and keys by position ----
+def rotate(desc, inv_freq, Q=None, K=None, Qr=None, Kr=None, adjacent=False):
+    """Q (B, Z, Lq, A) and K (B, Z, L, A), either of them or both, with their first 2 * len(inv_freq) elements a head turned by
+    token * inv_freq (fp32).  Pairs are half the turned part apart, with `adjacent` neighbours.  Qr, Kr may be Q, K."""
+    return _rotate(desc, inv_freq, Q, K, Qr, Kr, adjacent, False)
+
+
+def rotate_bwd(desc, inv_freq, dQr=None, dKr=None, dQ=None, dK=None, adjacent=False):
+    """The gradients of `rotate`'s Q and K from those of its results."""
+    return _rotate(desc, inv_freq, dQr, dKr, dQ, dK, adjacent, True)
+
+
+def _rotate(desc, inv_freq, Q, K, Qr, Kr, adjacent, back):
+    Qr, Kr = (r if x is None else _like(r, x) for x, r in ((Q, Qr), (K, Kr)))
+    return _done(_native().rotate(desc, inv_freq, Q, K, Qr, Kr, adjacent, back))
+
+
+# ---- a paged cache of keys and values, attention of one new token per sequence ----
+def make_cache_desc(Kc, table, Z, scale=0.0, Q=None, K=None, O=None):
+    """Descriptor for pools of shape (pages, Zkv, page, A), a table (B, width) and Z query heads.  Q, K, O, when given and not
+    contiguous, supply the strides of Q/Qr, of the new K/V and of O."""
+    pages, Zkv, page, A = Kc.shape
+    B, width = table.shape
+    d = CacheDesc(B, Z, Zkv, A, page, pages, width, _dtype_code(Kc), float(scale), 0)
+    for name, t in (("q_stride", Q), ("kv_stride", K), ("o_stride", O)):
+        if t is not None and not t.is_contiguous():
+            setattr(d, name, _strides(t))
+    return d
+
+
+def cache_append(desc, K, V, Kc, Vc, table, lengths, counts=None, first=None, inv_freq=None, adjacent=False, Q=None, Qr=None):
+    """rsa_cache_append: K, V (B, Zkv, T, A) into the pools' slots lengths - counts .. lengths of every sequence (counts
+    None: T), K turned by its position (first + slot).  Returns Q (B, Z, T, A) turned alike (None without Q); Qr may be Q.
+    Rows of Qr behind a sequence's count are left as they are; in a new tensor they are zero."""
+    if Q is not None and type(Q) not in _PLAIN:
+        Qr = _like(Qr, Q, torch.empty_like if counts is None else torch.zeros_like)
+    return _done(_native().cache_append(desc, K, V, Kc, Vc, table, lengths, counts, first, inv_freq, adjacent, Q, Qr))
+
+
+def cache_workspace_bytes(desc):
+    return int(lib().rsa_cache_workspace_bytes(ctypes.byref(desc)))
+
+
+def cache_attend(desc, Q, Kc, Vc, table, lengths, O=None, LSE=None, ws=None):
+    """rsa_cache_attend: Q (B, Z, 1, A) to the first lengths[b] slots of every sequence.  Returns (O, LSE)."""
+    return _done(_native().cache_attend(desc, Q, Kc, Vc, table, lengths, O, LSE, ws))
+
+
+def cache_join(desc, Op, LSEp, O=None, LSE=None):
+    """rsa_cache_join: results (N, B, Z, 1, A) and (N, B, Z, 1) over N shares of a cache.  Returns (O, LSE)."""
+    return _done(_native().cache_join(desc, Op, LSEp, O, LSE))

@@ -1,0 +1,159 @@
+"""Rotation of queries and keys by position against the fp64 oracle, forward and backward."""
+import numpy as np
+import pytest
+import torch
+
+from cache_helpers import DTYPES, f64, frequencies, normal, rotated_bound, within
+from oracle import cache as oracle
+from paper_2105_13120_amd import rsa
+
+pytestmark = pytest.mark.gpu
+
+CASES = [  # dtype, B, Z, L, N, ranks, A, R, adjacent, zigzag
+    ("bf16", 1, 2, 256, 4, (0, 4), 64, 64, False, False),
+    ("bf16", 1, 1, 64, 1, (0, 1), 64, 64, True, False),           # the shortest sequence, one head
+    ("bf16", 3, 5, 384, 3, (0, 3), 128, 128, False, False),
+    ("bf16", 2, 9, 512, 4, (2, 3), 64, 32, True, False),          # one rank's rows; heads beyond a work-group's eight
+    ("bf16", 2, 3, 1024, 4, (1, 3), 128, 96, False, True),
+    ("bf16", 1, 17, 256, 2, (0, 2), 64, 16, True, True),
+    ("bf16", 1, 2, 128, 2, (0, 2), 128, 20, False, False),        # pairs that are no whole 16 bytes
+    ("bf16", 1, 2, 128, 2, (0, 2), 64, 36, True, False),
+    ("bf16", 2, 3, 128, 2, (1, 2), 64, 2, False, False),
+    ("bf16", 1, 2, 128, 2, (0, 2), 128, 62, True, False),
+    ("bf16", 1, 2, 128, 1, (0, 1), 128, 126, False, False),
+    ("f32", 1, 2, 256, 4, (0, 4), 64, 64, False, False),
+    ("f32", 2, 3, 192, 3, (1, 2), 192, 192, True, False),
+    ("f32", 2, 2, 128, 2, (0, 2), 256, 256, False, False),
+    ("f32", 1, 9, 128, 2, (0, 2), 128, 40, False, False),
+    ("f32", 1, 2, 128, 2, (0, 2), 256, 250, True, False),
+    ("f32", 1, 2, 128, 2, (0, 2), 192, 10, False, False),
+]
+
+
+def setup(case, seed=0):
+    dtype, B, Z, L, N, (rb, re), A, R, adjacent, zigzag = case
+    rng = np.random.default_rng(seed)
+    Q, K = normal(rng, (B, Z, (re - rb) * L // N, A), dtype), normal(rng, (B, Z, L, A), dtype)
+    d = rsa.make_desc(K, N, rank_begin=rb, rank_end=re, zigzag=zigzag, mode=rsa.MODE_STAGED if dtype == "f32" else rsa.MODE_FUSED)
+    pos = oracle.tokens(L, N, rb, re, zigzag), np.arange(L)
+    return d, Q, K, pos, frequencies(R)
+
+
+@pytest.mark.parametrize("case", CASES)
+@pytest.mark.parametrize("back", [False, True])
+def test_against_the_oracle(case, back):
+    dtype, *_, R, adjacent, zigzag = case
+    d, Q, K, pos, f = setup(case)
+    out = (rsa.rotate_bwd if back else rsa.rotate)(d, f.cuda(), Q.cuda(), K.cuda(), adjacent=adjacent)
+    for name, x, p, y in zip("QK", (Q, K), pos, out):
+        ref = oracle.rotate(f64(x), p, f.numpy(), adjacent, back)
+        within(y, ref, rotated_bound(f64(x), ref, R, adjacent, dtype), name)
+        assert torch.equal(y.cpu()[..., R:], x[..., R:])
+
+
+@pytest.mark.parametrize("case", CASES[::3])
+def test_in_place_and_either_alone(case):
+    *_, adjacent, zigzag = case
+    d, Q, K, _, f = setup(case)
+    Q, K, f = Q.cuda(), K.cuda(), f.cuda()
+    Qr, Kr = rsa.rotate(d, f, Q, K, adjacent=adjacent)
+    assert torch.equal(rsa.rotate(d, f, Q, adjacent=adjacent)[0], Qr) and rsa.rotate(d, f, Q)[1] is None
+    assert torch.equal(rsa.rotate(d, f, K=K, adjacent=adjacent)[1], Kr)
+    q, k = Q.clone(), K.clone()
+    a, b = rsa.rotate(d, f, q, k, q, k, adjacent=adjacent)
+    assert a.data_ptr() == q.data_ptr() and torch.equal(q, Qr) and torch.equal(k, Kr)
+
+
+def test_slices_of_a_packed_projection():
+    B, L, Z, A, N = 2, 256, 3, 64, 2
+    g = torch.Generator(device="cuda").manual_seed(3)
+    x = torch.randn(B, L, 3, Z, A, generator=g, device="cuda").bfloat16()
+    Q, K, V = x.permute(2, 0, 3, 1, 4)
+    f = frequencies(A).cuda()
+    d = rsa.make_desc(K, N, Q=Q)
+    plain = rsa.rotate(rsa.make_desc(K.contiguous(), N), f, Q.contiguous(), K.contiguous())
+    before = V.clone()
+    rsa.rotate(d, f, Q, K, Q, K)
+    assert torch.equal(Q, plain[0]) and torch.equal(K, plain[1]) and torch.equal(V, before)
+    with pytest.raises(ValueError, match="has to be given"):
+        rsa.rotate(d, f, Q, K)
+
+
+@pytest.mark.parametrize("dtype,adjacent,R", [("f32", False, 64), ("f32", True, 20)])
+def test_gradient_against_differences(dtype, adjacent, R):
+    """<dy, (f(x + e) - f(x - e)) / 2> = <dx, e>: the rotation is linear, so any step will do."""
+    case = (dtype, 2, 2, 128, 2, (1, 2), 64, R, adjacent, False)
+    d, Q, _, pos, f = setup(case, 5)
+    rng = np.random.default_rng(6)
+    E, dY = normal(rng, Q.shape, dtype).cuda(), normal(rng, Q.shape, dtype).cuda()
+    Q, f = Q.cuda(), f.cuda()
+    up, down = (rsa.rotate(d, f, Q + s * E, adjacent=adjacent)[0].double() for s in (1, -1))
+    dX = rsa.rotate_bwd(d, f, dY, adjacent=adjacent)[0]
+    slope, want = ((up - down) / 2 * dY).sum().item(), (dX.double() * E).sum().item()
+    # both sides: 2^-21 of |x0| + |x1| per element as for the values, x about twice as large after the step
+    tol = 2.0 ** -21 * 4 * (dY.abs().double().sum() * (Q.abs() + E.abs()).max()).item()
+    assert abs(slope - want) <= tol and abs(want) > 10 * tol
+
+
+def test_rotated_scores_depend_on_distance_alone():
+    """Keys and queries that are one vector: the score of tokens i and j is that of any two as far apart."""
+    A, L = 64, 1024
+    x = torch.randn(1, 1, 1, A, generator=torch.Generator().manual_seed(0)).expand(1, 1, L, A).contiguous().cuda()
+    d = rsa.make_desc(x, 1, mode=rsa.MODE_STAGED)
+    q, k = (y[0, 0].double() for y in rsa.rotate(d, frequencies(A).cuda(), x, x))
+    S = q @ k.T
+    want = S[0]
+    for i in (1, 500, 1023):
+        assert (S[i, :i + 1].flip(0) - want[:i + 1]).abs().max() <= 2.0 ** -18 * (x[0, 0, 0].double() ** 2).sum()
+
+
+def test_graph_and_streams():
+    d, Q, K, _, f = setup(CASES[4])
+    Q, K, f = Q.cuda(), K.cuda(), f.cuda()
+    ref = rsa.rotate(d, f, Q, K)
+    q, k = torch.empty_like(Q), torch.empty_like(K)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        rsa.rotate(d, f, Q, K, q, k)
+    side.synchronize()
+    assert torch.equal(q, ref[0]) and torch.equal(k, ref[1])
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        rsa.rotate(d, f, Q, K, q, k)
+    for _ in range(3):
+        q.fill_(float("nan"))
+        k.fill_(float("nan"))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(q, ref[0]) and torch.equal(k, ref[1])
+
+
+def test_rotated_ring_attention_trains():
+    """Rotation, ring attention and its gradients as a training step runs them, zig-zag causal, against fp64 autograd."""
+    B, Z, L, A, N = 1, 2, 256, 64, 2
+    rng = np.random.default_rng(8)
+    Q, K, V, dO = (normal(rng, (B, Z, L, A), "bf16") for _ in range(4))
+    f = frequencies(A)
+    d = rsa.make_desc(K, N, causal=True, zigzag=True)
+    Qr, Kr = rsa.rotate(d, f.cuda(), Q.cuda(), K.cuda())
+    O, LSE = rsa.forward(d, Qr, Kr, V.cuda())
+    dQr, dKr, dV = rsa.backward(d, dO.cuda(), Qr, Kr, V.cuda(), O, LSE)
+    dQ, dK = rsa.rotate_bwd(d, f.cuda(), dQr, dKr)
+
+    tok = torch.from_numpy(oracle.tokens(L, N, 0, N, True))
+    x = [t.double().requires_grad_() for t in (Q, K, V)]
+
+    def turn(t, pos):
+        a = pos.double()[:, None] * f.double()
+        lo, hi = t[..., :A // 2], t[..., A // 2:]
+        return torch.cat([lo * a.cos() - hi * a.sin(), hi * a.cos() + lo * a.sin()], -1)
+    S = turn(x[0], tok) @ turn(x[1], torch.arange(L)).transpose(-1, -2) / 8
+    S = S.masked_fill(torch.arange(L)[None] > tok[:, None], -float("inf"))
+    o = S.softmax(-1) @ x[2]
+    o.backward(dO.double())
+    # bf16 storage of seven tensors in a chain, each rounding 2^-8 / sqrt 3 of the RMS at most and independent: 7^0.5 of it, with
+    # the operands' roundings inside the attention as much again
+    for name, got, want in zip(("O", "dQ", "dK", "dV"), (O, dQ, dK, dV), (o.detach(), *(t.grad for t in x))):
+        err = ((got.cpu().double() - want).square().mean() / want.square().mean()).sqrt().item()
+        assert err <= 2 * 7 ** 0.5 * 2.0 ** -8 / 3 ** 0.5, (name, err)
