@@ -97,61 +97,455 @@ void launch_append(const AppendArgs &a, int W, dim3 grid, hipStream_t st) {
 }
 
 // ---------------------------------------------------------------- attend ----
+// One new token per sequence: S = scale q K^T over the sequence's slots, softmax, O = P V, in one pass with the running
+// maximum and sum.  Every key and value is read once and takes part in 2 group products, so HBM bounds it: at 64 and more
+// bytes in flight per lane the matrix cores and the vector ALU idle.
+//
+// A wave takes tiles of 32 (fp32: 16) slots.  Its products need no LDS and no lane exchange:
+//   S^T = K Q^T   keys are the rows of a 16x16 tile, queries its columns.  K goes from memory to the operand as it lies: lane l
+//                 holds 16 bytes of key l % 16.  Group g = l / 16 receives the scores of keys 4 g .. 4 g + 3 for query l % 16.
+//   O^T = V^T P^T the order of the keys in the sum is free, so the probabilities stay in the lanes that have them: group g
+//                 takes keys 4 g .. 4 g + 3 (bf16: of both halves of the tile), and loads these rows of V, 16 (or 8) bytes each.  Lane m's
+//                 columns are VW m .. VW m + VW - 1, one per product; in bf16 eight rows' elements of one column are put together by
+//                 byte permutes, half an instruction an element.
+// Every accumulator of a lane belongs to its query l % 16: the rescaling by the running maximum is a product by one number.
+// Query heads of one key head are the 16 (or 32) columns; a lone one pays for the unused ones nothing that counts.
 struct AttendArgs {
   const void *Q, *Kc, *Vc;
   const int32_t *table, *lengths;
   void *O;
   float *LSE;
   int64_t qs[3], os[3];
-  FastDiv by_page;
-  int Z, Zkv, group, A, pages, width;
-  float scale;
+  FastDiv by_page, by_tiles;  // by_tiles: query tiles of a key head
+  int B, Z, Zkv, group, pages, width, per;  // per: sequences a thread counts
+  float c;           // scale log2(e)
+  float *part;       // partial results, nullptr: whole segments
+  int4 *joins;
+  uint32_t least;    // units of a share
 };
 
-// One work-group a row: scores of 256 keys at a time, their softmax against the running maximum, their values summed.
-template <typename T>
-__global__ __launch_bounds__(256) void attend_kernel(AttendArgs args) {
-  __shared__ float q[256], p[256], red[8];
-  __shared__ int64_t row[256];
-  const int tid = threadIdx.x, b = blockIdx.x / args.Z, z = blockIdx.x - b * args.Z, h = z / args.group, A = args.A;
-  if (tid < A) q[tid] = (float)static_cast<const T *>(args.Q)[b * args.qs[0] + z * args.qs[1] + tid];
-  const int64_t page = args.by_page.d, most = args.width * page;
-  int64_t len = args.lengths[b];
-  len = len < 0 ? 0 : len < most ? len : most;
-  float m = -INFINITY, sum = 0.f, o = 0.f;
-  for (int64_t j0 = 0; j0 < len; j0 += 256) {
-    __syncthreads();
-    const int64_t j = j0 + tid;
-    float s = -INFINITY;
-    int64_t at = -1;
-    if (j < len) {
-      const uint32_t pg = args.by_page((uint32_t)j);
-      const int id = args.table[(int64_t)b * args.width + pg];
-      if (id >= 0 && id < args.pages) {
-        at = (((int64_t)id * args.Zkv + h) * page + (j - pg * page)) * A;
-        s = 0.f;
-        for (int a = 0; a < A; ++a) s += q[a] * (float)static_cast<const T *>(args.Kc)[at + a];
-        s *= args.scale;
+template <typename T> struct AttendShape;
+template <> struct AttendShape<bf16_t> { static constexpr int kKeys = 32; };
+template <> struct AttendShape<float> { static constexpr int kKeys = 16; };
+constexpr int kAttendWaves = 4;
+
+// Shares of `units` units for `groups` work-groups: the first units % groups have one more.
+struct Shares {
+  uint32_t q, r;
+  __device__ __forceinline__ Shares(uint32_t units, uint32_t groups) : q(units / groups), r(units - units / groups * groups) {}
+  __device__ __forceinline__ uint32_t begin(uint32_t w) const { return w * q + (w < r ? w : r); }
+  __device__ __forceinline__ uint32_t of(uint32_t unit) const {  // (q > 0)
+    return unit < r * (q + 1) ? unit / (q + 1) : r + (unit - r * (q + 1)) / q;
+  }
+};
+
+template <typename T, int A, int NQ>
+struct Attend {
+  static constexpr int kKeys = AttendShape<T>::kKeys, kUnit = kKeys * kAttendWaves;
+  static constexpr bool kHalf = sizeof(T) == 2;
+  static constexpr int VW = kHalf && A % 128 == 0 ? 8 : 4;      // columns of a lane
+  static constexpr int NB = A / (16 * VW);                      // blocks of 16 lanes' columns
+  static constexpr int KT = kHalf ? 2 : 1;                      // 16-key tiles
+  static constexpr int KF = kHalf ? A / 32 : A / 16;            // 16-byte pieces of a key
+  static constexpr int VR = kHalf ? 8 : 4;                      // rows of V of a lane
+  static constexpr int kDw = kHalf ? VW / 2 : VW;               // dwords of a row of V
+  static constexpr int kRow = A + 4;                            // floats of a row in LDS
+  typedef __attribute__((__vector_size__(kDw * sizeof(uint32_t)))) uint32_t VReg;
+
+  struct Lds {
+    float o[kAttendWaves][16][kRow];
+    float m[kAttendWaves][16], l[kAttendWaves][16];
+  };
+
+  const AttendArgs &args;
+  Lds &lds;
+  int lane, wave, g, n16;
+
+  u32x4 q[NQ][KF];
+  f32x4 acc[NQ][NB * VW];
+  float m[NQ], l[NQ];
+  u32x4 kr[KT][KF];
+  VReg vr[VR][NB];
+
+  __device__ __forceinline__ Attend(const AttendArgs &a, Lds &s)
+      : args(a), lds(s), lane(threadIdx.x & 63), wave(threadIdx.x >> 6), g(lane >> 4), n16(lane & 15) {}
+
+  // Rows of the pools of a tile's slots, one slot a lane (lane % kKeys), and which of them are seen, as bits.
+  struct Rows { uint32_t row, seen; };
+  __device__ __forceinline__ Rows rows_of(const int32_t *table, uint32_t len, int h, uint32_t tile) const {
+    const uint32_t slot = tile * kKeys + (lane & (kKeys - 1));
+    const uint32_t pg = args.by_page(slot < len ? slot : 0);
+    const int id = slot < len ? table[pg] : -1;
+    const bool seen = id >= 0 && id < args.pages;
+    Rows r;
+    r.row = seen ? ((uint32_t)id * args.Zkv + h) * args.by_page.d + (slot - pg * args.by_page.d) : 0u;
+    r.seen = (uint32_t)__ballot(seen) & (kKeys == 32 ? ~0u : 0xffffu);
+    return r;
+  }
+  __device__ __forceinline__ void load_k(const Rows &r) {
+#pragma unroll
+    for (int t = 0; t < KT; ++t) {
+      const uint32_t row = __shfl(r.row, 16 * t + n16);
+      const u32x4 *p = reinterpret_cast<const u32x4 *>(static_cast<const T *>(args.Kc) + (uint64_t)row * A) + g;
+#pragma unroll
+      for (int i = 0; i < KF; ++i) kr[t][i] = p[4 * i];
+    }
+  }
+  __device__ __forceinline__ int key_of(int j) const { return 16 * (j >> 2) + 4 * g + (j & 3); }
+  __device__ __forceinline__ void load_v(const Rows &r) {
+#pragma unroll
+    for (int j = 0; j < VR; ++j) {
+      const uint32_t row = __shfl(r.row, key_of(j));
+      const VReg *p = reinterpret_cast<const VReg *>(static_cast<const T *>(args.Vc) + (uint64_t)row * A) + n16;
+#pragma unroll
+      for (int b = 0; b < NB; ++b) vr[j][b] = p[16 * b];
+    }
+  }
+  __device__ __forceinline__ void load_q(int b, int h, int tile) {
+#pragma unroll
+    for (int x = 0; x < NQ; ++x) {
+      const int in = (tile * NQ + x) * 16 + n16;
+      const u32x4 *p = reinterpret_cast<const u32x4 *>(static_cast<const T *>(args.Q) + (int64_t)b * args.qs[0] +
+                                                       (int64_t)(h * args.group + in) * args.qs[1]) + g;
+#pragma unroll
+      for (int i = 0; i < KF; ++i) q[x][i] = in < args.group ? p[4 * i] : u32x4{0, 0, 0, 0};
+    }
+  }
+
+  // Scores of the tile in kr: s[x][j] is key key_of(j)'s
+  __device__ __forceinline__ void scores(f32x4 (&s)[NQ][KT]) {
+#pragma unroll
+    for (int x = 0; x < NQ; ++x)
+#pragma unroll
+      for (int t = 0; t < KT; ++t) {
+        f32x4 a = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < KF; ++i) {
+          if constexpr (kHalf) {
+            a = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kr[t][i]), __builtin_bit_cast(bf16x8, q[x][i]), a, 0, 0, 0);
+          } else {
+            const f32x4 kf = __builtin_bit_cast(f32x4, kr[t][i]), qf = __builtin_bit_cast(f32x4, q[x][i]);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) a = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[e], qf[e], a, 0, 0, 0);
+          }
+        }
+        s[x][t] = a;
+      }
+  }
+  // The running maximum, and s to probabilities relative to it
+  __device__ __forceinline__ void softmax(f32x4 (&s)[NQ][KT], uint32_t seen) {
+    const bool all = seen == (kKeys == 32 ? ~0u : 0xffffu);
+#pragma unroll
+    for (int x = 0; x < NQ; ++x) {
+      if (!all) {
+#pragma unroll
+        for (int t = 0; t < KT; ++t)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) s[x][t][r] = (seen >> (16 * t + 4 * g + r)) & 1 ? s[x][t][r] : -INFINITY;
+      }
+      float top = -INFINITY;
+#pragma unroll
+      for (int t = 0; t < KT; ++t) top = fmaxf(top, fmaxf(fmaxf(s[x][t][0], s[x][t][1]), fmaxf(s[x][t][2], s[x][t][3])));
+      top = fmaxf(top, __shfl_xor(top, 16));
+      top = fmaxf(top, __shfl_xor(top, 32));
+      const float mn = fmaxf(m[x], top * args.c);
+      if (__any(mn > m[x])) {
+        const float keep = __builtin_amdgcn_exp2f(m[x] - (mn == -INFINITY ? 0.f : mn));
+        m[x] = mn;
+        l[x] *= keep;
+#pragma unroll
+        for (int k = 0; k < NB * VW; ++k) acc[x][k] *= keep;
+      }
+      const float ref = m[x] == -INFINITY ? 0.f : m[x];
+#pragma unroll
+      for (int t = 0; t < KT; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          s[x][t][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[x][t][r], args.c, -ref));
+          l[x] += s[x][t][r];
+        }
+    }
+  }
+  __device__ __forceinline__ void add_values(const f32x4 (&p)[NQ][KT], uint32_t seen) {
+    // (0 times what lies in a slot that is not seen could be NaN)
+    if (seen != (kKeys == 32 ? ~0u : 0xffffu)) {
+#pragma unroll
+      for (int j = 0; j < VR; ++j)
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+          for (int e = 0; e < kDw; ++e) vr[j][b][e] = (seen >> key_of(j)) & 1 ? vr[j][b][e] : 0u;
+    }
+    if constexpr (kHalf) {
+      // the probabilities are rounded to bf16, as the matrix core takes them; the sum l keeps them as they were
+      bf16x8 pb[NQ];
+#pragma unroll
+      for (int x = 0; x < NQ; ++x) {
+        const u32x4 w = {pack_bf16(p[x][0][0], p[x][0][1]), pack_bf16(p[x][0][2], p[x][0][3]),
+                         pack_bf16(p[x][KT - 1][0], p[x][KT - 1][1]), pack_bf16(p[x][KT - 1][2], p[x][KT - 1][3])};
+        pb[x] = __builtin_bit_cast(bf16x8, w);
+      }
+#pragma unroll
+      for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int i = 0; i < VW; ++i) {
+          u32x4 w;
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+            w[k] = __builtin_amdgcn_perm(vr[(2 * k + 1) % VR][b][(i >> 1) % kDw], vr[(2 * k) % VR][b][(i >> 1) % kDw],
+                                         i & 1 ? 0x07060302u : 0x05040100u);
+#pragma unroll
+          for (int x = 0; x < NQ; ++x)
+            acc[x][b * VW + i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, w), pb[x], acc[x][b * VW + i], 0, 0, 0);
+        }
+    } else {
+#pragma unroll
+      for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int i = 0; i < VW; ++i)
+#pragma unroll
+          for (int x = 0; x < NQ; ++x)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+              const f32x4 v = __builtin_bit_cast(f32x4, vr[r][b]);  // (as a whole: the cast of an element takes the first)
+              acc[x][b * VW + i] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[i % 4], p[x][0][r], acc[x][b * VW + i], 0, 0, 0);
+            }
+    }
+  }
+
+  // Units [first, first + units) of key head h, query tile `tile`, of sequence b: this wave's tiles are every fourth.
+  // The keys of the next tile are on their way while this one's probabilities are formed, its values while the next scores are,
+  // the rows of the tile behind that one before either.
+  __device__ __forceinline__ void walk(int b, int h, int tile, uint32_t len, uint32_t first, uint32_t units) {
+    const int32_t *table = args.table + (int64_t)b * args.width;
+    uint32_t t = first * kAttendWaves + wave;
+    const uint32_t tiles = (len + kKeys - 1) / kKeys, end = (first + units) * kAttendWaves < tiles ? (first + units) * kAttendWaves : tiles;
+    load_q(b, h, tile);
+#pragma unroll
+    for (int x = 0; x < NQ; ++x) {
+      m[x] = -INFINITY;
+      l[x] = 0.f;
+#pragma unroll
+      for (int k = 0; k < NB * VW; ++k) acc[x][k] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    if (t >= end) return;
+    Rows now = rows_of(table, len, h, t);
+    load_k(now);
+    load_v(now);
+    Rows next = rows_of(table, len, h, t + kAttendWaves);  // (behind the sequence: nothing seen, nothing read)
+    for (;;) {
+      f32x4 s[NQ][KT];
+      scores(s);
+      const bool more = t + kAttendWaves < end;
+      if (more) load_k(next);
+      const Rows after = rows_of(table, len, h, t + 2 * kAttendWaves);
+      softmax(s, now.seen);
+      add_values(s, now.seen);
+      if (!more) break;
+      load_v(next);
+      now = next;
+      next = after;
+      t += kAttendWaves;
+    }
+#pragma unroll
+    for (int x = 0; x < NQ; ++x) {
+      l[x] += __shfl_xor(l[x], 16);
+      l[x] += __shfl_xor(l[x], 32);
+    }
+  }
+
+  // The waves' results together: the segment's row, or (part) one share's
+  __device__ __forceinline__ void finish(int b, int h, int tile, float *part) {
+#pragma unroll
+    for (int x = 0; x < NQ; ++x) {
+      const int rows = args.group - (tile * NQ + x) * 16;  // of this tile
+      __syncthreads();                                     // (LDS is read to the end)
+      if (rows <= 0) break;
+      if (n16 < rows) {
+        if (g == 0) { lds.m[wave][n16] = m[x]; lds.l[wave][n16] = l[x]; }
+        // accumulator (b, i), register r: column b * 16 VW + VW * (4 g + r) + i
+#pragma unroll
+        for (int bl = 0; bl < NB; ++bl)
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+#pragma unroll
+            for (int i = 0; i < VW; i += 4) {
+              const f32x4 v = {acc[x][bl * VW + i][r], acc[x][bl * VW + i + 1][r], acc[x][bl * VW + i + 2][r], acc[x][bl * VW + i + 3][r]};
+              *reinterpret_cast<f32x4 *>(&lds.o[wave][n16][bl * 16 * VW + VW * (4 * g + r) + i]) = v;
+            }
+      }
+      __syncthreads();
+      const int most = rows < 16 ? rows : 16;
+      for (int e = threadIdx.x; e < most * (A / 4); e += 64 * kAttendWaves) {
+        const int row = e / (A / 4), col = (e - row * (A / 4)) * 4;
+        float top = -INFINITY, sum = 0.f;
+#pragma unroll
+        for (int w = 0; w < kAttendWaves; ++w) top = fmaxf(top, lds.m[w][row]);
+        const float ref = top == -INFINITY ? 0.f : top;
+        f32x4 o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int w = 0; w < kAttendWaves; ++w) {
+          const float f = __builtin_amdgcn_exp2f(lds.m[w][row] - ref);
+          sum += f * lds.l[w][row];
+          o += f * *reinterpret_cast<const f32x4 *>(&lds.o[w][row][col]);
+        }
+        if (part) {
+          float *p = part + (size_t)(x * 16 + row) * (A + 4);
+          p[col] = o[0]; p[col + 1] = o[1]; p[col + 2] = o[2]; p[col + 3] = o[3];
+          if (col == 0) { p[A] = top; p[A + 1] = sum; }
+        } else {
+          store_row(args, b, h * args.group + (tile * NQ + x) * 16 + row, col, o, top, sum);
+        }
       }
     }
-    row[tid] = at;
-    const float w = wave_max(s);
-    if ((tid & 63) == 0) red[tid >> 6] = w;
-    __syncthreads();
-    const float mn = fmaxf(fmaxf(m, fmaxf(red[0], red[1])), fmaxf(red[2], red[3])), ref = mn == -INFINITY ? 0.f : mn;
-    const float e = at >= 0 ? expf(s - ref) : 0.f, keep = expf(m - ref), ws = wave_sum(e);
-    p[tid] = e;
-    if ((tid & 63) == 0) red[4 + (tid >> 6)] = ws;
-    __syncthreads();
-    sum = sum * keep + ((red[4] + red[5]) + (red[6] + red[7]));
-    o *= keep;
-    m = mn;
-    if (tid < A)
-      for (int k = 0; k < 256; ++k)
-        if (row[k] >= 0) o += p[k] * (float)static_cast<const T *>(args.Vc)[row[k] + tid];
   }
-  if (tid < A) static_cast<T *>(args.O)[b * args.os[0] + z * args.os[1] + tid] = (T)(sum != 0.f ? o / sum : 0.f);
-  if (tid == 0) args.LSE[blockIdx.x] = sum != 0.f ? m + logf(sum) : -INFINITY;
+
+  // Four columns of a row's result from sums relative to 2^top, and its LSE.
+  static __device__ __forceinline__ void store_row(const AttendArgs &args, int b, int z, int col, f32x4 o, float top, float sum) {
+    const float inv = sum != 0.f ? 1.f / sum : 0.f;
+    T *y = static_cast<T *>(args.O) + (int64_t)b * args.os[0] + (int64_t)z * args.os[1] + col;
+    if constexpr (kHalf) {
+      *reinterpret_cast<u32x2 *>(y) = u32x2{pack_bf16(o[0] * inv, o[1] * inv), pack_bf16(o[2] * inv, o[3] * inv)};
+    } else {
+      *reinterpret_cast<f32x4 *>(y) = o * inv;
+    }
+    if (col == 0) args.LSE[(int64_t)b * args.Z + z] = sum != 0.f ? (top + __builtin_amdgcn_logf(sum)) * kLn2 : -INFINITY;
+  }
+};
+
+__device__ __forceinline__ uint32_t length_of(const AttendArgs &args, int b) {
+  const int n = args.lengths[b], most = args.width * (int)args.by_page.d;
+  return (uint32_t)(n < 0 ? 0 : n < most ? n : most);
+}
+
+// A sequence with no key.
+template <typename T, int A, int NQ> __device__ __forceinline__ void store_empty(const AttendArgs &args, int b) {
+  for (int e = threadIdx.x; e < args.Z * (A / 4); e += 64 * kAttendWaves)
+    Attend<T, A, NQ>::store_row(args, b, e / (A / 4), e % (A / 4) * 4, f32x4{0.f, 0.f, 0.f, 0.f}, -INFINITY, 0.f);
+}
+
+// One work-group a segment: a sequence's key head and query tile.
+template <typename T, int A, int NQ>
+__global__ __launch_bounds__(64 * kAttendWaves, 1) void attend_whole_kernel(AttendArgs args) {
+  typedef Attend<T, A, NQ> At;
+  __shared__ typename At::Lds lds;
+  At at(args, lds);
+  const uint32_t head = args.by_tiles(blockIdx.x), tile = blockIdx.x - head * args.by_tiles.d, b = head / (uint32_t)args.Zkv, h = head - b * args.Zkv;
+  const uint32_t len = length_of(args, b);
+  at.walk(b, h, tile, len, 0, (len + At::kUnit - 1) / At::kUnit);
+  at.finish(b, h, tile, nullptr);
+}
+
+// The work of all segments, in units of kUnit slots, in equal shares: sequences in their order, their key heads and query tiles,
+// their units.  A share may begin and end inside a segment; such parts go to the work-group's two places in the workspace, and the
+// work-group that has a divided segment's beginning writes down for the join where its parts lie.
+template <typename T, int A, int NQ>
+__global__ __launch_bounds__(64 * kAttendWaves, 1) void attend_shares_kernel(AttendArgs args) {
+  typedef Attend<T, A, NQ> At;
+  __shared__ typename At::Lds lds;
+  __shared__ uint32_t sums[kAttendWaves], found[2];
+  At at(args, lds);
+  const uint32_t heads = args.Zkv * args.by_tiles.d, w = blockIdx.x, tid = threadIdx.x;
+  for (int b = w; b < args.B; b += gridDim.x)
+    if (length_of(args, b) == 0) store_empty<T, A, NQ>(args, b);
+  // units before this thread's sequences
+  const int b0 = tid * args.per, b1 = b0 + args.per < args.B ? b0 + args.per : args.B;
+  uint32_t mine = 0;
+  for (int b = b0; b < b1; ++b) mine += (length_of(args, b) + At::kUnit - 1) / At::kUnit;
+  uint32_t upto = mine;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const uint32_t x = __shfl_up(upto, o);
+    if (at.lane >= o) upto += x;
+  }
+  if (at.lane == 63) sums[at.wave] = upto;
+  __syncthreads();
+  uint32_t units = 0;
+#pragma unroll
+  for (int k = 0; k < kAttendWaves; ++k) {
+    if (k < at.wave) upto += sums[k];
+    units += sums[k];
+  }
+  units *= heads;
+  uint32_t groups = (units + args.least - 1) / args.least;
+  groups = groups < gridDim.x ? groups : gridDim.x;
+  if (w >= groups) {
+    if (tid == 0) args.joins[w] = make_int4(-1, 0, 0, 0);
+    return;
+  }
+  const Shares sh(units, groups);
+  uint32_t unit = sh.begin(w);
+  const uint32_t end = sh.begin(w + 1);
+  // the sequence of the first unit
+  if (unit >= (upto - mine) * heads && unit < upto * heads) {
+    uint32_t before = upto - mine;
+    for (int b = b0; b < b1; ++b) {
+      const uint32_t n = (length_of(args, b) + At::kUnit - 1) / At::kUnit;
+      if (unit < (before + n) * heads) { found[0] = b; found[1] = before; break; }
+      before += n;
+    }
+  }
+  __syncthreads();
+  int b = __builtin_amdgcn_readfirstlane(found[0]);
+  uint32_t len = length_of(args, b), n = (len + At::kUnit - 1) / At::kUnit;
+  uint32_t rest = unit - __builtin_amdgcn_readfirstlane(found[1]) * heads, head = rest / n, in = rest - head * n;
+  int4 join = make_int4(-1, 0, 0, 0);
+  const size_t place = (size_t)(args.group < 16 * NQ ? args.group : 16 * NQ) * (A + 4);
+  for (bool begun = false; unit < end; begun = true) {
+    const uint32_t left = end - unit, take = n - in < left ? n - in : left;
+    const uint32_t h = args.by_tiles(head), tile = head - h * args.by_tiles.d;
+    at.walk(b, h, tile, len, in, take);
+    at.finish(b, h, tile, take == n ? nullptr : args.part + (size_t)(2 * w + begun) * place);
+    if (in == 0 && take < n) join = make_int4(b, (int)head, 2 * (int)w + begun, (int)sh.of(unit + n - 1));
+    unit += take;
+    in = 0;
+    if (unit < end && ++head == heads) {
+      head = 0;
+      do len = length_of(args, ++b); while (len == 0);  // (units are left: there is such a sequence)
+      n = (len + At::kUnit - 1) / At::kUnit;
+    }
+  }
+  if (tid == 0) args.joins[w] = join;
+}
+
+// A divided segment's parts: the first at place join.z, then place 2 v of the work-groups v behind it up to join.w.  A wave a row;
+// its halves (quarters) take every second (fourth) part.
+template <typename T, int A, int NQ>
+__global__ __launch_bounds__(64 * kAttendWaves) void attend_join_kernel(AttendArgs args) {
+  const int4 j = args.joins[blockIdx.x];
+  if (j.x < 0) return;
+  const uint32_t head = (uint32_t)j.y, h = args.by_tiles(head), tile = head - h * args.by_tiles.d;
+  const int most = args.group < 16 * NQ ? args.group : 16 * NQ, left = args.group - (int)tile * 16 * NQ, rows = left < most ? left : most;
+  const int row = blockIdx.y * kAttendWaves + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+  if (row >= rows) return;
+  const size_t place = (size_t)most * (A + 4);
+  const int first = j.z >> 1, parts = j.w - first + 1;
+  const float *base = args.part + (size_t)row * (A + 4);
+  auto part = [&](int k) { return base + (size_t)(k == 0 ? j.z : 2 * (first + k)) * place; };
+  float top = -INFINITY;
+  for (int k = lane; k < parts; k += 64) top = fmaxf(top, part(k)[A]);
+  top = wave_max(top);
+  const float ref = top == -INFINITY ? 0.f : top;
+  constexpr int cols = A / 4, teams = cols <= 16 ? 4 : cols <= 32 ? 2 : 1;  // (A = 192: 48 lanes, one team)
+  const int team = lane / (64 / teams), col = (lane - team * (64 / teams)) * 4;
+  float sum = 0.f;
+  f32x4 o = {0.f, 0.f, 0.f, 0.f};
+  if (col < A) {
+#pragma unroll 4
+    for (int k = team; k < parts; k += teams) {
+      const float *p = part(k);
+      const float f = __builtin_amdgcn_exp2f(p[A] - ref);
+      sum += f * p[A + 1];
+      o += f * f32x4{p[col], p[col + 1], p[col + 2], p[col + 3]};
+    }
+  }
+#pragma unroll
+  for (int s = 64 / teams; s < 64; s <<= 1) {
+    sum += __shfl_xor(sum, s);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[e] += __shfl_xor(o[e], s);
+  }
+  if (team == 0 && col < A) Attend<T, A, NQ>::store_row(args, j.x, (int)h * args.group + (int)tile * 16 * NQ + row, col, o, top, sum);
 }
 
 // ------------------------------------------------------------------ join ----
@@ -204,17 +598,75 @@ hipError_t cache_append(const CacheDims &d, int T, int R, int adjacent, const fl
   return hipGetLastError();
 }
 
-size_t cache_workspace_bytes(const CacheDims &) { return 0; }
+namespace {
+
+// How a call's work is laid over the chip, from what the host knows: the table's width, not the lengths.
+struct AttendPlan {
+  int nq, tiles, rows, groups;  // 16-query tiles of a wave; query tiles of a key head and their rows; shares (0: whole segments)
+};
+constexpr int kCUs = 256;
+
+AttendPlan attend_plan(const CacheDims &d) {
+  AttendPlan p;
+  const int group = d.Z / d.Zkv, unit = kAttendWaves * (d.dtype == RSA_BF16 ? AttendShape<bf16_t>::kKeys : AttendShape<float>::kKeys);
+  p.nq = group > 16 && d.A <= 128 ? 2 : 1;  // (two tiles of longer heads do not fit the registers)
+  p.tiles = (group + 16 * p.nq - 1) / (16 * p.nq);
+  p.rows = group < 16 * p.nq ? group : 16 * p.nq;
+  const int64_t slots = (int64_t)d.width * d.page, heads = (int64_t)d.Zkv * p.tiles, units = d.B * (slots / unit + 1) * heads;
+  p.groups = slots <= 512 || d.B > 16384 || units >= (1LL << 31) ? 0 : 2 * kCUs;
+  return p;
+}
+size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
+
+template <typename T, int A, int NQ>
+void launch_attend(const AttendArgs &a, const AttendPlan &p, hipStream_t st) {
+  if (p.groups == 0) {
+    attend_whole_kernel<T, A, NQ><<<a.B * a.Zkv * p.tiles, 64 * kAttendWaves, 0, st>>>(a);
+    return;
+  }
+  attend_shares_kernel<T, A, NQ><<<p.groups, 64 * kAttendWaves, 0, st>>>(a);
+  attend_join_kernel<T, A, NQ><<<dim3(p.groups, (p.rows + kAttendWaves - 1) / kAttendWaves), 64 * kAttendWaves, 0, st>>>(a);
+}
+template <typename T, int A>
+void launch_attend(const AttendArgs &a, const AttendPlan &p, hipStream_t st) {
+  if constexpr (A <= 128) {
+    if (p.nq == 2) return launch_attend<T, A, 2>(a, p, st);
+  }
+  launch_attend<T, A, 1>(a, p, st);
+}
+template <typename T>
+void launch_attend(const AttendArgs &a, const AttendPlan &p, int A, hipStream_t st) {
+  switch (A) {
+    case 64: return launch_attend<T, 64>(a, p, st);
+    case 128: return launch_attend<T, 128>(a, p, st);
+    case 192: return launch_attend<T, 192>(a, p, st);
+    default: return launch_attend<T, 256>(a, p, st);
+  }
+}
+
+}  // namespace
+
+// The join's notes, 16 bytes a share, then two parts of a segment a share: rows of A sums, the maximum, the sum, two unused.
+size_t cache_workspace_bytes(const CacheDims &d) {
+  const AttendPlan p = attend_plan(d);
+  return p.groups == 0 ? 0 : align256(p.groups * sizeof(int4)) + align256((size_t)2 * p.groups * p.rows * (d.A + 4) * 4);
+}
 
 hipError_t cache_attend(const CacheDims &d, const void *Q, const void *Kc, const void *Vc, const int32_t *table,
-                        const int32_t *lengths, void *O, float *LSE, void *, hipStream_t st) {
+                        const int32_t *lengths, void *O, float *LSE, void *ws, hipStream_t st) {
+  const AttendPlan p = attend_plan(d);
   AttendArgs a{};
   a.Q = Q; a.Kc = Kc; a.Vc = Vc; a.table = table; a.lengths = lengths; a.O = O; a.LSE = LSE;
   for (int k = 0; k < 3; ++k) { a.qs[k] = d.qs[k]; a.os[k] = d.os[k]; }
-  a.by_page = make_fast_div(d.page);
-  a.Z = d.Z; a.Zkv = d.Zkv; a.group = d.Z / d.Zkv; a.A = d.A; a.pages = d.pages; a.width = d.width; a.scale = d.scale;
-  if (d.dtype == RSA_BF16) attend_kernel<bf16_t><<<d.B * d.Z, 256, 0, st>>>(a);
-  else attend_kernel<float><<<d.B * d.Z, 256, 0, st>>>(a);
+  a.by_page = make_fast_div(d.page); a.by_tiles = make_fast_div(p.tiles);
+  a.B = d.B; a.Z = d.Z; a.Zkv = d.Zkv; a.group = d.Z / d.Zkv; a.pages = d.pages; a.width = d.width;
+  a.per = (d.B + 64 * kAttendWaves - 1) / (64 * kAttendWaves);
+  a.c = d.scale * kLog2e;
+  a.joins = static_cast<int4 *>(ws);
+  a.part = reinterpret_cast<float *>(static_cast<char *>(ws) + align256(p.groups * sizeof(int4)));
+  a.least = 1;
+  if (d.dtype == RSA_BF16) launch_attend<bf16_t>(a, p, d.A, st);
+  else launch_attend<float>(a, p, d.A, st);
   return hipGetLastError();
 }
 
