@@ -6,6 +6,8 @@
 namespace rsa {
 namespace {
 
+constexpr int kCUs = 256;
+
 // ---------------------------------------------------------------- append ----
 struct AppendArgs {
   const void *Q, *K, *V;
@@ -38,50 +40,71 @@ __device__ __forceinline__ Token token_of(const AppendArgs &a, uint32_t n) {
 template <typename T, int W>
 __global__ __launch_bounds__(256) void append_kernel(AppendArgs args) {
   __shared__ float2 angles[256];
+  constexpr int ahead = kAhead<T, W>;
   const TurnShape &sh = args.shape;
   const uint32_t tid = threadIdx.x, head0 = sh.by_lanes(tid), lane = tid - head0 * sh.lanes, rr = sh.by_units(lane);
   const int u = (int)(lane - rr * sh.by_units.d), heads = 256 / sh.lanes, half = args.ro.R / 2;
-  const uint32_t ar = sh.by_half(tid), ai = tid - ar * sh.by_half.d;  // this thread's angle
   const int2 at = Pair<T, W>::place(args.ro, u);
   const bool turns = u < args.ro.R / (2 * W);
   for (uint32_t tile = blockIdx.x; tile < args.tiles; tile += gridDim.x) {
-    const uint32_t n0 = tile * sh.rows;
-    if (tile != blockIdx.x) __syncthreads();  // (the angles of the tile before are read)
+    const uint32_t n0 = tile * sh.rows, n = n0 + rr;
+    const bool row = rr < (uint32_t)sh.rows && n < args.tokens;
+    // heads of Q, then of K, then of V; the first are on their way while the page is looked up and the angles are worked out
+    const uint32_t b = args.by_T(n), t = n - b * args.by_T.d;
+    const int64_t q = (int64_t)b * args.qs[0] + (int64_t)t * args.qs[2], kv = (int64_t)b * args.ks[0] + (int64_t)t * args.ks[2];
+    const int all = args.Zq + 2 * args.Zkv, step = heads * (int)gridDim.y;
+    const auto source = [&](int h) {
+      if (h < args.Zq) return static_cast<const T *>(args.Q) + q + h * args.qs[1];
+      h -= args.Zq;
+      return h < args.Zkv ? static_cast<const T *>(args.K) + kv + h * args.ks[1]
+                          : static_cast<const T *>(args.V) + kv + (h - args.Zkv) * args.ks[1];
+    };
+    int h = (int)(blockIdx.y * heads + head0);
+    Pair<T, W> p[ahead], q2[ahead];
+    Token tok{};
+    if (row) tok = token_of(args, n);
+    if (!__any(tok.there)) continue;  // (a wave sees all rows of the tile: all waves agree)
+#pragma unroll
+    for (int k = 0; k < ahead; ++k)
+      if (tok.there && h + k * step < all) p[k].load(source(h + k * step), at);
+    if (tile != blockIdx.x) barrier_lds();  // (the angles of the tile before are read)
+    const uint32_t ar = sh.by_half(tid);
     if (half && ar < (uint32_t)sh.rows && n0 + ar < args.tokens) {
       const Token k = token_of(args, n0 + ar);
-      angles[tid] = angle_of(k.slot + (args.first ? args.first[k.b] : 0), args.ro.inv_freq[ai]);
+      angles[tid] = angle_of(k.slot + (args.first ? args.first[k.b] : 0), args.ro.inv_freq[tid - ar * half]);
     }
-    __syncthreads();
-    const uint32_t n = n0 + rr;
-    if (rr >= (uint32_t)sh.rows || n >= args.tokens) continue;
-    const Token k = token_of(args, n);
-    if (!k.there) continue;
+    // where its keys and values go; -1: nowhere
+    int64_t dst = -1;
+    const uint32_t page = args.by_page.d;
+    if (tok.there && tok.slot >= 0 && tok.slot < (int64_t)args.width * page) {
+      const uint32_t pg = args.by_page((uint32_t)tok.slot);
+      const int id = args.table[(int64_t)b * args.width + pg];
+      if (id >= 0 && id < args.pages) dst = ((int64_t)id * args.Zkv * page + ((uint32_t)tok.slot - pg * page)) * args.A;
+    }
+    barrier_lds();
+    if (!tok.there) continue;
     float2 cs[W];
     if (turns) {
 #pragma unroll
       for (int i = 0; i < W; ++i) cs[i] = angles[rr * half + u * W + i];
     }
-    // where its keys and values go; -1: nowhere
-    int64_t dst = -1;
-    const uint32_t page = args.by_page.d;
-    if (k.slot >= 0 && k.slot < (int64_t)args.width * page) {
-      const uint32_t pg = args.by_page((uint32_t)k.slot);
-      const int id = args.table[(int64_t)k.b * args.width + pg];
-      if (id >= 0 && id < args.pages) dst = ((int64_t)id * args.Zkv * page + ((uint32_t)k.slot - pg * page)) * args.A;
-    }
-    const int64_t q = (int64_t)k.b * args.qs[0] + (int64_t)k.t * args.qs[2], kv = (int64_t)k.b * args.ks[0] + (int64_t)k.t * args.ks[2];
-    for (int h = (int)(blockIdx.y * heads + head0); h < args.Zq + 2 * args.Zkv; h += heads * gridDim.y) {
-      const bool query = h < args.Zq, value = h >= args.Zq + args.Zkv;
-      if (!query && dst < 0) break;
-      const int z = query ? h : h - args.Zq - (value ? args.Zkv : 0);
-      const T *src = query ? static_cast<const T *>(args.Q) + q + z * args.qs[1]
-                           : static_cast<const T *>(value ? args.V : args.K) + kv + z * args.ks[1];
-      T *to = query ? static_cast<T *>(args.Qr) + q + z * args.qs[1]
-                    : static_cast<T *>(value ? args.Vc : args.Kc) + dst + (int64_t)z * page * args.A;
-      Pair<T, W> p;
-      p.load(src, at);
-      if (turns && !value) p.turn(cs, args.ro.adjacent);
-      p.store(to, at);
+    for (; h < all; h += ahead * step) {
+      // (loads before stores: a wait for loads counts the stores in front of them)
+#pragma unroll
+      for (int k = 0; k < ahead; ++k)
+        if (h + (ahead + k) * step < all) q2[k].load(source(h + (ahead + k) * step), at);
+#pragma unroll
+      for (int k = 0; k < ahead; ++k) {
+        const int x = h + k * step, z = x - args.Zq, v = z - args.Zkv;
+        if (x < all && (z < 0 || dst >= 0)) {
+          T *to = z < 0 ? static_cast<T *>(args.Qr) + q + x * args.qs[1]
+                        : (v < 0 ? static_cast<T *>(args.Kc) + dst + (int64_t)z * page * args.A
+                                 : static_cast<T *>(args.Vc) + dst + (int64_t)v * page * args.A);
+          if (turns && v < 0) p[k].turn(cs, args.ro.adjacent);
+          p[k].store(to, at);
+        }
+        p[k] = q2[k];
+      }
     }
   }
 }
@@ -91,7 +114,8 @@ void launch_append(const AppendArgs &a, int W, dim3 grid, hipStream_t st) {
   constexpr int wide = sizeof(T) == 2 ? 8 : 4;
   if (W == wide) append_kernel<T, wide><<<grid, 256, 0, st>>>(a);
   else if constexpr (sizeof(T) == 2) {
-    if (W == 2) append_kernel<T, 2><<<grid, 256, 0, st>>>(a);
+    if (W == 4) append_kernel<T, 4><<<grid, 256, 0, st>>>(a);
+    else if (W == 2) append_kernel<T, 2><<<grid, 256, 0, st>>>(a);
     else append_kernel<T, 1><<<grid, 256, 0, st>>>(a);
   } else append_kernel<T, 1><<<grid, 256, 0, st>>>(a);
 }
@@ -117,7 +141,7 @@ struct AttendArgs {
   float *LSE;
   int64_t qs[3], os[3];
   FastDiv by_page, by_tiles;  // by_tiles: query tiles of a key head
-  int B, Z, Zkv, group, pages, width, per;  // per: sequences a thread counts
+  int B, Z, Zkv, group, pages, width, per;  // per: sequences a lane counts
   float c;           // scale log2(e)
   float *part;       // partial results, nullptr: whole segments
   int4 *joins;
@@ -152,6 +176,9 @@ struct Attend {
   static constexpr int kRow = A + 4;                            // floats of a row in LDS
   typedef __attribute__((__vector_size__(kDw * sizeof(uint32_t)))) uint32_t VReg;
 
+  // registers: tile, operands and accumulators, and about 60 more; up to 256 leave room for two waves on a SIMD
+  static constexpr int kSimd = 4 * (KT * KF + NQ * KF + NQ * NB * VW) + VR * NB * kDw + 60 <= 256 ? 2 : 1;
+
   struct Lds {
     float o[kAttendWaves][16][kRow];
     float m[kAttendWaves][16], l[kAttendWaves][16];
@@ -170,13 +197,16 @@ struct Attend {
   __device__ __forceinline__ Attend(const AttendArgs &a, Lds &s)
       : args(a), lds(s), lane(threadIdx.x & 63), wave(threadIdx.x >> 6), g(lane >> 4), n16(lane & 15) {}
 
-  // Rows of the pools of a tile's slots, one slot a lane (lane % kKeys), and which of them are seen, as bits.
+  // Rows of the pools of a tile's slots, one slot a lane (lane % kKeys), and which of them are seen, as bits.  The table's entry is
+  // loaded a tile before it is looked at (slots behind the sequence: the first one's).
   struct Rows { uint32_t row, seen; };
-  __device__ __forceinline__ Rows rows_of(const int32_t *table, uint32_t len, int h, uint32_t tile) const {
+  __device__ __forceinline__ int page_of(const int32_t *table, uint32_t len, uint32_t tile) const {
     const uint32_t slot = tile * kKeys + (lane & (kKeys - 1));
-    const uint32_t pg = args.by_page(slot < len ? slot : 0);
-    const int id = slot < len ? table[pg] : -1;
-    const bool seen = id >= 0 && id < args.pages;
+    return table[args.by_page(slot < len ? slot : 0)];
+  }
+  __device__ __forceinline__ Rows rows_of(int id, uint32_t len, int h, uint32_t tile) const {
+    const uint32_t slot = tile * kKeys + (lane & (kKeys - 1)), pg = args.by_page(slot < len ? slot : 0);
+    const bool seen = slot < len && id >= 0 && id < args.pages;
     Rows r;
     r.row = seen ? ((uint32_t)id * args.Zkv + h) * args.by_page.d + (slot - pg * args.by_page.d) : 0u;
     r.seen = (uint32_t)__ballot(seen) & (kKeys == 32 ? ~0u : 0xffffu);
@@ -188,7 +218,7 @@ struct Attend {
       const uint32_t row = __shfl(r.row, 16 * t + n16);
       const u32x4 *p = reinterpret_cast<const u32x4 *>(static_cast<const T *>(args.Kc) + (uint64_t)row * A) + g;
 #pragma unroll
-      for (int i = 0; i < KF; ++i) kr[t][i] = p[4 * i];
+      for (int i = 0; i < KF; ++i) kr[t][i] = __builtin_nontemporal_load(p + 4 * i);
     }
   }
   __device__ __forceinline__ int key_of(int j) const { return 16 * (j >> 2) + 4 * g + (j & 3); }
@@ -198,7 +228,7 @@ struct Attend {
       const uint32_t row = __shfl(r.row, key_of(j));
       const VReg *p = reinterpret_cast<const VReg *>(static_cast<const T *>(args.Vc) + (uint64_t)row * A) + n16;
 #pragma unroll
-      for (int b = 0; b < NB; ++b) vr[j][b] = p[16 * b];
+      for (int b = 0; b < NB; ++b) vr[j][b] = __builtin_nontemporal_load(p + 16 * b);
     }
   }
   __device__ __forceinline__ void load_q(int b, int h, int tile) {
@@ -315,7 +345,7 @@ struct Attend {
 
   // Units [first, first + units) of key head h, query tile `tile`, of sequence b: this wave's tiles are every fourth.
   // The keys of the next tile are on their way while this one's probabilities are formed, its values while the next scores are,
-  // the rows of the tile behind that one before either.
+  // the table's entries for the tile behind that one before its values.
   __device__ __forceinline__ void walk(int b, int h, int tile, uint32_t len, uint32_t first, uint32_t units) {
     const int32_t *table = args.table + (int64_t)b * args.width;
     uint32_t t = first * kAttendWaves + wave;
@@ -329,24 +359,27 @@ struct Attend {
       for (int k = 0; k < NB * VW; ++k) acc[x][k] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
     if (t >= end) return;
-    Rows now = rows_of(table, len, h, t);
+    Rows now = rows_of(page_of(table, len, t), len, h, t);
     load_k(now);
+    __builtin_amdgcn_sched_barrier(0);  // (issued in the loop's order, which its waits count by)
+    int id = page_of(table, len, t + kAttendWaves);
+    __builtin_amdgcn_sched_barrier(0);
     load_v(now);
-    Rows next = rows_of(table, len, h, t + kAttendWaves);  // (behind the sequence: nothing seen, nothing read)
-    for (;;) {
-      f32x4 s[NQ][KT];
+    __builtin_amdgcn_sched_barrier(0);
+    f32x4 s[NQ][KT];
+    for (; t + kAttendWaves < end; t += kAttendWaves) {  // (the last tile behind the loop: in it, no wait counts loads that may be missing)
       scores(s);
-      const bool more = t + kAttendWaves < end;
-      if (more) load_k(next);
-      const Rows after = rows_of(table, len, h, t + 2 * kAttendWaves);
+      const Rows next = rows_of(id, len, h, t + kAttendWaves);
+      load_k(next);
+      id = page_of(table, len, t + 2 * kAttendWaves);
       softmax(s, now.seen);
       add_values(s, now.seen);
-      if (!more) break;
       load_v(next);
       now = next;
-      next = after;
-      t += kAttendWaves;
     }
+    scores(s);
+    softmax(s, now.seen);
+    add_values(s, now.seen);
 #pragma unroll
     for (int x = 0; x < NQ; ++x) {
       l[x] += __shfl_xor(l[x], 16);
@@ -426,7 +459,7 @@ template <typename T, int A, int NQ> __device__ __forceinline__ void store_empty
 
 // One work-group a segment: a sequence's key head and query tile.
 template <typename T, int A, int NQ>
-__global__ __launch_bounds__(64 * kAttendWaves, 1) void attend_whole_kernel(AttendArgs args) {
+__global__ __launch_bounds__(64 * kAttendWaves, (Attend<T, A, NQ>::kSimd)) void attend_whole_kernel(AttendArgs args) {
   typedef Attend<T, A, NQ> At;
   __shared__ typename At::Lds lds;
   At at(args, lds);
@@ -440,55 +473,50 @@ __global__ __launch_bounds__(64 * kAttendWaves, 1) void attend_whole_kernel(Atte
 // their units.  A share may begin and end inside a segment; such parts go to the work-group's two places in the workspace, and the
 // work-group that has a divided segment's beginning writes down for the join where its parts lie.
 template <typename T, int A, int NQ>
-__global__ __launch_bounds__(64 * kAttendWaves, 1) void attend_shares_kernel(AttendArgs args) {
+__global__ __launch_bounds__(64 * kAttendWaves, (Attend<T, A, NQ>::kSimd)) void attend_shares_kernel(AttendArgs args) {
   typedef Attend<T, A, NQ> At;
   __shared__ typename At::Lds lds;
-  __shared__ uint32_t sums[kAttendWaves], found[2];
   At at(args, lds);
-  const uint32_t heads = args.Zkv * args.by_tiles.d, w = blockIdx.x, tid = threadIdx.x;
-  for (int b = w; b < args.B; b += gridDim.x)
-    if (length_of(args, b) == 0) store_empty<T, A, NQ>(args, b);
-  // units before this thread's sequences
-  const int b0 = tid * args.per, b1 = b0 + args.per < args.B ? b0 + args.per : args.B;
+  const uint32_t heads = args.Zkv * args.by_tiles.d, w = blockIdx.x;
+  // units before this lane's sequences (each wave counts for itself: nothing to wait for)
+  const int b0 = at.lane * args.per, b1 = b0 + args.per < args.B ? b0 + args.per : args.B;
   uint32_t mine = 0;
-  for (int b = b0; b < b1; ++b) mine += (length_of(args, b) + At::kUnit - 1) / At::kUnit;
+  bool empty = false;
+  for (int b = b0; b < b1; ++b) {
+    const uint32_t len = length_of(args, b);
+    empty |= len == 0;
+    mine += (len + At::kUnit - 1) / At::kUnit;
+  }
   uint32_t upto = mine;
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) {
     const uint32_t x = __shfl_up(upto, o);
     if (at.lane >= o) upto += x;
   }
-  if (at.lane == 63) sums[at.wave] = upto;
-  __syncthreads();
-  uint32_t units = 0;
-#pragma unroll
-  for (int k = 0; k < kAttendWaves; ++k) {
-    if (k < at.wave) upto += sums[k];
-    units += sums[k];
-  }
-  units *= heads;
+  const uint32_t units = __builtin_amdgcn_readlane(upto, 63) * heads;
+  if (__any(empty))
+    for (int b = w; b < args.B; b += gridDim.x)
+      if (length_of(args, b) == 0) store_empty<T, A, NQ>(args, b);
   uint32_t groups = (units + args.least - 1) / args.least;
   groups = groups < gridDim.x ? groups : gridDim.x;
   if (w >= groups) {
-    if (tid == 0) args.joins[w] = make_int4(-1, 0, 0, 0);
+    if (threadIdx.x == 0) args.joins[w] = make_int4(-1, 0, 0, 0);
     return;
   }
   const Shares sh(units, groups);
   uint32_t unit = sh.begin(w);
   const uint32_t end = sh.begin(w + 1);
   // the sequence of the first unit
-  if (unit >= (upto - mine) * heads && unit < upto * heads) {
-    uint32_t before = upto - mine;
-    for (int b = b0; b < b1; ++b) {
-      const uint32_t n = (length_of(args, b) + At::kUnit - 1) / At::kUnit;
-      if (unit < (before + n) * heads) { found[0] = b; found[1] = before; break; }
-      before += n;
-    }
+  const int lane = __builtin_ctzll(__ballot(unit < upto * heads));
+  int b = lane * args.per;
+  uint32_t before = __builtin_amdgcn_readlane(upto - mine, lane), len, n;
+  for (;; ++b) {
+    len = __builtin_amdgcn_readfirstlane(length_of(args, b));
+    n = (len + At::kUnit - 1) / At::kUnit;
+    if (unit < (before + n) * heads) break;  // (the lane's sequences hold the unit)
+    before += n;
   }
-  __syncthreads();
-  int b = __builtin_amdgcn_readfirstlane(found[0]);
-  uint32_t len = length_of(args, b), n = (len + At::kUnit - 1) / At::kUnit;
-  uint32_t rest = unit - __builtin_amdgcn_readfirstlane(found[1]) * heads, head = rest / n, in = rest - head * n;
+  uint32_t rest = unit - before * heads, head = rest / n, in = rest - head * n;
   int4 join = make_int4(-1, 0, 0, 0);
   const size_t place = (size_t)(args.group < 16 * NQ ? args.group : 16 * NQ) * (A + 4);
   for (bool begun = false; unit < end; begun = true) {
@@ -501,79 +529,124 @@ __global__ __launch_bounds__(64 * kAttendWaves, 1) void attend_shares_kernel(Att
     in = 0;
     if (unit < end && ++head == heads) {
       head = 0;
-      do len = length_of(args, ++b); while (len == 0);  // (units are left: there is such a sequence)
+      do len = __builtin_amdgcn_readfirstlane(length_of(args, ++b)); while (len == 0);  // (units are left: there is such a sequence)
       n = (len + At::kUnit - 1) / At::kUnit;
     }
   }
-  if (tid == 0) args.joins[w] = join;
+  if (threadIdx.x == 0) args.joins[w] = join;
 }
 
-// A divided segment's parts: the first at place join.z, then place 2 v of the work-groups v behind it up to join.w.  A wave a row;
-// its halves (quarters) take every second (fourth) part.
+// A divided segment's parts: the first at place join.z, then place 2 v of the work-groups v behind it up to join.w.  A work-group a
+// row: teams of A / 4 threads take the parts in turn, four in flight (another XCD has written them: a load is a trip to memory).
 template <typename T, int A, int NQ>
-__global__ __launch_bounds__(64 * kAttendWaves) void attend_join_kernel(AttendArgs args) {
+__global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs args) {
+  constexpr int cols = A / 4, teams = 256 / cols;
+  __shared__ f32x4 sums[teams * cols];
+  __shared__ float2 ends[teams];
   const int4 j = args.joins[blockIdx.x];
   if (j.x < 0) return;
   const uint32_t head = (uint32_t)j.y, h = args.by_tiles(head), tile = head - h * args.by_tiles.d;
-  const int most = args.group < 16 * NQ ? args.group : 16 * NQ, left = args.group - (int)tile * 16 * NQ, rows = left < most ? left : most;
-  const int row = blockIdx.y * kAttendWaves + (threadIdx.x >> 6), lane = threadIdx.x & 63;
-  if (row >= rows) return;
+  const int most = args.group < 16 * NQ ? args.group : 16 * NQ, in = (int)tile * 16 * NQ + blockIdx.y;
+  if (in >= args.group) return;
   const size_t place = (size_t)most * (A + 4);
-  const int first = j.z >> 1, parts = j.w - first + 1;
-  const float *base = args.part + (size_t)row * (A + 4);
-  auto part = [&](int k) { return base + (size_t)(k == 0 ? j.z : 2 * (first + k)) * place; };
-  float top = -INFINITY;
-  for (int k = lane; k < parts; k += 64) top = fmaxf(top, part(k)[A]);
-  top = wave_max(top);
-  const float ref = top == -INFINITY ? 0.f : top;
-  constexpr int cols = A / 4, teams = cols <= 16 ? 4 : cols <= 32 ? 2 : 1;  // (A = 192: 48 lanes, one team)
-  const int team = lane / (64 / teams), col = (lane - team * (64 / teams)) * 4;
-  float sum = 0.f;
+  const int first = j.z >> 1, parts = j.w - first + 1, team = threadIdx.x / cols, col = (threadIdx.x - team * cols) * 4;
+  const float *base = args.part + (size_t)blockIdx.y * (A + 4);
+  float top = -INFINITY, sum = 0.f;
   f32x4 o = {0.f, 0.f, 0.f, 0.f};
-  if (col < A) {
-#pragma unroll 4
-    for (int k = team; k < parts; k += teams) {
-      const float *p = part(k);
-      const float f = __builtin_amdgcn_exp2f(p[A] - ref);
-      sum += f * p[A + 1];
-      o += f * f32x4{p[col], p[col + 1], p[col + 2], p[col + 3]};
+  if (team < teams) {
+    for (int k0 = team; k0 < parts; k0 += 4 * teams) {
+      f32x4 x[4];
+      float2 ml[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const int i = k0 + k * teams;
+        ml[k] = make_float2(-INFINITY, 0.f);
+        x[k] = f32x4{0.f, 0.f, 0.f, 0.f};
+        if (i < parts) {
+          const float *p = base + (size_t)(i == 0 ? j.z : 2 * (first + i)) * place;
+          ml[k] = *reinterpret_cast<const float2 *>(p + A);
+          x[k] = *reinterpret_cast<const f32x4 *>(p + col);
+        }
+      }
+      const float mn = fmaxf(top, fmaxf(fmaxf(ml[0].x, ml[1].x), fmaxf(ml[2].x, ml[3].x)));
+      const float ref = mn == -INFINITY ? 0.f : mn, keep = __builtin_amdgcn_exp2f(top - ref);
+      top = mn;
+      sum *= keep;
+      o *= keep;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const float f = __builtin_amdgcn_exp2f(ml[k].x - ref);
+        sum += f * ml[k].y;
+        o += f * x[k];
+      }
     }
+    sums[threadIdx.x] = o;
+    if (col == 0) ends[team] = make_float2(top, sum);
   }
-#pragma unroll
-  for (int s = 64 / teams; s < 64; s <<= 1) {
-    sum += __shfl_xor(sum, s);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) o[e] += __shfl_xor(o[e], s);
+  __syncthreads();
+  if (team != 0) return;
+  const int used = parts < teams ? parts : teams;
+  for (int k = 1; k < used; ++k) top = fmaxf(top, ends[k].x);
+  const float ref = top == -INFINITY ? 0.f : top;
+  sum = 0.f;
+  o = f32x4{0.f, 0.f, 0.f, 0.f};
+  for (int k = 0; k < used; ++k) {
+    const float f = __builtin_amdgcn_exp2f(ends[k].x - ref);
+    sum += f * ends[k].y;
+    o += f * sums[k * cols + threadIdx.x];
   }
-  if (team == 0 && col < A) Attend<T, A, NQ>::store_row(args, j.x, (int)h * args.group + (int)tile * 16 * NQ + row, col, o, top, sum);
+  Attend<T, A, NQ>::store_row(args, j.x, (int)h * args.group + in, col, o, top, sum);
 }
 
 // ------------------------------------------------------------------ join ----
-// O = sum_n exp(LSE_n - LSE) O_n: a thread takes four elements of a row.
+// O = sum_n exp(LSE_n - LSE) O_n.  Every share is read once: HBM, or for few rows the trips to it, bound this.  A thread takes 16 bytes of a
+// row, A elements, eight shares in flight at a time, against the running maximum.
 template <typename T>
-__global__ __launch_bounds__(256) void join_kernel(const T *Op, const float *LSEp, T *O, float *LSE, uint32_t n4, uint32_t rows, int N,
-                                                   int A, OutLayout lay) {
+__global__ __launch_bounds__(256) void join_kernel(const T *Op, const float *LSEp, T *O, float *LSE, uint32_t units, uint32_t rows, int N,
+                                                   int A, FastDiv by_units, OutLayout lay) {
+  constexpr int W = 16 / sizeof(T), ahead = 8;
   const uint32_t i = blockIdx.x * 256 + threadIdx.x;
-  if (i >= n4) return;
-  const uint32_t row = (uint32_t)(((uint64_t)i * 4) / A);
-  const int a = (int)((uint64_t)i * 4 - (uint64_t)row * A);
-  float m = -INFINITY;
-  for (int n = 0; n < N; ++n) m = fmaxf(m, LSEp[(int64_t)n * rows + row]);
-  const float ref = m == -INFINITY ? 0.f : m;
-  float sum = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
-  for (int n = 0; n < N; ++n) {
-    const float l = LSEp[(int64_t)n * rows + row];
-    if (l == -INFINITY) continue;
-    const float w = expf(l - ref);
-    sum += w;
-    const T *x = Op + ((int64_t)n * rows + row) * A + a;
+  if (i >= units) return;
+  const uint32_t row = by_units(i);
+  const int col = (int)(i - row * by_units.d) * W;
+  const T *x = Op + (int64_t)row * A + col;
+  float top = -INFINITY, sum = 0.f, o[W];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) o[k] += w * (float)x[k];
+  for (int k = 0; k < W; ++k) o[k] = 0.f;
+  for (int n0 = 0; n0 < N; n0 += ahead) {
+    float l[ahead];
+    Chunk<T, W> c[ahead];
+#pragma unroll
+    for (int n = 0; n < ahead; ++n) {
+      l[n] = -INFINITY;
+      if (n0 + n < N) {
+        l[n] = LSEp[(int64_t)(n0 + n) * rows + row] * kLog2e;
+        c[n].load(x + (int64_t)(n0 + n) * rows * A);
+      }
+    }
+    float mn = top;
+#pragma unroll
+    for (int n = 0; n < ahead; ++n) mn = fmaxf(mn, l[n]);
+    const float ref = mn == -INFINITY ? 0.f : mn, keep = __builtin_amdgcn_exp2f(top - ref);
+    top = mn;
+    sum *= keep;
+#pragma unroll
+    for (int k = 0; k < W; ++k) o[k] *= keep;
+#pragma unroll
+    for (int n = 0; n < ahead; ++n) {
+      if (l[n] == -INFINITY) continue;  // (what such a share's row holds counts nothing)
+      const float w = __builtin_amdgcn_exp2f(l[n] - ref);
+      sum += w;
+#pragma unroll
+      for (int k = 0; k < W; ++k) o[k] += w * c[n].get(k);
+    }
   }
-  T *y = O + lay.row_off(row) + a;
+  const float inv = sum != 0.f ? 1.f / sum : 0.f;
+  Chunk<T, W> y;
 #pragma unroll
-  for (int k = 0; k < 4; ++k) y[k] = (T)(sum != 0.f ? o[k] / sum : 0.f);
-  if (a == 0) LSE[row] = sum != 0.f ? m + logf(sum) : -INFINITY;
+  for (int k = 0; k < W; k += 2) y.set2(k, o[k] * inv, o[k + 1] * inv);
+  y.store(O + lay.row_off(row) + col);
+  if (col == 0) LSE[row] = sum != 0.f ? (top + __builtin_amdgcn_logf(sum)) * kLn2 : -INFINITY;
 }
 
 }  // namespace
@@ -587,12 +660,15 @@ hipError_t cache_append(const CacheDims &d, int T, int R, int adjacent, const fl
   for (int k = 0; k < 3; ++k) { a.qs[k] = d.qs[k]; a.ks[k] = d.ks[k]; }
   const int W = chunk_width(d.dtype, R);
   a.ro = {R, adjacent, inv_freq, 1.f};
-  a.shape = make_turn_shape(d.A, R, W);
+  a.shape = make_turn_shape(d.A, R, W, 32);
   a.by_T = make_fast_div(T); a.by_page = make_fast_div(d.page);
   a.B = d.B; a.Zq = Q ? d.Z : 0; a.Zkv = d.Zkv; a.A = d.A; a.pages = d.pages; a.width = d.width;
   a.tokens = (uint32_t)((int64_t)d.B * T);
   a.tiles = (a.tokens + a.shape.rows - 1) / a.shape.rows;
-  const dim3 grid(a.tiles < (1u << 20) ? a.tiles : (1u << 20));
+  // few tokens: their heads go to several work-groups, up to two on a CU
+  const uint32_t heads = 256 / a.shape.lanes, passes = (a.Zq + 2 * a.Zkv + heads - 1) / heads;
+  const uint32_t split = (2 * kCUs + a.tiles - 1) / a.tiles;
+  const dim3 grid(a.tiles < (1u << 20) ? a.tiles : (1u << 20), split < passes ? split : passes);
   if (d.dtype == RSA_BF16) launch_append<bf16_t>(a, W, grid, st);
   else launch_append<float>(a, W, grid, st);
   return hipGetLastError();
@@ -604,8 +680,6 @@ namespace {
 struct AttendPlan {
   int nq, tiles, rows, groups;  // 16-query tiles of a wave; query tiles of a key head and their rows; shares (0: whole segments)
 };
-constexpr int kCUs = 256;
-
 AttendPlan attend_plan(const CacheDims &d) {
   AttendPlan p;
   const int group = d.Z / d.Zkv, unit = kAttendWaves * (d.dtype == RSA_BF16 ? AttendShape<bf16_t>::kKeys : AttendShape<float>::kKeys);
@@ -613,7 +687,7 @@ AttendPlan attend_plan(const CacheDims &d) {
   p.tiles = (group + 16 * p.nq - 1) / (16 * p.nq);
   p.rows = group < 16 * p.nq ? group : 16 * p.nq;
   const int64_t slots = (int64_t)d.width * d.page, heads = (int64_t)d.Zkv * p.tiles, units = d.B * (slots / unit + 1) * heads;
-  p.groups = slots <= 512 || d.B > 16384 || units >= (1LL << 31) ? 0 : 2 * kCUs;
+  p.groups = slots <= 512 || d.B > 4096 || units >= (1LL << 31) ? 0 : 2 * kCUs;
   return p;
 }
 size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
@@ -625,7 +699,7 @@ void launch_attend(const AttendArgs &a, const AttendPlan &p, hipStream_t st) {
     return;
   }
   attend_shares_kernel<T, A, NQ><<<p.groups, 64 * kAttendWaves, 0, st>>>(a);
-  attend_join_kernel<T, A, NQ><<<dim3(p.groups, (p.rows + kAttendWaves - 1) / kAttendWaves), 64 * kAttendWaves, 0, st>>>(a);
+  attend_join_kernel<T, A, NQ><<<dim3(p.groups, p.rows), 256, 0, st>>>(a);
 }
 template <typename T, int A>
 void launch_attend(const AttendArgs &a, const AttendPlan &p, hipStream_t st) {
@@ -660,7 +734,7 @@ hipError_t cache_attend(const CacheDims &d, const void *Q, const void *Kc, const
   for (int k = 0; k < 3; ++k) { a.qs[k] = d.qs[k]; a.os[k] = d.os[k]; }
   a.by_page = make_fast_div(d.page); a.by_tiles = make_fast_div(p.tiles);
   a.B = d.B; a.Z = d.Z; a.Zkv = d.Zkv; a.group = d.Z / d.Zkv; a.pages = d.pages; a.width = d.width;
-  a.per = (d.B + 64 * kAttendWaves - 1) / (64 * kAttendWaves);
+  a.per = (d.B + 63) / 64;
   a.c = d.scale * kLog2e;
   a.joins = static_cast<int4 *>(ws);
   a.part = reinterpret_cast<float *>(static_cast<char *>(ws) + align256(p.groups * sizeof(int4)));
@@ -671,11 +745,13 @@ hipError_t cache_attend(const CacheDims &d, const void *Q, const void *Kc, const
 }
 
 hipError_t cache_join(const CacheDims &d, int N, const void *Op, const float *LSEp, void *O, float *LSE, hipStream_t st) {
-  const uint32_t rows = (uint32_t)(d.B * d.Z), n4 = rows * (uint32_t)(d.A / 4);
+  const int unit = d.dtype == RSA_BF16 ? 8 : 4;
+  const uint32_t rows = (uint32_t)(d.B * d.Z), units = rows * (uint32_t)(d.A / unit);
   const OutLayout lay = make_out_layout(d.os, 1, d.Z);
-  const dim3 grid((n4 + 255) / 256);
-  if (d.dtype == RSA_BF16) join_kernel<<<grid, 256, 0, st>>>((const bf16_t *)Op, LSEp, (bf16_t *)O, LSE, n4, rows, N, d.A, lay);
-  else join_kernel<<<grid, 256, 0, st>>>((const float *)Op, LSEp, (float *)O, LSE, n4, rows, N, d.A, lay);
+  const FastDiv by_units = make_fast_div(d.A / unit);
+  const dim3 grid((units + 255) / 256);
+  if (d.dtype == RSA_BF16) join_kernel<<<grid, 256, 0, st>>>((const bf16_t *)Op, LSEp, (bf16_t *)O, LSE, units, rows, N, d.A, by_units, lay);
+  else join_kernel<<<grid, 256, 0, st>>>((const float *)Op, LSEp, (float *)O, LSE, units, rows, N, d.A, by_units, lay);
   return hipGetLastError();
 }
 

@@ -16,9 +16,10 @@ struct Rotary {
 // the fraction errs by less than 2^-50 of a turn at any position before it is rounded to fp32, once, as a number of at
 // most one half; with the sine's own rounding the results err by less than 2^-22.
 __device__ __forceinline__ float2 angle_of(int64_t pos, float freq) {
+#pragma clang fp contract(off)  // (t is to be the rounded product, whose error te is)
   constexpr double hi = 0.15915494309189535, lo = -9.839338337591243e-18;  // 1 / (2 pi)
-  const double n = (double)pos, p = n * (double)freq, pe = __builtin_fma(n, (double)freq, -p);
-  const double t = p * hi, te = __builtin_fma(p, hi, -t) + (p * lo + pe * hi);
+  const double n = (double)pos, f = (double)freq, p = n * f, pe = __builtin_fma(n, f, -p);
+  const double t = p * hi, te = __builtin_fma(p, hi, -t) + __builtin_fma(p, lo, pe * hi);
   const float x = 2.f * (float)((t - __builtin_rint(t)) + te);
   return make_float2(cospif(x), sinpif(x));
 }
@@ -29,6 +30,15 @@ template <> struct Chunk<bf16_t, 8> {
   u32x4 r;
   __device__ __forceinline__ void load(const bf16_t *p) { r = *reinterpret_cast<const u32x4 *>(p); }
   __device__ __forceinline__ void store(bf16_t *p) const { *reinterpret_cast<u32x4 *>(p) = r; }
+  __device__ __forceinline__ float get(int k) const {
+    return __builtin_bit_cast(float, k & 1 ? r[k >> 1] & 0xffff0000u : r[k >> 1] << 16);
+  }
+  __device__ __forceinline__ void set2(int k, float x, float y) { r[k >> 1] = pack_bf16(x, y); }
+};
+template <> struct Chunk<bf16_t, 4> {
+  u32x2 r;
+  __device__ __forceinline__ void load(const bf16_t *p) { r = *reinterpret_cast<const u32x2 *>(p); }
+  __device__ __forceinline__ void store(bf16_t *p) const { *reinterpret_cast<u32x2 *>(p) = r; }
   __device__ __forceinline__ float get(int k) const {
     return __builtin_bit_cast(float, k & 1 ? r[k >> 1] & 0xffff0000u : r[k >> 1] << 16);
   }
@@ -91,21 +101,23 @@ template <typename T, int W> struct Pair {
 };
 
 // How the 256 threads of a work-group lie over rows and heads: groups of `lanes` threads take one head's `rows` rows,
-// `units` threads a row, 256 / lanes heads at a time.  rows * R / 2 angles are at most 256: one per thread, then shared through LDS
-// by all heads.
+// `units` threads a row, 256 / lanes heads at a time.  The rows' R / 2 angles each are shared through LDS by all heads; there are
+// at most lanes * W.
 struct TurnShape {
   int lanes, rows;
   FastDiv by_lanes, by_units, by_half;  // threads of a group; of a row; R / 2 angles of a row
 };
-// The widest chunks that the pairs allow: 16 bytes, or a pair of elements, or one.
+// The widest chunks that the pairs allow: 16 bytes, a half or a quarter of it, an element.
 inline int chunk_width(int dtype, int R) {
-  const int w = dtype == RSA_BF16 ? 8 : 4;
-  return R % (2 * w) == 0 ? w : dtype == RSA_BF16 && R % 4 == 0 ? 2 : 1;
+  if (dtype != RSA_BF16) return R % 8 == 0 ? 4 : 1;
+  return R % 16 == 0 ? 8 : R % 8 == 0 ? 4 : R % 4 == 0 ? 2 : 1;
 }
-inline TurnShape make_turn_shape(int A, int R, int W) {
+template <typename T, int W> constexpr int kAhead = W * (int)sizeof(T) >= 8 ? 2 : 4;  // heads of a thread whose loads are in flight
+// `least`: threads of a group where they are enough for a row, 32 or 64
+inline TurnShape make_turn_shape(int A, int R, int W, int least) {
   const int units = A / (2 * W);
   TurnShape s;
-  s.lanes = units <= 32 ? 32 : units <= 64 ? 64 : 128;
+  s.lanes = units <= least ? least : units <= 64 ? 64 : 128;
   s.rows = s.lanes / units;
   s.by_lanes = make_fast_div(s.lanes); s.by_units = make_fast_div(units); s.by_half = make_fast_div(R > 1 ? R / 2 : 1);
   return s;

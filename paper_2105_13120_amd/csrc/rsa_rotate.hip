@@ -1,7 +1,8 @@
 // Rotation of queries and keys by position (rsa_rotate, rsa_rotate_bwd).
 //
-// y = x turned by its token's angles: every element is read and written once, so HBM bounds it.  A work-group takes a few rows
-// of one sequence, works out their angles (one a thread) and turns all heads of these rows with them.
+// y = x turned by its token's angles: every element is read and written once, so HBM bounds it.  The angles are the same for all
+// sequences and heads, and 75 instructions each: a work-group takes a few rows, works out their angles (one a thread) and
+// turns a part of all sequences' heads in these rows.
 #include "rsa_kernels.h"
 #include "rsa_rotary.h"
 
@@ -12,63 +13,71 @@ struct Side {  // Q or K
   const void *x;
   void *y;
   int64_t st[3];
-  FastDiv by_rows;  // rows of a sequence
-  uint32_t rows;    // of all sequences
-  uint32_t tiles;
+  uint32_t rows, tiles;  // of a sequence
 };
 struct RotateArgs {
   Side side[2];
   Rotary ro;
   TurnShape shape;
   RowMap map;  // rows of Q
-  int Z;
+  FastDiv by_Z;
+  int heads;   // of all sequences
 };
 
 template <typename T, int W>
 __global__ __launch_bounds__(256) void rotate_kernel(RotateArgs args) {
-  __shared__ float2 angles[256];
+  constexpr int ahead = kAhead<T, W>;
+  __shared__ float2 angles[64 * 8];
   const TurnShape &sh = args.shape;
   const uint32_t tid = threadIdx.x, head0 = sh.by_lanes(tid), lane = tid - head0 * sh.lanes, rr = sh.by_units(lane);
-  const int u = (int)(lane - rr * sh.by_units.d), heads = 256 / sh.lanes;
-  const uint32_t ar = sh.by_half(tid), ai = tid - ar * sh.by_half.d;  // this thread's angle
+  const int u = (int)(lane - rr * sh.by_units.d), heads = 256 / sh.lanes, step = heads * (int)gridDim.y;
+  const bool keys = blockIdx.x >= args.side[0].tiles;
+  const Side &s = args.side[keys ? 1 : 0];
+  const uint32_t n0 = (blockIdx.x - (keys ? args.side[0].tiles : 0u)) * sh.rows, n = n0 + rr;
+  const bool have = rr < (uint32_t)sh.rows && n < s.rows;
   const int2 at = Pair<T, W>::place(args.ro, u);
-  const bool turns = u < args.ro.R / (2 * W);
-  const uint32_t tiles = args.side[0].tiles + args.side[1].tiles;
-  for (uint32_t tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
-    const bool keys = tile >= args.side[0].tiles;
-    const Side &s = args.side[keys ? 1 : 0];
-    const uint32_t n0 = (tile - (keys ? args.side[0].tiles : 0u)) * sh.rows;
-    if (tile != blockIdx.x) __syncthreads();  // (the angles of the tile before are read)
-    if (ar < (uint32_t)sh.rows && n0 + ar < s.rows) {
-      const uint32_t n = n0 + ar, r = n - s.by_rows(n) * s.by_rows.d;
-      const float2 cs = angle_of(keys ? (int64_t)r : args.map((int64_t)r), args.ro.inv_freq[ai]);
-      angles[tid] = make_float2(cs.x, args.ro.sign * cs.y);
-    }
-    __syncthreads();
-    const uint32_t n = n0 + rr;
-    if (rr >= (uint32_t)sh.rows || n >= s.rows) continue;
-    float2 cs[W];
-    if (turns) {
+  const int64_t row = (int64_t)n * s.st[2];
+  const auto offset = [&](int h) { return head_offset((uint32_t)h, args.by_Z, s.st) + row; };
+  // the first heads are on their way while the angles are worked out
+  int h = have ? (int)(blockIdx.y * heads + head0) : args.heads;
+  Pair<T, W> p[ahead], q[ahead];
 #pragma unroll
-      for (int k = 0; k < W; ++k) cs[k] = angles[rr * sh.by_half.d + u * W + k];
-    }
-    const uint32_t b = s.by_rows(n);
-    const int64_t off = (int64_t)b * s.st[0] + (int64_t)(n - b * s.by_rows.d) * s.st[2];
-    for (int h = (int)head0; h < args.Z; h += heads) {
-      Pair<T, W> p;
-      p.load(static_cast<const T *>(s.x) + off + h * s.st[1], at);
-      if (turns) p.turn(cs, args.ro.adjacent);
-      p.store(static_cast<T *>(s.y) + off + h * s.st[1], at);
-    }
+  for (int k = 0; k < ahead; ++k)
+    if (h + k * step < args.heads) p[k].load(static_cast<const T *>(s.x) + offset(h + k * step), at);
+  for (uint32_t e = tid; e < sh.rows * sh.by_half.d; e += 256) {
+    const uint32_t ar = sh.by_half(e);
+    if (n0 + ar >= s.rows) break;
+    const int64_t pos = keys ? (int64_t)(n0 + ar) : args.map((int64_t)(n0 + ar));
+    const float2 cs = angle_of(pos, args.ro.inv_freq[e - ar * sh.by_half.d]);
+    angles[e] = make_float2(cs.x, args.ro.sign * cs.y);
+  }
+  barrier_lds();
+  const bool turns = u < args.ro.R / (2 * W);
+  float2 cs[W];
+#pragma unroll
+  for (int k = 0; k < W; ++k) cs[k] = turns ? angles[(have ? rr * sh.by_half.d : 0u) + u * W + k] : make_float2(1.f, 0.f);
+  for (; h < args.heads; h += ahead * step) {
+    // (loads before stores: a wait for loads counts the stores in front of them)
+#pragma unroll
+    for (int k = 0; k < ahead; ++k)
+      if (h + (ahead + k) * step < args.heads) q[k].load(static_cast<const T *>(s.x) + offset(h + (ahead + k) * step), at);
+#pragma unroll
+    for (int k = 0; k < ahead; ++k)
+      if (h + k * step < args.heads) {
+        if (turns) p[k].turn(cs, args.ro.adjacent);
+        p[k].store(static_cast<T *>(s.y) + offset(h + k * step), at);
+        p[k] = q[k];
+      }
   }
 }
 
 template <typename T>
-void launch(const RotateArgs &a, int W, unsigned grid, hipStream_t st) {
+void launch(const RotateArgs &a, int W, dim3 grid, hipStream_t st) {
   constexpr int wide = sizeof(T) == 2 ? 8 : 4;
   if (W == wide) rotate_kernel<T, wide><<<grid, 256, 0, st>>>(a);
   else if constexpr (sizeof(T) == 2) {
-    if (W == 2) rotate_kernel<T, 2><<<grid, 256, 0, st>>>(a);
+    if (W == 4) rotate_kernel<T, 4><<<grid, 256, 0, st>>>(a);
+    else if (W == 2) rotate_kernel<T, 2><<<grid, 256, 0, st>>>(a);
     else rotate_kernel<T, 1><<<grid, 256, 0, st>>>(a);
   } else rotate_kernel<T, 1><<<grid, 256, 0, st>>>(a);
 }
@@ -80,21 +89,20 @@ hipError_t rotate_rows(const Dims &d, int dtype, int R, int adjacent, const floa
   const int W = chunk_width(dtype, R);
   RotateArgs a{};
   a.ro = {R, adjacent, inv_freq, back ? -1.f : 1.f};
-  a.shape = make_turn_shape(d.A, R, W);
+  a.shape = make_turn_shape(d.A, R, W, 64);
   a.map = make_row_map(d);
-  a.Z = d.Z;
+  a.by_Z = make_fast_div(d.Z);
+  a.heads = d.B * d.Z;
   for (int i = 0; i < 2; ++i) {
     Side &s = a.side[i];
-    const int64_t rows = i ? d.L : d.Lq;
     s.x = i ? K : Q; s.y = i ? Kr : Qr;
     for (int k = 0; k < 3; ++k) s.st[k] = i ? d.ks[k] : d.qs[k];
-    s.by_rows = make_fast_div(rows);
-    s.rows = s.x ? (uint32_t)(d.B * rows) : 0;
+    s.rows = s.x ? (uint32_t)(i ? d.L : d.Lq) : 0;
     s.tiles = (s.rows + a.shape.rows - 1) / a.shape.rows;
   }
-  const uint64_t tiles = (uint64_t)a.side[0].tiles + a.side[1].tiles;
-  const unsigned grid = (unsigned)(tiles < (1u << 20) ? tiles : (1u << 20));
-  if (grid == 0) return hipSuccess;
+  const uint32_t tiles = a.side[0].tiles + a.side[1].tiles, heads = 256 / a.shape.lanes, passes = (a.heads + heads - 1) / heads;
+  const uint32_t split = (4 * 256 + tiles - 1) / tiles;  // (few rows: the heads go to several work-groups, up to four on a CU)
+  const dim3 grid(tiles, split < passes ? split : passes);
   if (dtype == RSA_BF16) launch<bf16_t>(a, W, grid, st);
   else launch<float>(a, W, grid, st);
   return hipGetLastError();
