@@ -274,10 +274,12 @@ void check(int i, const at::Tensor &t, at::ScalarType type, at::IntArrayRef shap
 }
 // ... and that they are where the work is enqueued
 void check_device(const Call &c, int n) {
+  int current = -1;  // (asked for once a tensor of a GPU is there)
   for (int i = 1; i < n; ++i)
     if (THPVariable_Check(c.args[i])) {
-      const at::Tensor &t = c.tensor(i);
-      if (!t.is_cuda() || t.get_device() != c10::hip::getCurrentHIPStream().device_index()) {
+      const at::Tensor &t = THPVariable_Unpack(c.args[i]);
+      if (t.is_cuda() && current < 0) current = c10::hip::getCurrentHIPStream().device_index();
+      if (!t.is_cuda() || t.get_device() != current) {
         PyErr_Format(PyExc_AssertionError, "argument %d: a tensor of the current GPU expected", i);
         throw Refused{};
       }

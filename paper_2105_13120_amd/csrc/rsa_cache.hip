@@ -145,13 +145,11 @@ struct AttendArgs {
   float c;           // scale log2(e)
   float *part;       // partial results, nullptr: whole segments
   int4 *joins;
-  uint32_t least;    // units of a share
 };
 
 template <typename T> struct AttendShape;
 template <> struct AttendShape<bf16_t> { static constexpr int kKeys = 32; };
 template <> struct AttendShape<float> { static constexpr int kKeys = 16; };
-constexpr int kAttendWaves = 4;
 
 // Shares of `units` units for `groups` work-groups: the first units % groups have one more.
 struct Shares {
@@ -163,9 +161,17 @@ struct Shares {
   }
 };
 
+// The larger of lanes l and l ^ 16: v_permlane16_swap exchanges the odd rows of 16 lanes of its first operand with the even ones of
+// its second.
+__device__ __forceinline__ float xrow_max(float x) {
+  uint32_t a = __builtin_bit_cast(uint32_t, x), b = a;
+  asm volatile("s_nop 1\n\tv_permlane16_swap_b32 %0, %1" : "+v"(a), "+v"(b));
+  return fmaxf(__builtin_bit_cast(float, a), __builtin_bit_cast(float, b));
+}
+
 template <typename T, int A, int NQ>
 struct Attend {
-  static constexpr int kKeys = AttendShape<T>::kKeys, kUnit = kKeys * kAttendWaves;
+  static constexpr int kKeys = AttendShape<T>::kKeys;
   static constexpr bool kHalf = sizeof(T) == 2;
   static constexpr int VW = kHalf && A % 128 == 0 ? 8 : 4;      // columns of a lane
   static constexpr int NB = A / (16 * VW);                      // blocks of 16 lanes' columns
@@ -176,12 +182,14 @@ struct Attend {
   static constexpr int kRow = A + 4;                            // floats of a row in LDS
   typedef __attribute__((__vector_size__(kDw * sizeof(uint32_t)))) uint32_t VReg;
 
-  // registers: tile, operands and accumulators, and about 60 more; up to 256 leave room for two waves on a SIMD
-  static constexpr int kSimd = 4 * (KT * KF + NQ * KF + NQ * NB * VW) + VR * NB * kDw + 60 <= 256 ? 2 : 1;
+  // registers: tile, operands and accumulators, and about 60 more; of 512 a SIMD has room for these waves
+  static constexpr int kRegs = 4 * (KT * KF + NQ * KF + NQ * NB * VW) + VR * NB * kDw + 60;
+  static constexpr int kSimd = kRegs <= 128 ? 4 : kRegs <= 256 ? 2 : 1;
+  static constexpr int kWaves = 4, kTiles = kWaves, kUnit = kKeys * kTiles;
 
   struct Lds {
-    float o[kAttendWaves][16][kRow];
-    float m[kAttendWaves][16], l[kAttendWaves][16];
+    float o[kWaves][16][kRow];
+    float m[kWaves][16], l[kWaves][16];
   };
 
   const AttendArgs &args;
@@ -213,20 +221,26 @@ struct Attend {
     return r;
   }
   __device__ __forceinline__ void load_k(const Rows &r) {
+    uint32_t row[KT];
+#pragma unroll
+    for (int t = 0; t < KT; ++t) row[t] = __shfl(r.row, 16 * t + n16);
+    __builtin_amdgcn_sched_barrier(0);  // (one wait for all of them)
 #pragma unroll
     for (int t = 0; t < KT; ++t) {
-      const uint32_t row = __shfl(r.row, 16 * t + n16);
-      const u32x4 *p = reinterpret_cast<const u32x4 *>(static_cast<const T *>(args.Kc) + (uint64_t)row * A) + g;
+      const u32x4 *p = reinterpret_cast<const u32x4 *>(static_cast<const T *>(args.Kc) + (uint64_t)row[t] * A) + g;
 #pragma unroll
       for (int i = 0; i < KF; ++i) kr[t][i] = __builtin_nontemporal_load(p + 4 * i);
     }
   }
   __device__ __forceinline__ int key_of(int j) const { return 16 * (j >> 2) + 4 * g + (j & 3); }
   __device__ __forceinline__ void load_v(const Rows &r) {
+    uint32_t row[VR];
+#pragma unroll
+    for (int j = 0; j < VR; ++j) row[j] = __shfl(r.row, key_of(j));
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int j = 0; j < VR; ++j) {
-      const uint32_t row = __shfl(r.row, key_of(j));
-      const VReg *p = reinterpret_cast<const VReg *>(static_cast<const T *>(args.Vc) + (uint64_t)row * A) + n16;
+      const VReg *p = reinterpret_cast<const VReg *>(static_cast<const T *>(args.Vc) + (uint64_t)row[j] * A) + n16;
 #pragma unroll
       for (int b = 0; b < NB; ++b) vr[j][b] = __builtin_nontemporal_load(p + 16 * b);
     }
@@ -276,8 +290,7 @@ struct Attend {
       float top = -INFINITY;
 #pragma unroll
       for (int t = 0; t < KT; ++t) top = fmaxf(top, fmaxf(fmaxf(s[x][t][0], s[x][t][1]), fmaxf(s[x][t][2], s[x][t][3])));
-      top = fmaxf(top, __shfl_xor(top, 16));
-      top = fmaxf(top, __shfl_xor(top, 32));
+      top = xhalf_max(xrow_max(top));
       const float mn = fmaxf(m[x], top * args.c);
       if (__any(mn > m[x])) {
         const float keep = __builtin_amdgcn_exp2f(m[x] - (mn == -INFINITY ? 0.f : mn));
@@ -343,13 +356,12 @@ struct Attend {
     }
   }
 
-  // Units [first, first + units) of key head h, query tile `tile`, of sequence b: this wave's tiles are every fourth.
+  // Tiles [t, end) of key head h, query tile `tile`, of sequence b: this wave's are every fourth.
   // The keys of the next tile are on their way while this one's probabilities are formed, its values while the next scores are,
   // the table's entries for the tile behind that one before its values.
-  __device__ __forceinline__ void walk(int b, int h, int tile, uint32_t len, uint32_t first, uint32_t units) {
+  __device__ __forceinline__ void walk(int b, int h, int tile, uint32_t len, uint32_t t, uint32_t end) {
     const int32_t *table = args.table + (int64_t)b * args.width;
-    uint32_t t = first * kAttendWaves + wave;
-    const uint32_t tiles = (len + kKeys - 1) / kKeys, end = (first + units) * kAttendWaves < tiles ? (first + units) * kAttendWaves : tiles;
+    t += wave;
     load_q(b, h, tile);
 #pragma unroll
     for (int x = 0; x < NQ; ++x) {
@@ -362,16 +374,16 @@ struct Attend {
     Rows now = rows_of(page_of(table, len, t), len, h, t);
     load_k(now);
     __builtin_amdgcn_sched_barrier(0);  // (issued in the loop's order, which its waits count by)
-    int id = page_of(table, len, t + kAttendWaves);
+    int id = page_of(table, len, t + kWaves);
     __builtin_amdgcn_sched_barrier(0);
     load_v(now);
     __builtin_amdgcn_sched_barrier(0);
     f32x4 s[NQ][KT];
-    for (; t + kAttendWaves < end; t += kAttendWaves) {  // (the last tile behind the loop: in it, no wait counts loads that may be missing)
+    for (; t + kWaves < end; t += kWaves) {  // (the last tile behind the loop: in it, no wait counts loads that may be missing)
       scores(s);
-      const Rows next = rows_of(id, len, h, t + kAttendWaves);
+      const Rows next = rows_of(id, len, h, t + kWaves);
       load_k(next);
-      id = page_of(table, len, t + 2 * kAttendWaves);
+      id = page_of(table, len, t + 2 * kWaves);
       softmax(s, now.seen);
       add_values(s, now.seen);
       load_v(next);
@@ -409,23 +421,23 @@ struct Attend {
       }
       __syncthreads();
       const int most = rows < 16 ? rows : 16;
-      for (int e = threadIdx.x; e < most * (A / 4); e += 64 * kAttendWaves) {
+      for (int e = threadIdx.x; e < most * (A / 4); e += 64 * kWaves) {
         const int row = e / (A / 4), col = (e - row * (A / 4)) * 4;
         float top = -INFINITY, sum = 0.f;
 #pragma unroll
-        for (int w = 0; w < kAttendWaves; ++w) top = fmaxf(top, lds.m[w][row]);
+        for (int w = 0; w < kWaves; ++w) top = fmaxf(top, lds.m[w][row]);
         const float ref = top == -INFINITY ? 0.f : top;
         f32x4 o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int w = 0; w < kAttendWaves; ++w) {
+        for (int w = 0; w < kWaves; ++w) {
           const float f = __builtin_amdgcn_exp2f(lds.m[w][row] - ref);
           sum += f * lds.l[w][row];
           o += f * *reinterpret_cast<const f32x4 *>(&lds.o[w][row][col]);
         }
         if (part) {
           float *p = part + (size_t)(x * 16 + row) * (A + 4);
-          p[col] = o[0]; p[col + 1] = o[1]; p[col + 2] = o[2]; p[col + 3] = o[3];
-          if (col == 0) { p[A] = top; p[A + 1] = sum; }
+          *reinterpret_cast<f32x4 *>(p + col) = o;
+          if (col == 0) *reinterpret_cast<float2 *>(p + A) = make_float2(top, sum);
         } else {
           store_row(args, b, h * args.group + (tile * NQ + x) * 16 + row, col, o, top, sum);
         }
@@ -453,27 +465,27 @@ __device__ __forceinline__ uint32_t length_of(const AttendArgs &args, int b) {
 
 // A sequence with no key.
 template <typename T, int A, int NQ> __device__ __forceinline__ void store_empty(const AttendArgs &args, int b) {
-  for (int e = threadIdx.x; e < args.Z * (A / 4); e += 64 * kAttendWaves)
+  for (int e = threadIdx.x; e < args.Z * (A / 4); e += 64 * Attend<T, A, NQ>::kWaves)
     Attend<T, A, NQ>::store_row(args, b, e / (A / 4), e % (A / 4) * 4, f32x4{0.f, 0.f, 0.f, 0.f}, -INFINITY, 0.f);
 }
 
 // One work-group a segment: a sequence's key head and query tile.
 template <typename T, int A, int NQ>
-__global__ __launch_bounds__(64 * kAttendWaves, (Attend<T, A, NQ>::kSimd)) void attend_whole_kernel(AttendArgs args) {
+__global__ __launch_bounds__((64 * Attend<T, A, NQ>::kWaves), (Attend<T, A, NQ>::kSimd)) void attend_whole_kernel(AttendArgs args) {
   typedef Attend<T, A, NQ> At;
   __shared__ typename At::Lds lds;
   At at(args, lds);
   const uint32_t head = args.by_tiles(blockIdx.x), tile = blockIdx.x - head * args.by_tiles.d, b = head / (uint32_t)args.Zkv, h = head - b * args.Zkv;
   const uint32_t len = length_of(args, b);
-  at.walk(b, h, tile, len, 0, (len + At::kUnit - 1) / At::kUnit);
+  at.walk(b, h, tile, len, 0, (len + At::kKeys - 1) / At::kKeys);
   at.finish(b, h, tile, nullptr);
 }
 
-// The work of all segments, in units of kUnit slots, in equal shares: sequences in their order, their key heads and query tiles,
+// The work of all segments, in units of kKeys slots, in equal shares: sequences in their order, their key heads and query tiles,
 // their units.  A share may begin and end inside a segment; such parts go to the work-group's two places in the workspace, and the
 // work-group that has a divided segment's beginning writes down for the join where its parts lie.
 template <typename T, int A, int NQ>
-__global__ __launch_bounds__(64 * kAttendWaves, (Attend<T, A, NQ>::kSimd)) void attend_shares_kernel(AttendArgs args) {
+__global__ __launch_bounds__((64 * Attend<T, A, NQ>::kWaves), (Attend<T, A, NQ>::kSimd)) void attend_shares_kernel(AttendArgs args) {
   typedef Attend<T, A, NQ> At;
   __shared__ typename At::Lds lds;
   At at(args, lds);
@@ -497,8 +509,10 @@ __global__ __launch_bounds__(64 * kAttendWaves, (Attend<T, A, NQ>::kSimd)) void 
   if (__any(empty))
     for (int b = w; b < args.B; b += gridDim.x)
       if (length_of(args, b) == 0) store_empty<T, A, NQ>(args, b);
-  uint32_t groups = (units + args.least - 1) / args.least;
+  // one share a CU, a second (third) where each then still has four units
+  uint32_t groups = kCUs * (1 + units / (4 * kCUs));
   groups = groups < gridDim.x ? groups : gridDim.x;
+  groups = groups < units ? groups : units;
   if (w >= groups) {
     if (threadIdx.x == 0) args.joins[w] = make_int4(-1, 0, 0, 0);
     return;
@@ -522,7 +536,7 @@ __global__ __launch_bounds__(64 * kAttendWaves, (Attend<T, A, NQ>::kSimd)) void 
   for (bool begun = false; unit < end; begun = true) {
     const uint32_t left = end - unit, take = n - in < left ? n - in : left;
     const uint32_t h = args.by_tiles(head), tile = head - h * args.by_tiles.d;
-    at.walk(b, h, tile, len, in, take);
+    at.walk(b, h, tile, len, in * At::kTiles, take == n - in ? (len + At::kKeys - 1) / At::kKeys : (in + take) * At::kTiles);
     at.finish(b, h, tile, take == n ? nullptr : args.part + (size_t)(2 * w + begun) * place);
     if (in == 0 && take < n) join = make_int4(b, (int)head, 2 * (int)w + begun, (int)sh.of(unit + n - 1));
     unit += take;
@@ -537,47 +551,56 @@ __global__ __launch_bounds__(64 * kAttendWaves, (Attend<T, A, NQ>::kSimd)) void 
 }
 
 // A divided segment's parts: the first at place join.z, then place 2 v of the work-groups v behind it up to join.w.  A work-group a
-// row: teams of A / 4 threads take the parts in turn, four in flight (another XCD has written them: a load is a trip to memory).
+// row: teams of A / 4 threads take the parts in turn, eight in flight (another XCD has written them: a load is a trip to memory).
 template <typename T, int A, int NQ>
 __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs args) {
   constexpr int cols = A / 4, teams = 256 / cols;
   __shared__ f32x4 sums[teams * cols];
   __shared__ float2 ends[teams];
-  const int4 j = args.joins[blockIdx.x];
+  const int w = blockIdx.x, most = args.group < 16 * NQ ? args.group : 16 * NQ, team = threadIdx.x / cols, col = (threadIdx.x - team * cols) * 4;
+  const size_t place = (size_t)most * (A + 4);
+  const float *base = args.part + (size_t)blockIdx.y * (A + 4);
+  struct Part {
+    f32x4 o;
+    float2 ml;
+    __device__ __forceinline__ void load(const float *p, int col) {
+      ml = *reinterpret_cast<const float2 *>(p + A);
+      o = *reinterpret_cast<const f32x4 *>(p + col);
+    }
+    __device__ __forceinline__ void none() {
+      ml = make_float2(-INFINITY, 0.f);
+      o = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+  };
+  const int4 j = args.joins[w];
   if (j.x < 0) return;
   const uint32_t head = (uint32_t)j.y, h = args.by_tiles(head), tile = head - h * args.by_tiles.d;
-  const int most = args.group < 16 * NQ ? args.group : 16 * NQ, in = (int)tile * 16 * NQ + blockIdx.y;
+  const int in = (int)tile * 16 * NQ + blockIdx.y, parts = j.w - w + 1;
   if (in >= args.group) return;
-  const size_t place = (size_t)most * (A + 4);
-  const int first = j.z >> 1, parts = j.w - first + 1, team = threadIdx.x / cols, col = (threadIdx.x - team * cols) * 4;
-  const float *base = args.part + (size_t)blockIdx.y * (A + 4);
   float top = -INFINITY, sum = 0.f;
   f32x4 o = {0.f, 0.f, 0.f, 0.f};
   if (team < teams) {
-    for (int k0 = team; k0 < parts; k0 += 4 * teams) {
-      f32x4 x[4];
-      float2 ml[4];
+    constexpr int ahead = 8;
+    for (int k0 = team; k0 < parts; k0 += ahead * teams) {
+      Part x[ahead];
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
+      for (int k = 0; k < ahead; ++k) {
         const int i = k0 + k * teams;
-        ml[k] = make_float2(-INFINITY, 0.f);
-        x[k] = f32x4{0.f, 0.f, 0.f, 0.f};
-        if (i < parts) {
-          const float *p = base + (size_t)(i == 0 ? j.z : 2 * (first + i)) * place;
-          ml[k] = *reinterpret_cast<const float2 *>(p + A);
-          x[k] = *reinterpret_cast<const f32x4 *>(p + col);
-        }
+        if (i < parts) x[k].load(base + (size_t)(i == 0 ? j.z : 2 * (w + i)) * place, col);
+        else x[k].none();
       }
-      const float mn = fmaxf(top, fmaxf(fmaxf(ml[0].x, ml[1].x), fmaxf(ml[2].x, ml[3].x)));
+      float mn = top;
+#pragma unroll
+      for (int k = 0; k < ahead; ++k) mn = fmaxf(mn, x[k].ml.x);
       const float ref = mn == -INFINITY ? 0.f : mn, keep = __builtin_amdgcn_exp2f(top - ref);
       top = mn;
       sum *= keep;
       o *= keep;
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const float f = __builtin_amdgcn_exp2f(ml[k].x - ref);
-        sum += f * ml[k].y;
-        o += f * x[k];
+      for (int k = 0; k < ahead; ++k) {
+        const float f = __builtin_amdgcn_exp2f(x[k].ml.x - ref);
+        sum += f * x[k].ml.y;
+        o += f * x[k].o;
       }
     }
     sums[threadIdx.x] = o;
@@ -680,14 +703,15 @@ namespace {
 struct AttendPlan {
   int nq, tiles, rows, groups;  // 16-query tiles of a wave; query tiles of a key head and their rows; shares (0: whole segments)
 };
+int attend_most(const CacheDims &d) { return d.A == 64 ? 3 : d.A == 256 ? 1 : 2; }
 AttendPlan attend_plan(const CacheDims &d) {
   AttendPlan p;
-  const int group = d.Z / d.Zkv, unit = kAttendWaves * (d.dtype == RSA_BF16 ? AttendShape<bf16_t>::kKeys : AttendShape<float>::kKeys);
+  const int group = d.Z / d.Zkv, unit = 16;  // (of at least that many slots)
   p.nq = group > 16 && d.A <= 128 ? 2 : 1;  // (two tiles of longer heads do not fit the registers)
   p.tiles = (group + 16 * p.nq - 1) / (16 * p.nq);
   p.rows = group < 16 * p.nq ? group : 16 * p.nq;
   const int64_t slots = (int64_t)d.width * d.page, heads = (int64_t)d.Zkv * p.tiles, units = d.B * (slots / unit + 1) * heads;
-  p.groups = slots <= 512 || d.B > 4096 || units >= (1LL << 31) ? 0 : 2 * kCUs;
+  p.groups = slots <= 512 || d.B > 4096 || units >= (1LL << 31) ? 0 : attend_most(d) * kCUs;
   return p;
 }
 size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
@@ -695,10 +719,10 @@ size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 template <typename T, int A, int NQ>
 void launch_attend(const AttendArgs &a, const AttendPlan &p, hipStream_t st) {
   if (p.groups == 0) {
-    attend_whole_kernel<T, A, NQ><<<a.B * a.Zkv * p.tiles, 64 * kAttendWaves, 0, st>>>(a);
+    attend_whole_kernel<T, A, NQ><<<a.B * a.Zkv * p.tiles, 64 * Attend<T, A, NQ>::kWaves, 0, st>>>(a);
     return;
   }
-  attend_shares_kernel<T, A, NQ><<<p.groups, 64 * kAttendWaves, 0, st>>>(a);
+  attend_shares_kernel<T, A, NQ><<<p.groups, 64 * Attend<T, A, NQ>::kWaves, 0, st>>>(a);
   attend_join_kernel<T, A, NQ><<<dim3(p.groups, p.rows), 256, 0, st>>>(a);
 }
 template <typename T, int A>
@@ -738,7 +762,6 @@ hipError_t cache_attend(const CacheDims &d, const void *Q, const void *Kc, const
   a.c = d.scale * kLog2e;
   a.joins = static_cast<int4 *>(ws);
   a.part = reinterpret_cast<float *>(static_cast<char *>(ws) + align256(p.groups * sizeof(int4)));
-  a.least = 1;
   if (d.dtype == RSA_BF16) launch_attend<bf16_t>(a, p, d.A, st);
   else launch_attend<float>(a, p, d.A, st);
   return hipGetLastError();

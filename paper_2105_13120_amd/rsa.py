@@ -338,17 +338,20 @@ def linformer_project_bwd(desc, dXp, X, E, dX=None, dE=None):
 def rotate(desc, inv_freq, Q=None, K=None, Qr=None, Kr=None, adjacent=False):
     """Q (B, Z, Lq, A) and K (B, Z, L, A), either of them or both, with their first 2 * len(inv_freq) elements a head turned by
     token * inv_freq (fp32).  Pairs are half the turned part apart, with `adjacent` neighbours.  Qr, Kr may be Q, K."""
-    return _rotate(desc, inv_freq, Q, K, Qr, Kr, adjacent, False)
+    if type(Q) not in _PLAIN or type(K) not in _PLAIN:
+        Qr, Kr = _like_given(Qr, Q), _like_given(Kr, K)
+    return _done(_native().rotate(desc, inv_freq, Q, K, Qr, Kr, adjacent, False))
 
 
 def rotate_bwd(desc, inv_freq, dQr=None, dKr=None, dQ=None, dK=None, adjacent=False):
     """The gradients of `rotate`'s Q and K from those of its results."""
-    return _rotate(desc, inv_freq, dQr, dKr, dQ, dK, adjacent, True)
+    if type(dQr) not in _PLAIN or type(dKr) not in _PLAIN:
+        dQ, dK = _like_given(dQ, dQr), _like_given(dK, dKr)
+    return _done(_native().rotate(desc, inv_freq, dQr, dKr, dQ, dK, adjacent, True))
 
 
-def _rotate(desc, inv_freq, Q, K, Qr, Kr, adjacent, back):
-    Qr, Kr = (r if x is None else _like(r, x) for x, r in ((Q, Qr), (K, Kr)))
-    return _done(_native().rotate(desc, inv_freq, Q, K, Qr, Kr, adjacent, back))
+def _like_given(given, t):
+    return given if t is None else _like(given, t)
 
 
 # ---- a paged cache of keys and values, attention of one new token per sequence ----
