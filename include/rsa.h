@@ -326,7 +326,7 @@ int rsa_rotate_bwd(const rsa_desc *d, int32_t R, int32_t adjacent, const float *
  * Tables and lengths are device memory that the kernels check, so a
  * captured graph replays with new contents.  Key head h serves query heads [h Z/Zkv, (h+1) Z/Zkv).
  * bf16 or fp32 (arithmetic as for rsa_forward in bf16; fp32 multiply-adds in fp32), A a
- * multiple of 64 up to 256, any page size, B below 2^16.
+ * multiple of 64 up to 256, any page size, B below 2^16, B * Z below 2^24, width * page below 2^31, pages * Zkv * page below 2^32.
  */
 typedef struct {
   int32_t B;          /* sequences of a call (rows of the table)               */

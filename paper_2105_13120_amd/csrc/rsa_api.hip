@@ -503,7 +503,7 @@ int cache_validate(const rsa_cache_desc *d, int32_t tokens, rsa::CacheDims *out)
   if (!(d->scale >= 0.0f) || !std::isfinite(d->scale)) return RSA_ERR_SHAPE;
   // slots, rows of a pool, rows of queries and tokens of a call are counted in 32 bits
   const int64_t most = 1LL << 31;
-  if (d->B > 65535 || (int64_t)d->B * d->Z > (1 << 24) || (int64_t)d->width * d->page >= most || (int64_t)d->B * tokens >= most ||
+  if (d->B > 65535 || (int64_t)d->B * d->Z >= (1 << 24) || (int64_t)d->width * d->page >= most || (int64_t)d->B * tokens >= most ||
       (int64_t)d->pages * d->Zkv > (2 * most - 1) / d->page)
     return RSA_ERR_UNSUPPORTED;
   out->B = d->B; out->Z = d->Z; out->Zkv = d->Zkv; out->A = d->A;

@@ -16,62 +16,99 @@ struct AppendArgs {
   int64_t qs[3], ks[3];
   Rotary ro;
   TurnShape shape;
-  FastDiv by_T, by_page;
+  FastDiv by_T, by_page, by_split;  // by_split: work-groups that share a tile's heads
   int B, Zq, Zkv, A, pages, width;  // Zq: 0 without queries
-  uint32_t tokens, tiles;           // B T
+  uint32_t tokens;                  // B T
+  int per;                          // sequences a lane counts; 0: no count, all of the B T tokens in turn
 };
 
 // Token t of sequence b: whether it is there, its slot.
 struct Token {
-  uint32_t b, t;
   int64_t slot;
   bool there;
 };
-__device__ __forceinline__ Token token_of(const AppendArgs &a, uint32_t n) {
-  Token k;
-  k.b = a.by_T(n); k.t = n - k.b * a.by_T.d;
-  const int T = (int)a.by_T.d, c = a.counts ? a.counts[k.b] : T, count = c < T ? c : T;
-  k.there = (int)k.t < count;
-  k.slot = (int64_t)a.lengths[k.b] - count + k.t;
-  return k;
+__device__ __forceinline__ int count_of(const AppendArgs &a, uint32_t b) {
+  const int T = (int)a.by_T.d, c = a.counts ? a.counts[b] : T;
+  return c < T ? c : T;
+}
+__device__ __forceinline__ Token token_of(const AppendArgs &a, uint32_t b, uint32_t t) {
+  const int count = count_of(a, b);
+  return {(int64_t)a.lengths[b] - count + t, (int)t < count};
 }
 
 // A work-group takes a few tokens, works out their angles (one a thread), turns their heads of Q and K and moves those of V.
+// Where sequences have uneven numbers of tokens, every wave counts the tiles that there are and the work-groups take them in
+// turn (work-groups for all B T tokens: of 16384 tokens 6700 there, the other tiles' work-groups took 10 us).
 template <typename T, int W>
-__global__ __launch_bounds__(256) void append_kernel(AppendArgs args) {
-  __shared__ float2 angles[256];
+__global__ __launch_bounds__(256, 4) void append_kernel(AppendArgs args) {
   constexpr int ahead = kAhead<T, W>;
+  __shared__ float2 angles[256];
   const TurnShape &sh = args.shape;
-  const uint32_t tid = threadIdx.x, head0 = sh.by_lanes(tid), lane = tid - head0 * sh.lanes, rr = sh.by_units(lane);
+  const uint32_t tid = threadIdx.x, head0 = sh.by_lanes(tid), lane = tid - head0 * sh.lanes, rr = sh.by_units(lane), rows = sh.rows;
   const int u = (int)(lane - rr * sh.by_units.d), heads = 256 / sh.lanes, half = args.ro.R / 2;
   const int2 at = Pair<T, W>::place(args.ro, u);
+  const uint32_t ar = sh.by_half(tid);  // row of this thread's angle
   const bool turns = u < args.ro.R / (2 * W);
-  for (uint32_t tile = blockIdx.x; tile < args.tiles; tile += gridDim.x) {
-    const uint32_t n0 = tile * sh.rows, n = n0 + rr;
-    const bool row = rr < (uint32_t)sh.rows && n < args.tokens;
+  uint32_t tiles = (args.tokens + rows - 1) / rows, mine = 0, upto = 0;
+  if (args.per) {
+    const int l = tid & 63, b0 = l * args.per, b1 = b0 + args.per < args.B ? b0 + args.per : args.B;
+    for (int b = b0; b < b1; ++b) {
+      const int c = count_of(args, b);
+      mine += c > 0 ? (c + rows - 1) / rows : 0;
+    }
+    upto = mine;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const uint32_t x = __shfl_up(upto, o);
+      if (l >= o) upto += x;
+    }
+    tiles = __builtin_amdgcn_readlane(upto, 63);
+  }
+  const uint32_t items = tiles * args.by_split.d;
+  for (uint32_t item = blockIdx.x; item < items; item += gridDim.x) {
+    const uint32_t tile = args.by_split(item);
+    // sequence and token of a row of the tile
+    uint32_t b0 = 0, t0 = tile * rows;
+    if (args.per) {
+      const int l = __builtin_ctzll(__ballot(tile < upto));
+      uint32_t before = __builtin_amdgcn_readlane(upto - mine, l);
+      for (b0 = l * args.per;; ++b0) {
+        const int c = __builtin_amdgcn_readfirstlane(count_of(args, b0));
+        const uint32_t n = c > 0 ? (c + rows - 1) / rows : 0;
+        if (tile < before + n) break;  // (the lane's sequences hold the tile)
+        before += n;
+      }
+      t0 = (tile - before) * rows;
+    }
+    const auto place = [&](uint32_t r, uint32_t &b, uint32_t &t) {
+      b = b0; t = t0 + r;
+      if (!args.per) { b = args.by_T(t); t -= b * args.by_T.d; }
+      return r < rows && (args.per ? t < args.by_T.d : t0 + r < args.tokens);
+    };
+    uint32_t b, t;
+    const bool row = place(rr, b, t);
     // heads of Q, then of K, then of V; the first are on their way while the page is looked up and the angles are worked out
-    const uint32_t b = args.by_T(n), t = n - b * args.by_T.d;
     const int64_t q = (int64_t)b * args.qs[0] + (int64_t)t * args.qs[2], kv = (int64_t)b * args.ks[0] + (int64_t)t * args.ks[2];
-    const int all = args.Zq + 2 * args.Zkv, step = heads * (int)gridDim.y;
+    const int all = args.Zq + 2 * args.Zkv, step = heads * (int)args.by_split.d;
     const auto source = [&](int h) {
       if (h < args.Zq) return static_cast<const T *>(args.Q) + q + h * args.qs[1];
       h -= args.Zq;
       return h < args.Zkv ? static_cast<const T *>(args.K) + kv + h * args.ks[1]
                           : static_cast<const T *>(args.V) + kv + (h - args.Zkv) * args.ks[1];
     };
-    int h = (int)(blockIdx.y * heads + head0);
-    Pair<T, W> p[ahead], q2[ahead];
+    int h = (int)((item - tile * args.by_split.d) * heads + head0);
+    Pair<T, W> p[ahead], next[ahead];
     Token tok{};
-    if (row) tok = token_of(args, n);
+    if (row) tok = token_of(args, b, t);
     if (!__any(tok.there)) continue;  // (a wave sees all rows of the tile: all waves agree)
 #pragma unroll
     for (int k = 0; k < ahead; ++k)
       if (tok.there && h + k * step < all) p[k].load(source(h + k * step), at);
-    if (tile != blockIdx.x) barrier_lds();  // (the angles of the tile before are read)
-    const uint32_t ar = sh.by_half(tid);
-    if (half && ar < (uint32_t)sh.rows && n0 + ar < args.tokens) {
-      const Token k = token_of(args, n0 + ar);
-      angles[tid] = angle_of(k.slot + (args.first ? args.first[k.b] : 0), args.ro.inv_freq[tid - ar * half]);
+    if (item != blockIdx.x) barrier_lds();  // (the angles of the tile before are read)
+    uint32_t ab, at_token;
+    if (half && place(ar, ab, at_token)) {
+      const int64_t slot = token_of(args, ab, at_token).slot;
+      angles[tid] = angle_of(slot + (args.first ? args.first[ab] : 0), args.ro.inv_freq[tid - ar * half]);
     }
     // where its keys and values go; -1: nowhere
     int64_t dst = -1;
@@ -92,7 +129,7 @@ __global__ __launch_bounds__(256) void append_kernel(AppendArgs args) {
       // (loads before stores: a wait for loads counts the stores in front of them)
 #pragma unroll
       for (int k = 0; k < ahead; ++k)
-        if (h + (ahead + k) * step < all) q2[k].load(source(h + (ahead + k) * step), at);
+        if (h + (ahead + k) * step < all) next[k].load(source(h + (ahead + k) * step), at);
 #pragma unroll
       for (int k = 0; k < ahead; ++k) {
         const int x = h + k * step, z = x - args.Zq, v = z - args.Zkv;
@@ -103,14 +140,14 @@ __global__ __launch_bounds__(256) void append_kernel(AppendArgs args) {
           if (turns && v < 0) p[k].turn(cs, args.ro.adjacent);
           p[k].store(to, at);
         }
-        p[k] = q2[k];
+        p[k] = next[k];
       }
     }
   }
 }
 
 template <typename T>
-void launch_append(const AppendArgs &a, int W, dim3 grid, hipStream_t st) {
+void launch_append(const AppendArgs &a, int W, uint32_t grid, hipStream_t st) {
   constexpr int wide = sizeof(T) == 2 ? 8 : 4;
   if (W == wide) append_kernel<T, wide><<<grid, 256, 0, st>>>(a);
   else if constexpr (sizeof(T) == 2) {
@@ -627,7 +664,7 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs args) {
 template <typename T>
 __global__ __launch_bounds__(256) void join_kernel(const T *Op, const float *LSEp, T *O, float *LSE, uint32_t units, uint32_t rows, int N,
                                                    int A, FastDiv by_units, OutLayout lay) {
-  constexpr int W = 16 / sizeof(T), ahead = 8;
+  constexpr int W = 16 / sizeof(T), ahead = 4;
   const uint32_t i = blockIdx.x * 256 + threadIdx.x;
   if (i >= units) return;
   const uint32_t row = by_units(i);
@@ -644,7 +681,7 @@ __global__ __launch_bounds__(256) void join_kernel(const T *Op, const float *LSE
       l[n] = -INFINITY;
       if (n0 + n < N) {
         l[n] = LSEp[(int64_t)(n0 + n) * rows + row] * kLog2e;
-        c[n].load(x + (int64_t)(n0 + n) * rows * A);
+        c[n].load_once(x + (int64_t)(n0 + n) * rows * A);
       }
     }
     float mn = top;
@@ -687,11 +724,15 @@ hipError_t cache_append(const CacheDims &d, int T, int R, int adjacent, const fl
   a.by_T = make_fast_div(T); a.by_page = make_fast_div(d.page);
   a.B = d.B; a.Zq = Q ? d.Z : 0; a.Zkv = d.Zkv; a.A = d.A; a.pages = d.pages; a.width = d.width;
   a.tokens = (uint32_t)((int64_t)d.B * T);
-  a.tiles = (a.tokens + a.shape.rows - 1) / a.shape.rows;
+  // uneven sequences, each of several tiles: counted (4096 of them at most, 64 a lane)
+  const uint32_t rows = a.shape.rows;
+  a.per = counts && T > (int)rows && d.B <= 4096 ? (d.B + 63) / 64 : 0;
+  const uint32_t tiles = a.per ? d.B * ((T + rows - 1) / rows) : (a.tokens + rows - 1) / rows;
   // few tokens: their heads go to several work-groups, up to two on a CU
-  const uint32_t heads = 256 / a.shape.lanes, passes = (a.Zq + 2 * a.Zkv + heads - 1) / heads;
-  const uint32_t split = (2 * kCUs + a.tiles - 1) / a.tiles;
-  const dim3 grid(a.tiles < (1u << 20) ? a.tiles : (1u << 20), split < passes ? split : passes);
+  const uint32_t heads = 256 / a.shape.lanes, passes = (a.Zq + 2 * a.Zkv + heads - 1) / heads, few = (2 * kCUs + tiles - 1) / tiles;
+  a.by_split = make_fast_div(few < passes ? few : passes);
+  const uint64_t items = (uint64_t)tiles * a.by_split.d, most = a.per ? 4 * kCUs : 1u << 20;  // (four fit a CU)
+  const uint32_t grid = (uint32_t)(items < most ? items : most);
   if (d.dtype == RSA_BF16) launch_append<bf16_t>(a, W, grid, st);
   else launch_append<float>(a, W, grid, st);
   return hipGetLastError();
@@ -706,7 +747,7 @@ struct AttendPlan {
 int attend_most(const CacheDims &d) { return d.A == 64 ? 3 : d.A == 256 ? 1 : 2; }
 AttendPlan attend_plan(const CacheDims &d) {
   AttendPlan p;
-  const int group = d.Z / d.Zkv, unit = 16;  // (of at least that many slots)
+  const int group = d.Z / d.Zkv, unit = 64;  // (of at least that many slots)
   p.nq = group > 16 && d.A <= 128 ? 2 : 1;  // (two tiles of longer heads do not fit the registers)
   p.tiles = (group + 16 * p.nq - 1) / (16 * p.nq);
   p.rows = group < 16 * p.nq ? group : 16 * p.nq;

@@ -29,6 +29,7 @@ template <typename T, int W> struct Chunk;
 template <> struct Chunk<bf16_t, 8> {
   u32x4 r;
   __device__ __forceinline__ void load(const bf16_t *p) { r = *reinterpret_cast<const u32x4 *>(p); }
+  __device__ __forceinline__ void load_once(const bf16_t *p) { r = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(p)); }
   __device__ __forceinline__ void store(bf16_t *p) const { *reinterpret_cast<u32x4 *>(p) = r; }
   __device__ __forceinline__ float get(int k) const {
     return __builtin_bit_cast(float, k & 1 ? r[k >> 1] & 0xffff0000u : r[k >> 1] << 16);
@@ -54,6 +55,7 @@ template <> struct Chunk<bf16_t, 2> {
 template <> struct Chunk<float, 4> {
   f32x4 r;
   __device__ __forceinline__ void load(const float *p) { r = *reinterpret_cast<const f32x4 *>(p); }
+  __device__ __forceinline__ void load_once(const float *p) { r = __builtin_nontemporal_load(reinterpret_cast<const f32x4 *>(p)); }
   __device__ __forceinline__ void store(float *p) const { *reinterpret_cast<f32x4 *>(p) = r; }
   __device__ __forceinline__ float get(int k) const { return r[k]; }
   __device__ __forceinline__ void set2(int k, float x, float y) { r[k] = x; r[k + 1] = y; }

@@ -31,9 +31,11 @@ __global__ __launch_bounds__(256) void rotate_kernel(RotateArgs args) {
   const TurnShape &sh = args.shape;
   const uint32_t tid = threadIdx.x, head0 = sh.by_lanes(tid), lane = tid - head0 * sh.lanes, rr = sh.by_units(lane);
   const int u = (int)(lane - rr * sh.by_units.d), heads = 256 / sh.lanes, step = heads * (int)gridDim.y;
-  const bool keys = blockIdx.x >= args.side[0].tiles;
+  const uint32_t tile = blockIdx.z * gridDim.x + blockIdx.x;
+  if (tile >= args.side[0].tiles + args.side[1].tiles) return;
+  const bool keys = tile >= args.side[0].tiles;
   const Side &s = args.side[keys ? 1 : 0];
-  const uint32_t n0 = (blockIdx.x - (keys ? args.side[0].tiles : 0u)) * sh.rows, n = n0 + rr;
+  const uint32_t n0 = (tile - (keys ? args.side[0].tiles : 0u)) * sh.rows, n = n0 + rr;
   const bool have = rr < (uint32_t)sh.rows && n < s.rows;
   const int2 at = Pair<T, W>::place(args.ro, u);
   const int64_t row = (int64_t)n * s.st[2];
@@ -102,7 +104,8 @@ hipError_t rotate_rows(const Dims &d, int dtype, int R, int adjacent, const floa
   }
   const uint32_t tiles = a.side[0].tiles + a.side[1].tiles, heads = 256 / a.shape.lanes, passes = (a.heads + heads - 1) / heads;
   const uint32_t split = (4 * 256 + tiles - 1) / tiles;  // (few rows: the heads go to several work-groups, up to four on a CU)
-  const dim3 grid(tiles, split < passes ? split : passes);
+  const uint32_t x = tiles < (1u << 22) ? tiles : (1u << 22);  // (a dimension of a grid has less than 2^32 threads)
+  const dim3 grid(x, split < passes ? split : passes, (tiles + x - 1) / x);
   if (dtype == RSA_BF16) launch<bf16_t>(a, W, grid, st);
   else launch<float>(a, W, grid, st);
   return hipGetLastError();

@@ -28,6 +28,10 @@ APPEND = [  # dtype, Z, Zkv, A, page, T, R, adjacent, lengths, counts
     ("f32", 3, 3, 192, 7, 6, 192, True, [6, 20], [6, 5]),
     ("f32", 2, 1, 256, 16, 5, 250, False, [9, 5], [5, 5]),
     ("f32", 9, 3, 128, 32, 4, 40, True, [70, 4, 33], [1, 4, 2]),
+    # more sequences than lanes, many of them without tokens, tiles that end inside a sequence
+    ("bf16", 2, 1, 64, 16, 21, 64, False, [21 + 7 * b % 50 for b in range(150)], [(13 * b) % 29 - 4 for b in range(150)]),
+    ("f32", 1, 1, 64, 4, 6, 64, True, [6 + b % 9 for b in range(70)], [6 if b in (0, 69) else 0 for b in range(70)]),
+    ("bf16", 2, 2, 128, 16, 9, 24, True, [9, 9, 9], [0, 0, 0]),             # no tokens at all
 ]
 
 
@@ -42,12 +46,12 @@ def append_case(case, seed=0, width=8):
 
 
 @pytest.mark.parametrize("case", APPEND)
-@pytest.mark.parametrize("first", [None, 70000])
+@pytest.mark.parametrize("first", [None, 70000, 2 ** 31 - 100])          # (fp32 holds the last one's turns to a few hundred)
 def test_append(case, first):
     dtype, Z, Zkv, A, page, T, R, adjacent, lengths, counts = case
     c, Q, K, V, f = append_case(case)
     B = len(lengths)
-    base = None if first is None else [first + 3 * b for b in range(B)]
+    base = None if first is None else [min(first + 3 * b, 2 ** 31 - 1) for b in range(B)]      # (int32)
     Kc, Vc, table, n = c.gpu()
     d = rsa.make_cache_desc(Kc, table, Z)
     Qr = torch.full_like(Q, 5.0).cuda()
