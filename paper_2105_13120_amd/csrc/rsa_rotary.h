@@ -114,12 +114,15 @@ inline int chunk_width(int dtype, int R) {
   if (dtype != RSA_BF16) return R % 8 == 0 ? 4 : 1;
   return R % 16 == 0 ? 8 : R % 8 == 0 ? 4 : R % 4 == 0 ? 2 : 1;
 }
-template <typename T, int W> constexpr int kAhead = W * (int)sizeof(T) >= 8 ? 2 : 4;  // heads of a thread whose loads are in flight
-// `least`: threads of a group where they are enough for a row, 32 or 64
+// heads of a thread whose loads are in flight
+template <typename T, int W> constexpr int kAhead = W * (int)sizeof(T) >= 8 ? 2 : 4;
+inline int heads_in_flight(int dtype, int W) { return W * (dtype == RSA_BF16 ? 2 : 4) >= 8 ? 2 : 4; }
+// groups of `least` threads, rounded to a power of two from 32 to 128, where they are enough for a row
 inline TurnShape make_turn_shape(int A, int R, int W, int least) {
   const int units = A / (2 * W);
   TurnShape s;
-  s.lanes = units <= least ? least : units <= 64 ? 64 : 128;
+  s.lanes = 32;
+  while (s.lanes < 128 && (s.lanes < least || s.lanes < units)) s.lanes *= 2;
   s.rows = s.lanes / units;
   s.by_lanes = make_fast_div(s.lanes); s.by_units = make_fast_div(units); s.by_half = make_fast_div(R > 1 ? R / 2 : 1);
   return s;

@@ -52,8 +52,8 @@ def test_one_byte_less_of_workspace_is_refused():
         assert rsa.lib().rsa_cache_attend(ctypes.byref(d), p, p, p, p, p, p, p, ws, n, None) == -4
 
 
-@pytest.mark.parametrize("A,R,dtype,rows", [(64, 64, "bf16", 16), (128, 128, "bf16", 8), (64, 8, "bf16", 8), (64, 20, "bf16", 4),
-                                            (128, 6, "bf16", 1), (64, 64, "f32", 8), (256, 256, "f32", 2), (256, 6, "f32", 1)])
+@pytest.mark.parametrize("A,R,dtype,rows", [(64, 64, "bf16", 8), (128, 128, "bf16", 8), (64, 8, "bf16", 8), (64, 20, "bf16", 8),
+                                            (128, 6, "bf16", 2), (64, 64, "f32", 8), (256, 256, "f32", 4), (256, 6, "f32", 1)])
 @pytest.mark.parametrize("L,B", [(64, 1), (4096, 3), (1 << 20, 1), (1 << 30, 1)])
 def test_rotation_covers_all_rows(rec, A, R, dtype, rows, L, B):
     code = rsa.RSA_BF16 if dtype == "bf16" else rsa.RSA_F32
@@ -62,7 +62,7 @@ def test_rotation_covers_all_rows(rec, A, R, dtype, rows, L, B):
         (k,) = rec("rotate", d, R, 0, "f", *tensors)
         x, y, z = k.grid
         assert k.threads == 256 and x * z >= sides * -(-L // rows) and x * (z - 1) < sides * -(-L // rows)
-        assert x * 256 < 1 << 32 and 1 <= y <= B * 2
+        assert x * 256 < 1 << 32 and y == 1
 
 
 @pytest.mark.parametrize("T,B,counts,work_groups", [(1, 1, False, 3), (1, 64, False, 24), (2048, 8, False, 2048), (2048, 8, True, 1024), (1, 9, True, 6)])
