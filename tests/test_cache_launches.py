@@ -62,7 +62,7 @@ def test_rotation_covers_all_rows(rec, A, R, dtype, rows, L, B):
         (k,) = rec("rotate", d, R, 0, "f", *tensors)
         x, y, z = k.grid
         assert k.threads == 256 and x * z >= sides * -(-L // rows) and x * (z - 1) < sides * -(-L // rows)
-        assert x * 256 < 1 << 32 and y == 1
+        assert x * 256 < 1 << 32 and 1 <= y <= B
 
 
 @pytest.mark.parametrize("T,B,counts,work_groups", [(1, 1, False, 3), (1, 64, False, 24), (2048, 8, False, 2048), (2048, 8, True, 1024), (1, 9, True, 6)])
