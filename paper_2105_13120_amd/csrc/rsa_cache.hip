@@ -744,15 +744,20 @@ namespace {
 struct AttendPlan {
   int nq, tiles, rows, groups;  // 16-query tiles of a wave; query tiles of a key head and their rows; shares (0: whole segments)
 };
-int attend_most(const CacheDims &d) { return d.A == 64 ? 3 : d.A == 256 ? 1 : 2; }
+// Whole segments where a table has room for 96 KB of a key head's keys at most.  One work-group then takes 2 us and as many again for
+// every 256 slots of 64 elements; shares and their join take 2.5 us more at the least, but no longer for longer sequences.  us,
+// shares and whole segments: 16 key heads of 64 with 768 slots 7.8 and 7.0, with 1024 7.8 and 9.1; 8 of 128, four queries each, 384
+// slots 8.1 and 6.4, 768 8.8 and 9.8; four of 256, 192 slots 10.3 and 8.0, 384 10.8 and 12.1; fp32, 48 of 64, 384 slots 8.3 and 8.9.
+// Shares: up to three a CU for heads of 64, two, or with heads of 256 one, as registers leave room.
 AttendPlan attend_plan(const CacheDims &d) {
   AttendPlan p;
   const int group = d.Z / d.Zkv, unit = 64;  // (of at least that many slots)
-  p.nq = group > 16 && d.A <= 128 ? 2 : 1;  // (two tiles of longer heads do not fit the registers)
+  p.nq = group > 16 && d.A <= 128 ? 2 : 1;   // (two tiles of longer heads do not fit the registers)
   p.tiles = (group + 16 * p.nq - 1) / (16 * p.nq);
   p.rows = group < 16 * p.nq ? group : 16 * p.nq;
   const int64_t slots = (int64_t)d.width * d.page, heads = (int64_t)d.Zkv * p.tiles, units = d.B * (slots / unit + 1) * heads;
-  p.groups = slots <= 512 || d.B > 4096 || units >= (1LL << 31) ? 0 : attend_most(d) * kCUs;
+  const bool whole = slots * d.A * (d.dtype == RSA_BF16 ? 2 : 4) <= 96 * 1024 || d.B > 4096 || units >= (1LL << 31);
+  p.groups = whole ? 0 : (d.A == 64 ? 3 : d.A == 256 ? 1 : 2) * kCUs;
   return p;
 }
 size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }

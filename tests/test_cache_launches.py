@@ -24,7 +24,8 @@ def attend(rec, d):
 
 
 @pytest.mark.parametrize("kw,whole,queries", [
-    (dict(width=32), True, 1), (dict(width=33), False, 1), (dict(width=2, page=256), True, 1), (dict(width=513, page=1), False, 1),
+    (dict(width=48), True, 1), (dict(width=49), False, 1), (dict(width=3, page=256), True, 1), (dict(width=769, page=1), False, 1),
+    (dict(width=24, dtype=rsa.RSA_F32), True, 1), (dict(width=25, dtype=rsa.RSA_F32), False, 1), (dict(width=12, A=256), True, 1),
     (dict(width=100, Z=32), False, 1), (dict(width=100, Z=34), False, 2), (dict(width=100, Z=80, A=128), False, 2),
     (dict(width=100, Z=80, A=192), False, 1), (dict(width=100, B=4096), False, 1), (dict(width=100, B=4097), True, 1),
     (dict(width=1 << 20, page=2047, Zkv=8, B=4), False, 1), (dict(width=1 << 20, page=2047, Zkv=8, B=9), True, 1)])
