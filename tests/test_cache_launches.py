@@ -35,7 +35,7 @@ def test_whole_segments_or_shares(rec, kw, whole, queries):
     tiles = -(-group // (16 * queries))
     k = attend(rec, d)
     # (bf16 in a template's arguments stays as the compiler writes it: ..kernelI<type>Li<A>ELi<queries>E..)
-    forms = [re.search(r"attend_(\w+?)_kernelI\w+?Li(\d+)ELi(\d)E", x.name).groups() for x in k]
+    forms = [re.search(r"attend_(\w+?)_kernel(?:I\w+?Li|<float, )(\d+)(?:ELi|, )(\d)", x.name).groups() for x in k]
     assert forms == [(f, str(d.A), str(queries)) for f in (["whole"] if whole else ["shares", "join"])]
     if whole:
         assert k[0].grid == (d.B * d.Zkv * tiles, 1, 1) and rsa.cache_workspace_bytes(d) == 0
