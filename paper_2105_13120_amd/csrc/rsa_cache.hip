@@ -8,6 +8,43 @@ namespace {
 
 constexpr int kCUs = 256;
 
+// Uneven sequences, each of some items of work (none for b outside [0, B)), as every wave counts them for itself: lane l has
+// sequences [l per, (l + 1) per), per <= 64.
+struct Count {
+  uint32_t mine, upto;  // items of this lane's sequences; of theirs and all before
+  __device__ __forceinline__ static uint32_t scan(uint32_t x) {
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const uint32_t y = __shfl_up(x, o);
+      if ((int)(threadIdx.x & 63) >= o) x += y;
+    }
+    return x;
+  }
+  template <class F> __device__ __forceinline__ Count(int B, int per, F items) : mine(0) {
+    const int b0 = (int)(threadIdx.x & 63) * per, b1 = b0 + per < B ? b0 + per : B;
+    if (per == 1) mine = b0 < b1 ? items(b0) : 0u;
+    else for (int b = b0; b < b1; b += 8) {  // (eight loads on their way at a time)
+      uint32_t n[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) n[k] = items(b + k < b1 ? b + k : b);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) mine += b + k < b1 ? n[k] : 0u;
+    }
+    upto = scan(mine);
+  }
+  __device__ __forceinline__ uint32_t all() const { return __builtin_amdgcn_readlane(upto, 63); }
+  // The sequence of item x < all(), and the items before it
+  template <class F> __device__ __forceinline__ int find(uint32_t x, int B, int per, F items, uint32_t &before) const {
+    const int l = __builtin_ctzll(__ballot(x < upto)), lane = (int)(threadIdx.x & 63), b = l * per + lane;
+    before = __builtin_amdgcn_readlane(upto - mine, l);
+    if (per == 1) return l;
+    const uint32_t n = lane < per && b < B ? items(b) : 0u, s = scan(n);
+    const int k = __builtin_ctzll(__ballot(x < before + s));
+    before += __builtin_amdgcn_readlane(s - n, k);
+    return l * per + k;
+  }
+};
+
 // ---------------------------------------------------------------- append ----
 struct AppendArgs {
   const void *Q, *K, *V;
@@ -49,35 +86,20 @@ __global__ __launch_bounds__(256, 4) void append_kernel(AppendArgs args) {
   const int2 at = Pair<T, W>::place(args.ro, u);
   const uint32_t ar = sh.by_half(tid);  // row of this thread's angle
   const bool turns = u < args.ro.R / (2 * W);
-  uint32_t tiles = (args.tokens + rows - 1) / rows, mine = 0, upto = 0;
-  if (args.per) {
-    const int l = tid & 63, b0 = l * args.per, b1 = b0 + args.per < args.B ? b0 + args.per : args.B;
-    for (int b = b0; b < b1; ++b) {
-      const int c = count_of(args, b);
-      mine += c > 0 ? (c + rows - 1) / rows : 0;
-    }
-    upto = mine;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const uint32_t x = __shfl_up(upto, o);
-      if (l >= o) upto += x;
-    }
-    tiles = __builtin_amdgcn_readlane(upto, 63);
-  }
+  const auto tiles_of = [&](int b) {
+    const int c = count_of(args, b);
+    return c > 0 ? (c + rows - 1) / rows : 0u;
+  };
+  const Count count(args.per ? args.B : 0, args.per, tiles_of);
+  const uint32_t tiles = args.per ? count.all() : (args.tokens + rows - 1) / rows;
   const uint32_t items = tiles * args.by_split.d;
   for (uint32_t item = blockIdx.x; item < items; item += gridDim.x) {
     const uint32_t tile = args.by_split(item);
     // sequence and token of a row of the tile
     uint32_t b0 = 0, t0 = tile * rows;
     if (args.per) {
-      const int l = __builtin_ctzll(__ballot(tile < upto));
-      uint32_t before = __builtin_amdgcn_readlane(upto - mine, l);
-      for (b0 = l * args.per;; ++b0) {
-        const int c = __builtin_amdgcn_readfirstlane(count_of(args, b0));
-        const uint32_t n = c > 0 ? (c + rows - 1) / rows : 0;
-        if (tile < before + n) break;  // (the lane's sequences hold the tile)
-        before += n;
-      }
+      uint32_t before;
+      b0 = count.find(tile, args.B, args.per, tiles_of, before);
       t0 = (tile - before) * rows;
     }
     const auto place = [&](uint32_t r, uint32_t &b, uint32_t &t) {
@@ -527,22 +549,14 @@ __global__ __launch_bounds__((64 * Attend<T, A, NQ>::kWaves), (Attend<T, A, NQ>:
   __shared__ typename At::Lds lds;
   At at(args, lds);
   const uint32_t heads = args.Zkv * args.by_tiles.d, w = blockIdx.x;
-  // units before this lane's sequences (each wave counts for itself: nothing to wait for)
-  const int b0 = at.lane * args.per, b1 = b0 + args.per < args.B ? b0 + args.per : args.B;
-  uint32_t mine = 0;
   bool empty = false;
-  for (int b = b0; b < b1; ++b) {
+  const auto units_of = [&](int b) {
     const uint32_t len = length_of(args, b);
     empty |= len == 0;
-    mine += (len + At::kUnit - 1) / At::kUnit;
-  }
-  uint32_t upto = mine;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const uint32_t x = __shfl_up(upto, o);
-    if (at.lane >= o) upto += x;
-  }
-  const uint32_t units = __builtin_amdgcn_readlane(upto, 63) * heads;
+    return (len + At::kUnit - 1) / At::kUnit;
+  };
+  const Count count(args.B, args.per, units_of);
+  const uint32_t units = count.all() * heads;
   if (__any(empty))
     for (int b = w; b < args.B; b += gridDim.x)
       if (length_of(args, b) == 0) store_empty<T, A, NQ>(args, b);
@@ -557,16 +571,10 @@ __global__ __launch_bounds__((64 * Attend<T, A, NQ>::kWaves), (Attend<T, A, NQ>:
   const Shares sh(units, groups);
   uint32_t unit = sh.begin(w);
   const uint32_t end = sh.begin(w + 1);
-  // the sequence of the first unit
-  const int lane = __builtin_ctzll(__ballot(unit < upto * heads));
-  int b = lane * args.per;
-  uint32_t before = __builtin_amdgcn_readlane(upto - mine, lane), len, n;
-  for (;; ++b) {
-    len = __builtin_amdgcn_readfirstlane(length_of(args, b));
-    n = (len + At::kUnit - 1) / At::kUnit;
-    if (unit < (before + n) * heads) break;  // (the lane's sequences hold the unit)
-    before += n;
-  }
+  // where the first unit is
+  uint32_t before;
+  int b = count.find(unit / heads, args.B, args.per, units_of, before);
+  uint32_t len = __builtin_amdgcn_readfirstlane(length_of(args, b)), n = (len + At::kUnit - 1) / At::kUnit;
   uint32_t rest = unit - before * heads, head = rest / n, in = rest - head * n;
   int4 join = make_int4(-1, 0, 0, 0);
   const size_t place = (size_t)(args.group < 16 * NQ ? args.group : 16 * NQ) * (A + 4);

@@ -301,6 +301,29 @@ def test_long_and_many_sequences(dtype, Z, Zkv, A, page, lengths):
     assert torch.equal(again[0], O) and torch.equal(again[1], LSE)            # sums in a fixed order
 
 
+@pytest.mark.parametrize("B", [65, 4096, 4097])
+def test_more_sequences_than_lanes(B):
+    """Most of them empty or short, on pages that they share, in tables with room for long ones."""
+    Z, Zkv, A, page, W, pages = 2, 1, 64, 16, 64, 300
+    g = torch.Generator(device="cuda").manual_seed(18)
+    Kc, Vc = (torch.randn(pages, Zkv, page, A, generator=g, device="cuda").bfloat16() for _ in range(2))
+    table = torch.randint(pages, (B, W), generator=g, device="cuda", dtype=torch.int32)
+    rng = np.random.default_rng(19)
+    lengths = np.where(rng.random(B) < 0.4, 0, rng.integers(1, 1025, B) ** 2 // 1024)
+    lengths[0], lengths[-1] = 0, 1024
+    Q = torch.randn(B, Z, 1, A, generator=g, device="cuda").bfloat16()
+    O, LSE = rsa.cache_attend(rsa.make_cache_desc(Kc, table, Z), Q, Kc, Vc, table, i32(lengths))
+    none = torch.from_numpy(lengths == 0).cuda()
+    assert (O[none] == 0).all() and torch.isneginf(LSE[none]).all()
+    some = np.flatnonzero(lengths)
+    rO, rLSE, P2 = vectorised(Q[~none], Kc, Vc, table[~none], lengths[some])
+    # as in test_long_and_many_sequences
+    rel = 2 * (A + 4) * F32 * A ** 0.5 * 6 + 2.0 ** -21 + 2 * 1024 * F32
+    bound = rel * rO.abs().clamp(min=1.0) + STEP["bf16"] * rO.abs() + 6 * 2.0 ** -8 / 3 ** 0.5 * P2.sqrt()
+    within(O[~none], f64(rO), f64(bound), "O")
+    within(LSE[~none], f64(rLSE), rel + 4 * F32 * np.abs(f64(rLSE)), "LSE")
+
+
 def test_strided_queries_and_results():
     """Q and O as a projection's rows of one token per sequence, (1, Z, B, A) seen as (B, Z, 1, A)."""
     rng = np.random.default_rng(12)
