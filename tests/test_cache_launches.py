@@ -54,7 +54,7 @@ def test_one_byte_less_of_workspace_is_refused():
 
 
 @pytest.mark.parametrize("A,R,dtype,rows", [(64, 64, "bf16", 8), (128, 128, "bf16", 8), (64, 8, "bf16", 8), (64, 20, "bf16", 8),
-                                            (128, 6, "bf16", 2), (64, 64, "f32", 8), (256, 256, "f32", 4), (256, 6, "f32", 1)])
+                                            (128, 6, "bf16", 8), (64, 64, "f32", 8), (192, 192, "f32", 4), (256, 256, "f32", 4), (256, 6, "f32", 4)])
 @pytest.mark.parametrize("L,B", [(64, 1), (4096, 3), (1 << 20, 1), (1 << 30, 1)])
 def test_rotation_covers_all_rows(rec, A, R, dtype, rows, L, B):
     code = rsa.RSA_BF16 if dtype == "bf16" else rsa.RSA_F32

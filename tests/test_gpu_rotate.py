@@ -64,6 +64,36 @@ def test_in_place_and_either_alone(case):
     assert a.data_ptr() == q.data_ptr() and torch.equal(q, Qr) and torch.equal(k, Kr)
 
 
+@pytest.mark.parametrize("dtype,B,Z,L,A,R,adjacent", [("bf16", 8, 5, 2048, 128, 128, False), ("f32", 5, 3, 1088, 192, 130, True), ("bf16", 30, 2, 2112, 64, 20, False)])
+def test_large_calls_are_small_ones(dtype, B, Z, L, A, R, adjacent):
+    """Results of 16 MB and more, which are written in another way, against calls for one sequence."""
+    g = torch.Generator(device="cuda").manual_seed(20)
+    Q, K = (torch.randn(B, Z, L, A, generator=g, device="cuda").to(DTYPES[dtype]) for _ in range(2))
+    f, mode = frequencies(R).cuda(), rsa.MODE_STAGED if dtype == "f32" else rsa.MODE_FUSED
+    got = rsa.rotate(rsa.make_desc(K, 1, mode=mode), f, Q, K, adjacent=adjacent)
+    for b in range(B):
+        one = rsa.rotate(rsa.make_desc(K[b:b + 1], 1, mode=mode), f, Q[b:b + 1], K[b:b + 1], adjacent=adjacent)
+        assert torch.equal(got[0][b], one[0][0]) and torch.equal(got[1][b], one[1][0])
+    into = Q.clone(), K.clone()
+    rsa.rotate(rsa.make_desc(K, 1, mode=mode), f, *into, *into, adjacent=adjacent)
+    assert torch.equal(into[0], got[0]) and torch.equal(into[1], got[1])
+
+
+def test_infinities_and_nan_stay_in_their_pairs():
+    for dtype, A, R, adjacent in (("bf16", 64, 20, False), ("bf16", 64, 36, True), ("bf16", 128, 64, False), ("f32", 64, 10, False), ("f32", 64, 6, True)):
+        d, Q, K, _, f = setup((dtype, 1, 1, 64, 1, (0, 1), A, R, adjacent, False), 21)
+        half = R // 2
+        ref = rsa.rotate(d, f.cuda(), K=K.cuda(), adjacent=adjacent)[1].cpu()
+        for e, partner in ((0, 1 if adjacent else half), (R - 1, R - 2 if adjacent else half - 1), (R, R), (A - 1, A - 1)):
+            for bad in (float("inf"), float("nan")):
+                x = K.clone()
+                x[0, 0, 5, e] = bad
+                y = rsa.rotate(d, f.cuda(), K=x.cuda(), adjacent=adjacent)[1].cpu()
+                assert not y[0, 0, 5, e].isfinite() and not y[0, 0, 5, partner].isfinite()
+                y[0, 0, 5, e], y[0, 0, 5, partner] = ref[0, 0, 5, e], ref[0, 0, 5, partner]
+                assert torch.equal(y, ref), (dtype, A, R, adjacent, e)
+
+
 def test_slices_of_a_packed_projection():
     B, L, Z, A, N = 2, 256, 3, 64, 2
     g = torch.Generator(device="cuda").manual_seed(3)
