@@ -325,8 +325,8 @@ int rsa_rotate_bwd(const rsa_desc *d, int32_t R, int32_t adjacent, const float *
  * tokens that the call appends included; slots below 0 or behind the table do not exist.
  * Tables and lengths are device memory that the kernels check, so a
  * captured graph replays with new contents.  Key head h serves query heads [h Z/Zkv, (h+1) Z/Zkv).
- * bf16 or fp32 (arithmetic as for rsa_forward in bf16; fp32 multiply-adds in fp32), A a
- * multiple of 64 up to 256, any page size, B below 2^16, B * Z below 2^24, width * page below 2^31, pages * Zkv * page below 2^32.
+ * bf16 (fp32 sums and softmax, probabilities to 2^-15, one rounding per stored element) or fp32 (fp32
+ * multiply-adds), A a multiple of 64 up to 256, any page size, B below 2^16, B * Z below 2^24, width * page below 2^31, pages * Zkv * page below 2^32.
  */
 typedef struct {
   int32_t B;          /* sequences of a call (rows of the table)               */
@@ -361,7 +361,7 @@ int rsa_cache_append(const rsa_cache_desc *d, int32_t T, const void *Q, const vo
  * that are held: O (B, Z, 1, A) and LSE (B, Z, 1) fp32 as rsa_forward's.  A row that sees no key
  * gets O = 0 and LSE = -inf.  Pool memory outside the seen slots does not reach a result, whatever it holds.
  * The walk over the cache is divided among work-groups by what the lengths say, in a fixed
- * order of sums for given lengths.  ws: rsa_cache_workspace_bytes(d) bytes (may be NULL if that is 0), of one call at a
+ * order of sums for given lengths.  Outputs must not overlap inputs.  ws: rsa_cache_workspace_bytes(d) bytes (may be NULL if that is 0), of one call at a
  * time; the kernels read nothing there that the call has not written. */
 size_t rsa_cache_workspace_bytes(const rsa_cache_desc *d);
 int rsa_cache_attend(const rsa_cache_desc *d, const void *Q, const void *Kc, const void *Vc,

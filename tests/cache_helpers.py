@@ -41,8 +41,7 @@ def attend_bounds(Q, Kc, Vc, table, lengths, O, LSE, dtype, scale=None):
     """Bounds of |O| and |LSE| errors against fp64, from the definition.  A score is a sum of A products in fp32, off by at most
     dS = (A + 4) 2^-24 s sum|q k| (the scale and the exponent's argument are the 4); exp adds 2^-22, so probabilities are off by
     2 dS + 2^-21 relative to their normalised value, and n terms' sum by n 2^-24 at most.  In bf16 the probabilities that
-    weigh V are rounded once more: independent errors of at most 2^-8 P each (standard deviation 2^-8 / sqrt 3 of it), of which
-    six standard deviations are allowed for.  The stored O is rounded once."""
+    weigh V are two bf16 numbers each, eight bits and what they leave, rounded: off by 2^-15.  The stored O is rounded once."""
     B, Z, _, A = Q.shape
     pages, Zkv, page, _ = Kc.shape
     s = 1.0 / np.sqrt(A) if scale is None else scale
@@ -63,7 +62,7 @@ def attend_bounds(Q, Kc, Vc, table, lengths, O, LSE, dtype, scale=None):
             bL[b, z, 0] = rel + 4 * F32 * np.abs(LSE[b, z, 0])
             bO[b, z, 0] = rel * (P @ np.abs(v)) + STEP[dtype] * np.abs(O[b, z, 0])
             if dtype == "bf16":
-                bO[b, z, 0] += 6 * 2.0 ** -8 / np.sqrt(3) * np.sqrt(P ** 2 @ v ** 2)
+                bO[b, z, 0] += 2.0 ** -15 * (P @ np.abs(v))
     return bO, bL
 
 
