@@ -306,6 +306,7 @@ struct AttendArgs {
   float c;           // scale log2(e)
   float *part;       // partial results, nullptr: whole segments
   int4 *joins;
+  int by_segment;    // one note a segment, else one a share
 };
 
 template <typename T> struct AttendShape;
@@ -654,15 +655,18 @@ __global__ __launch_bounds__((64 * Attend<T, A, NQ>::kWaves), (Attend<T, A, NQ>:
   at.finish(b, h, tile, nullptr);
 }
 
-// The work of all segments, in units of kKeys slots, in equal shares: sequences in their order, their key heads and query tiles,
+// The work of all segments, in units of kUnit slots, in equal shares: sequences in their order, their key heads and query tiles,
 // their units.  A share may begin and end inside a segment; such parts go to the work-group's two places in the workspace, and the
-// work-group that has a divided segment's beginning writes down for the join where its parts lie.
+// work-group that has a divided segment's beginning writes down for the join where its parts lie: in the place of the segment or, if
+// there are more segments than shares, in its own (a share begins one divided segment at most).  Every place gets a note, if only that
+// there is nothing to do.
 template <typename T, int A, int NQ>
 __global__ __launch_bounds__((64 * Attend<T, A, NQ>::kWaves), (Attend<T, A, NQ>::kSimd)) void attend_shares_kernel(AttendArgs args) {
   typedef Attend<T, A, NQ> At;
   __shared__ typename At::Lds lds;
   At at(args, lds);
   const uint32_t heads = args.Zkv * args.by_tiles.d, w = blockIdx.x;
+  const int4 nothing = make_int4(-1, 0, 0, 0);
   bool empty = false;
   const auto units_of = [&](int b) {
     const uint32_t len = length_of(args, b);
@@ -673,13 +677,17 @@ __global__ __launch_bounds__((64 * Attend<T, A, NQ>::kWaves), (Attend<T, A, NQ>:
   const uint32_t units = count.all() * heads;
   if (__any(empty))
     for (int b = w; b < args.B; b += gridDim.x)
-      if (length_of(args, b) == 0) store_empty<T, A, NQ>(args, b);
+      if (length_of(args, b) == 0) {
+        store_empty<T, A, NQ>(args, b);
+        if (args.by_segment)
+          for (uint32_t k = threadIdx.x; k < heads; k += 64 * At::kWaves) args.joins[b * heads + k] = nothing;
+      }
   // one share a CU, a second (third) where each then still has four units
   uint32_t groups = kCUs * (1 + units / (4 * kCUs));
   groups = groups < gridDim.x ? groups : gridDim.x;
   groups = groups < units ? groups : units;
   if (w >= groups) {
-    if (threadIdx.x == 0) args.joins[w] = make_int4(-1, 0, 0, 0);
+    if (threadIdx.x == 0 && !args.by_segment) args.joins[w] = nothing;
     return;
   }
   const Shares sh(units, groups);
@@ -690,14 +698,18 @@ __global__ __launch_bounds__((64 * Attend<T, A, NQ>::kWaves), (Attend<T, A, NQ>:
   int b = count.find(unit / heads, args.B, args.per, units_of, before);
   uint32_t len = __builtin_amdgcn_readfirstlane(length_of(args, b)), n = (len + At::kUnit - 1) / At::kUnit;
   uint32_t rest = unit - before * heads, head = rest / n, in = rest - head * n;
-  int4 join = make_int4(-1, 0, 0, 0);
+  int4 join = nothing;
   const size_t place = (size_t)(args.group < 16 * NQ ? args.group : 16 * NQ) * (A + 4);
   for (bool begun = false; unit < end; begun = true) {
     const uint32_t left = end - unit, take = n - in < left ? n - in : left;
     const uint32_t h = args.by_tiles(head), tile = head - h * args.by_tiles.d;
     at.walk(b, h, tile, len, in * At::kTiles, take == n - in ? (len + At::kKeys - 1) / At::kKeys : (in + take) * At::kTiles);
     at.finish(b, h, tile, take == n ? nullptr : args.part + (size_t)(2 * w + begun) * place);
-    if (in == 0 && take < n) join = make_int4(b, (int)head, 2 * (int)w + begun, (int)sh.of(unit + n - 1));
+    if (in == 0) {
+      const int4 note = take == n ? nothing : make_int4(b, (int)head, 2 * (int)w + begun, (int)sh.of(unit + n - 1));
+      if (take < n) join = note;
+      if (args.by_segment && threadIdx.x == 0) args.joins[b * heads + head] = note;
+    }
     unit += take;
     in = 0;
     if (unit < end && ++head == heads) {
@@ -706,17 +718,21 @@ __global__ __launch_bounds__((64 * Attend<T, A, NQ>::kWaves), (Attend<T, A, NQ>:
       n = (len + At::kUnit - 1) / At::kUnit;
     }
   }
-  if (threadIdx.x == 0) args.joins[w] = join;
+  if (threadIdx.x == 0 && !args.by_segment) args.joins[w] = join;
 }
 
-// A divided segment's parts: the first at place join.z, then place 2 v of the work-groups v behind it up to join.w.  A work-group a
-// row: teams of A / 4 threads take the parts in turn, eight in flight (another XCD has written them: a load is a trip to memory).
-template <typename T, int A, int NQ>
+// A divided segment's parts: the first at place note.z, then place 2 v of the shares v behind it up to note.w.  A work-group a
+// row and CB columns: teams of CB / 4 threads take the parts in turn, eight in flight (another XCD has written them: a load is a trip to
+// memory).  Segments of 128 parts and more: 32 columns, so that 256 parts are in flight (one key head of 256, 16 queries, 32768
+// slots, 23.6 us as a whole with all columns, 18.6 with 32; one of 128, 32 queries, 131072 slots, 32.1 and 28.2; but eight of 128
+// with 8192 slots, 32 parts each, 13.8 and 14.5).
+template <typename T, int A, int NQ, int CB>
 __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs args) {
-  constexpr int cols = A / 4, teams = 256 / cols;
+  constexpr int cols = CB / 4, teams = 256 / cols;
   __shared__ f32x4 sums[teams * cols];
   __shared__ float2 ends[teams];
-  const int w = blockIdx.x, most = args.group < 16 * NQ ? args.group : 16 * NQ, team = threadIdx.x / cols, col = (threadIdx.x - team * cols) * 4;
+  const int most = args.group < 16 * NQ ? args.group : 16 * NQ, team = threadIdx.x / cols;
+  const int col = (int)blockIdx.z * CB + (threadIdx.x - team * cols) * 4;
   const size_t place = (size_t)most * (A + 4);
   const float *base = args.part + (size_t)blockIdx.y * (A + 4);
   struct Part {
@@ -731,10 +747,10 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs args) {
       o = f32x4{0.f, 0.f, 0.f, 0.f};
     }
   };
-  const int4 j = args.joins[w];
+  const int4 j = args.joins[blockIdx.x];
   if (j.x < 0) return;
   const uint32_t head = (uint32_t)j.y, h = args.by_tiles(head), tile = head - h * args.by_tiles.d;
-  const int in = (int)tile * 16 * NQ + blockIdx.y, parts = j.w - w + 1;
+  const int in = (int)tile * 16 * NQ + blockIdx.y, w = j.z >> 1, parts = j.w - w + 1;
   if (in >= args.group) return;
   float top = -INFINITY, sum = 0.f;
   f32x4 o = {0.f, 0.f, 0.f, 0.f};
@@ -763,15 +779,17 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs args) {
       }
     }
     sums[threadIdx.x] = o;
-    if (col == 0) ends[team] = make_float2(top, sum);
+    if (threadIdx.x == team * cols) ends[team] = make_float2(top, sum);
   }
   __syncthreads();
   if (team != 0) return;
   const int used = parts < teams ? parts : teams;
+#pragma unroll 8
   for (int k = 1; k < used; ++k) top = fmaxf(top, ends[k].x);
   const float ref = top == -INFINITY ? 0.f : top;
   sum = 0.f;
   o = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 8
   for (int k = 0; k < used; ++k) {
     const float f = __builtin_amdgcn_exp2f(ends[k].x - ref);
     sum += f * ends[k].y;
@@ -865,6 +883,7 @@ namespace {
 // How a call's work is laid over the chip, from what the host knows: the table's width, not the lengths.
 struct AttendPlan {
   int nq, tiles, rows, groups;  // 16-query tiles of a wave; query tiles of a key head and their rows; shares (0: whole segments)
+  bool by_segment, many_parts;  // notes for the join; whether segments may be in so many parts that each goes to several work-groups
 };
 // Whole segments where a table has room for 96 KB of a key head's keys at most.  One work-group then takes 2 us and as many again for
 // every 256 slots of 64 elements; shares and their join take 2.5 us more at the least, but no longer for longer sequences.  us,
@@ -880,6 +899,11 @@ AttendPlan attend_plan(const CacheDims &d) {
   const int64_t slots = (int64_t)d.width * d.page, heads = (int64_t)d.Zkv * p.tiles, units = d.B * (slots / unit + 1) * heads;
   const bool whole = slots * d.A * (d.dtype == RSA_BF16 ? 2 : 4) <= 96 * 1024 || d.B > 4096 || units >= (1LL << 31);
   p.groups = whole ? 0 : (d.A == 64 ? 3 : d.A == 256 ? 1 : 2) * kCUs;
+  const int64_t segments = d.B * heads;
+  p.by_segment = segments <= p.groups;
+  // 128 parts a segment and more, where the table is full
+  const int64_t most = units < p.groups ? units : p.groups;
+  p.many_parts = most >= 128 * segments;
   return p;
 }
 size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
@@ -891,7 +915,9 @@ void launch_attend(const AttendArgs &a, const AttendPlan &p, hipStream_t st) {
     return;
   }
   attend_shares_kernel<T, A, NQ><<<p.groups, 64 * Attend<T, A, NQ>::kWaves, 0, st>>>(a);
-  attend_join_kernel<T, A, NQ><<<dim3(p.groups, p.rows), 256, 0, st>>>(a);
+  const uint32_t notes = a.by_segment ? a.B * a.Zkv * p.tiles : p.groups;
+  if (p.many_parts) attend_join_kernel<T, A, NQ, 32><<<dim3(notes, p.rows, A / 32), 256, 0, st>>>(a);
+  else attend_join_kernel<T, A, NQ, A><<<dim3(notes, p.rows), 256, 0, st>>>(a);
 }
 template <typename T, int A>
 void launch_attend(const AttendArgs &a, const AttendPlan &p, hipStream_t st) {
@@ -929,6 +955,7 @@ hipError_t cache_attend(const CacheDims &d, const void *Q, const void *Kc, const
   a.per = (d.B + 63) / 64;
   a.c = d.scale * kLog2e;
   a.joins = static_cast<int4 *>(ws);
+  a.by_segment = p.by_segment;
   a.part = reinterpret_cast<float *>(static_cast<char *>(ws) + align256(p.groups * sizeof(int4)));
   if (d.dtype == RSA_BF16) launch_attend<bf16_t>(a, p, d.A, st);
   else launch_attend<float>(a, p, d.A, st);

@@ -37,12 +37,19 @@ def test_whole_segments_or_shares(rec, kw, whole, queries):
     # (bf16 in a template's arguments stays as the compiler writes it: ..kernelI<type>Li<A>ELi<queries>E..)
     forms = [re.search(r"attend_(\w+?)_kernel(?:I\w+?Li|<float, )(\d+)(?:ELi|, )(\d)", x.name).groups() for x in k]
     assert forms == [(f, str(d.A), str(queries)) for f in (["whole"] if whole else ["shares", "join"])]
+    segments = d.B * d.Zkv * tiles
     if whole:
-        assert k[0].grid == (d.B * d.Zkv * tiles, 1, 1) and rsa.cache_workspace_bytes(d) == 0
+        assert k[0].grid == (segments, 1, 1) and rsa.cache_workspace_bytes(d) == 0
     else:
         shares, rows = k[0].grid[0], min(group, 16 * queries)
-        assert k[1].grid == (shares, rows, 1)
+        assert k[1].grid[:2] == (segments if segments <= shares else shares, rows)      # a work-group a note and row
         assert rsa.cache_workspace_bytes(d) >= 16 * shares + 2 * shares * rows * (d.A + 4) * 4
+
+
+@pytest.mark.parametrize("kw,blocks", [(dict(B=1, Z=4, Zkv=1, A=128, width=4096), 4), (dict(B=1, Z=4, Zkv=1, A=128, width=400), 1), (dict(B=2, Z=4, Zkv=2, A=128, width=4096), 4),
+                                       (dict(B=5, Z=4, Zkv=1, A=128, width=4096), 1), (dict(B=1, Z=40, Zkv=1, A=256, width=4096), 1), (dict(B=1, Z=30, Zkv=1, A=256, width=4096), 8)])
+def test_segments_of_many_parts_are_joined_by_columns(rec, kw, blocks):
+    assert attend(rec, cache(**kw))[1].grid[2] == blocks
 
 
 def test_one_byte_less_of_workspace_is_refused():

@@ -160,6 +160,9 @@ def test_results_that_do_not_fit():
         rsa.cache_append(d, x["K"], x["V"], x["Kc"], x["Vc"], x["table"], x["lengths"], Qr=x["Q"])
     with pytest.raises((ValueError, TypeError)):
         rsa.cache_append(d, x["K"], x["V"], x["Kc"], x["Vc"], None, x["lengths"])
+    none = x["K"][:, :, :0]
+    with pytest.raises(ValueError, match="argument"):
+        rsa.cache_append(d, none, none, x["Kc"], x["Vc"], x["table"], x["lengths"])
     K = torch.zeros(1, 2, 256, 64).bfloat16()
     d = rsa.make_desc(K, 4, rank_end=1)
     for bad in (dict(Q=K), dict(Q=K[:, :, :64].float()), dict(K=K[:, :, :64]), dict(K=K, Kr=K[:, :, :64]), dict(Qr=K)):

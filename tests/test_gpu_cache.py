@@ -112,6 +112,29 @@ def test_append_by_shares_of_strided_tensors():
     assert rsa.cache_append(d, K, V, pools[2], pools[3], table, lengths, counts, None, f) is None
 
 
+@pytest.mark.parametrize("B,T", [(4096, 9), (4097, 9), (5000, 1)])
+def test_append_for_many_sequences(B, T):
+    """... against calls for a few of them at a time."""
+    Zkv, A, page, W, pages = 1, 64, 8, 3, 3 * 5000
+    g = torch.Generator(device="cuda").manual_seed(23)
+    rng = np.random.default_rng(24)
+    Q, K, V = (torch.randn(B, Zkv, T, A, generator=g, device="cuda").bfloat16() for _ in range(3))
+    table = torch.randperm(pages, generator=g, device="cuda")[:B * W].reshape(B, W).int()
+    counts = np.where(rng.random(B) < 0.7, 0, rng.integers(-1, T + 2, B))
+    n, c = i32(rng.integers(0, W * page + 3, B)), i32(counts)
+    f = frequencies(A).cuda()
+
+    def run(step):
+        Kc = torch.zeros(pages, Zkv, page, A, dtype=torch.bfloat16, device="cuda")
+        Vc, Qr = torch.zeros_like(Kc), torch.full_like(Q, 3.0)
+        for b in range(0, B, step):
+            s = slice(b, b + step)
+            rsa.cache_append(rsa.make_cache_desc(Kc, table[s], Zkv), K[s], V[s], Kc, Vc, table[s], n[s], c[s], None, f, Q=Q[s], Qr=Qr[s])
+        return Kc, Vc, Qr
+    for x, y in zip(run(B), run(61)):
+        assert torch.equal(x, y) and (x != 0).any()
+
+
 def test_append_in_a_pool_beyond_32_bits():
     """A page whose elements lie more than 2^31 elements (4 GB) into the pool."""
     A, page, Zkv = 256, 64, 8
@@ -279,7 +302,8 @@ def vectorised(Q, Kc, Vc, table, lengths):
     ("bf16", 8, 2, 128, 64, [20000]), ("bf16", 4, 4, 64, 16, [9000, 1, 5000, 33]), ("bf16", 32, 1, 64, 16, [40000, 700]),
     ("bf16", 20, 4, 128, 48, [3000 + 61 * b for b in range(40)]), ("bf16", 6, 2, 256, 32, [7000, 8192, 12]),
     ("bf16", 5, 5, 192, 16, [6001, 2]), ("f32", 6, 3, 64, 24, [9000, 300, 4096]), ("f32", 20, 1, 128, 16, [6000] * 3),
-    ("bf16", 2, 1, 64, 16, [50 + 3 * b for b in range(700)])])
+    ("bf16", 2, 1, 64, 16, [50 + 3 * b for b in range(700)]), ("bf16", 16, 1, 256, 16, [9000]), ("f32", 3, 1, 192, 16, [5001]),
+    ("f32", 20, 1, 64, 16, [9999]), ("bf16", 3, 3, 192, 16, [300 + 5 * b for b in range(200)])])
 def test_long_and_many_sequences(dtype, Z, Zkv, A, page, lengths):
     g = torch.Generator(device="cuda").manual_seed(11)
     B, W = len(lengths), -(-max(lengths) // page)
@@ -361,6 +385,18 @@ def test_join(dtype, N, B, Z, A):
     within(O, rO, rel * size + STEP[dtype] * np.abs(rO), "O")
     within(LSE, rLSE, rel + 4 * F32 * np.abs(np.where(np.isinf(rLSE), 0, rLSE)), "LSE")
     assert (O[0, 0] == 0).all() and torch.isneginf(LSE[0, 0]).all()
+
+
+def test_join_into_a_projections_rows():
+    g = torch.Generator(device="cuda").manual_seed(22)
+    Op = torch.randn(3, 5, 4, 1, 64, generator=g, device="cuda").bfloat16()
+    LSEp = torch.randn(3, 5, 4, 1, generator=g, device="cuda")
+    pool, table = torch.zeros(1, 2, 16, 64, dtype=torch.bfloat16, device="cuda"), i32(np.zeros((5, 1)))
+    ref = rsa.cache_join(rsa.make_cache_desc(pool, table, 4), Op, LSEp)
+    y = torch.full((1, 4, 64, 64), 9.0, dtype=torch.bfloat16, device="cuda")
+    O = y.permute(2, 1, 0, 3)[:5]
+    got = rsa.cache_join(rsa.make_cache_desc(pool, table, 4, O=O), Op, LSEp, O)
+    assert torch.equal(got[0], ref[0]) and torch.equal(got[1], ref[1]) and (y[:, :, 5:] == 9).all()
 
 
 def test_join_of_ranks_that_share_a_cache():

@@ -21,6 +21,9 @@ CASES = [  # dtype, B, Z, L, N, ranks, A, R, adjacent, zigzag
     ("bf16", 2, 3, 128, 2, (1, 2), 64, 2, False, False),
     ("bf16", 1, 2, 128, 2, (0, 2), 128, 62, True, False),
     ("bf16", 1, 2, 128, 1, (0, 1), 128, 126, False, False),
+    ("bf16", 1, 3, 128, 2, (0, 2), 192, 192, False, False),      # heads that the two-pass layout alone has
+    ("bf16", 2, 1, 192, 3, (1, 3), 256, 250, False, False),
+    ("bf16", 1, 5, 64, 1, (0, 1), 256, 256, True, False),
     ("f32", 1, 2, 256, 4, (0, 4), 64, 64, False, False),
     ("f32", 2, 3, 192, 3, (1, 2), 192, 192, True, False),
     ("f32", 2, 2, 128, 2, (0, 2), 256, 256, False, False),
@@ -34,7 +37,7 @@ def setup(case, seed=0):
     dtype, B, Z, L, N, (rb, re), A, R, adjacent, zigzag = case
     rng = np.random.default_rng(seed)
     Q, K = normal(rng, (B, Z, (re - rb) * L // N, A), dtype), normal(rng, (B, Z, L, A), dtype)
-    d = rsa.make_desc(K, N, rank_begin=rb, rank_end=re, zigzag=zigzag, mode=rsa.MODE_STAGED if dtype == "f32" else rsa.MODE_FUSED)
+    d = rsa.make_desc(K, N, rank_begin=rb, rank_end=re, zigzag=zigzag, mode=rsa.MODE_STAGED if dtype == "f32" or A > 128 else rsa.MODE_FUSED)
     pos = oracle.tokens(L, N, rb, re, zigzag), np.arange(L)
     return d, Q, K, pos, frequencies(R)
 
