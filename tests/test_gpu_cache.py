@@ -323,6 +323,37 @@ def test_long_and_many_sequences(dtype, Z, Zkv, A, page, lengths):
     assert torch.equal(again[0], O) and torch.equal(again[1], LSE)            # sums in a fixed order
 
 
+@pytest.mark.parametrize("dtype,Z,Zkv,A,B", [
+    ("bf16", 16, 1, 256, 1), ("bf16", 32, 1, 128, 2), ("f32", 2, 1, 64, 3),                # segments of many parts
+    ("bf16", 8, 2, 128, 5), ("f32", 6, 3, 64, 4), ("bf16", 40, 40, 64, 30)])               # of fewer; more segments than shares
+def test_a_workspace_in_which_a_longer_call_has_left_its_notes(dtype, Z, Zkv, A, B):
+    """Every call of one workspace against the same call of its own: what lies there does not count."""
+    page, W = 16, 2048 if B < 30 else 256
+    g = torch.Generator(device="cuda").manual_seed(23)
+    pages = W if B < 30 else 1000
+    Kc, Vc = (torch.randn(pages, Zkv, page, A, generator=g, device="cuda").to(DTYPES[dtype]) for _ in range(2))
+    table = torch.randint(pages, (B, W), generator=g, device="cuda", dtype=torch.int32)
+    Q = torch.randn(B, Z, 1, A, generator=g, device="cuda").to(DTYPES[dtype])
+    d = rsa.make_cache_desc(Kc, table, Z)
+    n = rsa.cache_workspace_bytes(d)
+    assert n > 0
+    used = torch.full((n,), 0xFF, dtype=torch.uint8, device="cuda")
+    most = W * page
+    for lengths in ([most] * B, [most - 1 - 37 * b for b in range(B)], [0] * (B - 1) + [1], [0] * B, [most // 2] + [0] * (B - 1),
+                    [most if b % 2 else 0 for b in range(B)], [1] * B, [0] * B, [700 - 23 * b for b in range(B)]):
+        O, LSE = rsa.cache_attend(d, Q, Kc, Vc, table, i32(lengths), ws=used)
+        fresh = torch.full((n,), 0xFF, dtype=torch.uint8, device="cuda")
+        own = rsa.cache_attend(d, Q, Kc, Vc, table, i32(lengths), ws=fresh)
+        assert torch.equal(O, own[0]) and torch.equal(LSE, own[1])
+        none = i32(lengths) <= 0
+        assert (O[none] == 0).all() and torch.isneginf(LSE[none]).all()
+        assert torch.isfinite(LSE[~none]).all()
+        # (a row of the first slot alone is its value)
+        if lengths == [1] * B:
+            v = Vc[table[:, 0].long(), :, 0].repeat_interleave(Z // Zkv, 1).unsqueeze(2)
+            within(O, f64(v), f64(v.abs().double() * (STEP[dtype] + 2.0 ** -15 + 2.0 ** -20)), "O")
+
+
 @pytest.mark.parametrize("B", [65, 4096, 4097])
 def test_more_sequences_than_lanes(B):
     """Most of them empty or short, on pages that they share, in tables with room for long ones."""
