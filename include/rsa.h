@@ -325,7 +325,7 @@ int rsa_rotate_bwd(const rsa_desc *d, int32_t R, int32_t adjacent, const float *
  * tokens that the call appends included; slots below 0 or behind the table do not exist.
  * Tables and lengths are device memory that the kernels check, so a
  * captured graph replays with new contents.  Key head h serves query heads [h Z/Zkv, (h+1) Z/Zkv).
- * bf16 (fp32 sums and softmax, probabilities to 2^-15, one rounding per stored element) or fp32 (fp32
+ * bf16 (fp32 sums, softmax and probabilities, one rounding per stored element) or fp32 (fp32
  * multiply-adds), A a multiple of 64 up to 256, any page size, B below 2^16, B * Z below 2^24, width * page below 2^31, pages * Zkv * page below 2^32.
  */
 typedef struct {

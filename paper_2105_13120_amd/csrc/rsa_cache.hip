@@ -331,6 +331,11 @@ __device__ __forceinline__ float xrow_max(float x) {
   return fmaxf(__builtin_bit_cast(float, a), __builtin_bit_cast(float, b));
 }
 
+// The eight bits of x that a bf16 number has, cut off behind.
+__device__ __forceinline__ float first_bits(float x) {
+  return __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, x) & 0xffff0000u);
+}
+
 template <typename T, int A, int NQ>
 struct Attend {
   static constexpr int kKeys = AttendShape<T>::kKeys;
@@ -482,23 +487,29 @@ struct Attend {
           for (int e = 0; e < kDw; ++e) vr[j][b][e] = (seen >> key_of(j)) & 1 ? vr[j][b][e] : 0u;
     }
     if constexpr (kHalf) {
-      // The matrix core takes bf16: a probability goes to it as two, its first eight bits and what they leave of it, of which 2^-15
-      // is lost (one rounded number of 2^-8 made half as much error as the result's own rounding; the matrix cores wait for
-      // memory all the same, 0.1 us of a call of 5).  Neither is ever 0 or negative where the probability is not: times an infinite
-      // value that were NaN.
-      bf16x8 pb[NQ], pr[NQ];
+      // The matrix core takes bf16: a probability goes to it as three, its first eight bits, the next eight and the rest, all 24 of
+      // it (as two, 2^-16 of it is lost, which shows where values cancel; the matrix cores wait for memory all the same).  No part is 0
+      // where the probability is not: times an infinite value that were NaN.
+      bf16x8 pb[NQ][3];
 #pragma unroll
       for (int x = 0; x < NQ; ++x) {
-        u32x4 w, v;
+        u32x4 w[3];
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-          const float y = p[x][k >> 1 ? KT - 1 : 0][2 * (k & 1)], z = p[x][k >> 1 ? KT - 1 : 0][2 * (k & 1) + 1];
-          w[k] = __builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, z), __builtin_bit_cast(uint32_t, y), 0x07060302u);
-          v[k] = pack_bf16(fmaxf(y - __builtin_bit_cast(float, w[k] << 16), y * 0x1p-26f),
-                           fmaxf(z - __builtin_bit_cast(float, w[k] & 0xffff0000u), z * 0x1p-26f));
+          float part[3][2];
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const float y = p[x][k >> 1 ? KT - 1 : 0][2 * (k & 1) + e], least = y * 0x1p-26f, r = y - first_bits(y);
+            part[0][e] = y;
+            part[1][e] = fmaxf(r, least);
+            part[2][e] = fmaxf(r - first_bits(r), least);
+          }
+#pragma unroll
+          for (int i = 0; i < 3; ++i)
+            w[i][k] = __builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, part[i][1]), __builtin_bit_cast(uint32_t, part[i][0]), 0x07060302u);
         }
-        pb[x] = __builtin_bit_cast(bf16x8, w);
-        pr[x] = __builtin_bit_cast(bf16x8, v);
+#pragma unroll
+        for (int i = 0; i < 3; ++i) pb[x][i] = __builtin_bit_cast(bf16x8, w[i]);
       }
 #pragma unroll
       for (int b = 0; b < NB; ++b)
@@ -510,10 +521,10 @@ struct Attend {
             w[k] = __builtin_amdgcn_perm(vr[(2 * k + 1) % VR][b][(i >> 1) % kDw], vr[(2 * k) % VR][b][(i >> 1) % kDw],
                                          i & 1 ? 0x07060302u : 0x05040100u);
 #pragma unroll
-          for (int x = 0; x < NQ; ++x) {
-            acc[x][b * VW + i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, w), pr[x], acc[x][b * VW + i], 0, 0, 0);
-            acc[x][b * VW + i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, w), pb[x], acc[x][b * VW + i], 0, 0, 0);
-          }
+          for (int x = 0; x < NQ; ++x)
+#pragma unroll
+            for (int n = 2; n >= 0; --n)
+              acc[x][b * VW + i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, w), pb[x][n], acc[x][b * VW + i], 0, 0, 0);
         }
     } else {
 #pragma unroll

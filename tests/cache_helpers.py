@@ -41,7 +41,7 @@ def attend_bounds(Q, Kc, Vc, table, lengths, O, LSE, dtype, scale=None):
     """Bounds of |O| and |LSE| errors against fp64, from the definition.  A score is a sum of A products in fp32, off by at most
     dS = (A + 4) 2^-24 s sum|q k| (the scale and the exponent's argument are the 4); exp adds 2^-22, so probabilities are off by
     2 dS + 2^-21 relative to their normalised value, and n terms' sum by n 2^-24 at most.  In bf16 the probabilities that
-    weigh V are two bf16 numbers each, eight bits and what they leave, rounded: off by 2^-15.  The stored O is rounded once."""
+    weigh V may be two bf16 numbers each, eight bits and what they leave, rounded: off by 2^-15.  The stored O is rounded once."""
     B, Z, _, A = Q.shape
     pages, Zkv, page, _ = Kc.shape
     s = 1.0 / np.sqrt(A) if scale is None else scale

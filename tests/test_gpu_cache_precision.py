@@ -1,0 +1,50 @@
+"""How exactly a new token attends and shares are joined, where a lost bit shows."""
+import numpy as np
+import pytest
+import torch
+
+from cache_helpers import F32, STEP, f64, within
+from paper_2105_13120_amd import rsa
+
+pytestmark = pytest.mark.gpu
+
+
+def one_page(keys, values, width, room=64):
+    """Pools, table and lengths of sequences (B, Zkv, n, A), a page of `room` slots each, in tables of `width` entries."""
+    B, Zkv, n, A = keys.shape
+    Kc, Vc = (torch.full((B, Zkv, room, A), float("nan"), dtype=keys.dtype) for _ in range(2))
+    Kc[:, :, :n], Vc[:, :, :n] = keys, values
+    table = torch.full((B, width), -1, dtype=torch.int32)
+    table[:, 0] = torch.arange(B)
+    return Kc.cuda(), Vc.cuda(), table.cuda(), torch.full((B,), n, dtype=torch.int32).cuda()
+
+
+def cancelling(n, B=64, Z=16, A=64):
+    """Two slots of n count, the first and the last: probabilities 1 and p of each query before they are divided by their sum,
+    and in each column values that cancel for one of the queries.  Scores are single products (k = 0, -1 and, for slots that do
+    not count, -30000)."""
+    rng = np.random.default_rng(30 + n)
+    Q, K, V = torch.zeros(B, Z, 1, A).bfloat16(), torch.zeros(B, 1, n, A).bfloat16(), torch.ones(B, 1, n, A).bfloat16()
+    Q[..., 0, 0] = torch.from_numpy(rng.uniform(1, 16, (B, Z))).bfloat16()
+    K[:, 0, 1:n - 1, 0], K[:, 0, n - 1, 0] = -30000.0, -1.0
+    p = torch.exp(-Q[..., 0, 0].double() / 8)
+    V[:, 0, 0] = torch.from_numpy(rng.uniform(0.5, 2, (B, A))).bfloat16()
+    V[:, 0, n - 1] = (-V[:, 0, 0].double() / p[:, torch.arange(A) % Z]).bfloat16()
+    P = torch.stack([torch.ones_like(p), p], -1)
+    v = V[:, 0, [0, n - 1]].double()
+    total = P.sum(-1, keepdim=True)
+    return Q, K, V, (P @ v / total)[:, :, None].numpy(), (P @ v.abs() / total)[:, :, None].numpy()
+
+
+@pytest.mark.parametrize("width", [1, 1000])            # whole segments; shares
+@pytest.mark.parametrize("n", [2, 30, 40])
+def test_probabilities_are_held_to_32_bits(n, width):
+    """Scores (below 2) are exact, their products by the scale and log2(e) off by 4 roundings, exp by 2^-22: p is off by 2^-20 at
+    most, and the sums of two that count by a rounding each; the result is rounded once."""
+    Q, K, V, O, PV = cancelling(n)
+    Kc, Vc, table, lengths = one_page(K, V, width)
+    d = rsa.make_cache_desc(Kc, table, Q.shape[1])
+    assert (rsa.cache_workspace_bytes(d) > 0) == (width == 1000)
+    got, _ = rsa.cache_attend(d, Q.cuda(), Kc, Vc, table, lengths)
+    assert (np.abs(O) < 2.0 ** -11 * PV).sum() > 500    # (many cancel)
+    within(got, O, (2.0 ** -20 + 6 * F32) * PV + STEP["bf16"] * np.abs(O), "O")
