@@ -48,3 +48,20 @@ def test_probabilities_are_held_to_32_bits(n, width):
     got, _ = rsa.cache_attend(d, Q.cuda(), Kc, Vc, table, lengths)
     assert (np.abs(O) < 2.0 ** -11 * PV).sum() > 500    # (many cancel)
     within(got, O, (2.0 ** -20 + 6 * F32) * PV + STEP["bf16"] * np.abs(O), "O")
+
+
+@pytest.mark.parametrize("width", [1, 1000])
+@pytest.mark.parametrize("sign", [1, -1])
+def test_an_infinite_value_under_a_small_probability(width, sign):
+    """Probabilities of 2^-125 to 2^-87 of the row's largest: fp32 holds them, so an infinite value is the result."""
+    B, Z, A = 64, 16, 64
+    rng = np.random.default_rng(33)
+    Q, K, V = torch.zeros(B, Z, 1, A).bfloat16(), torch.zeros(B, 1, 30, A).bfloat16(), torch.ones(B, 1, 30, A).bfloat16()
+    Q[..., 0, 0] = torch.from_numpy(rng.uniform(60, 87, (B, Z))).bfloat16()
+    K[:, 0, 1, 0], K[:, 0, 2:, 0] = -1.0, -30000.0
+    V[:, 0, 1, 5] = sign * float("inf")
+    Kc, Vc, table, lengths = one_page(K, V, width)
+    got, LSE = rsa.cache_attend(rsa.make_cache_desc(Kc, table, Z, scale=1.0), Q.cuda(), Kc, Vc, table, lengths)
+    want = torch.ones(B, Z, 1, A).bfloat16()
+    want[..., 5] = sign * float("inf")
+    assert torch.equal(got.cpu(), want) and (LSE == 0).all()
