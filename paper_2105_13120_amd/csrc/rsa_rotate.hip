@@ -60,25 +60,35 @@ TurnShape make_turn_shape(int A, int R, int dtype) {
 }
 constexpr int kTurnAngles = 1024;  // of a work-group at most: 8 rows of 128 pairs
 
-// A thread's place in that, and what it turns by: y = x co + partner si.
+// A thread's place in that.
+struct Place {
+  int lane, group, row, c;  // group: which head; row, c: row of the tile, chunk of the row
+  __host__ __device__ __forceinline__ Place(const TurnShape &s, uint32_t thread) {
+    const int wave = (int)(thread >> 6);
+    lane = (int)(thread & 63);
+    const int in = (int)s.by_chunks((uint32_t)lane);
+    group = s.waves == 1 ? wave : s.waves == 2 ? wave >> 1 : 0;
+    // Lanes behind the wave's whole rows (heads of 192 leave 16) have none: a row behind the tile's, and a chunk behind a row's, whose
+    // elements nothing turns.
+    const bool some = in < s.wave_rows;
+    row = some ? (wave - group * s.waves) * s.wave_rows + in : 1 << 20;
+    c = some ? lane - in * s.chunks : lane;
+  }
+};
+// Where the element that e of a row is turned with is, in pairs half the turned part apart.
+__host__ __device__ __forceinline__ int partner_of(int e, int R) { return e < R / 2 ? e + R / 2 : e < R ? e - R / 2 : e; }
+
+// What a thread turns by: y = x co + partner si.
 // WHOLE: a chunk is turned as a whole or not, and its partner in a half is one lane's chunk.
 bool whole_chunks(int dtype, int R, int adjacent) {
   const int w = dtype == RSA_BF16 ? 8 : 4;
   return R % (adjacent ? w : 2 * w) == 0;
 }
-template <typename T, bool WHOLE> struct Turn {
+template <typename T, bool WHOLE> struct Turn : Place {
   static constexpr int W = Chunk<T>::W;
-  int lane, group, row, c;  // group: which head; row, c: row of the tile (none: at least its rows), chunk of the row
   float co[W], si[W];
 
-  __device__ __forceinline__ explicit Turn(const TurnShape &s) {
-    const int wave = threadIdx.x >> 6;
-    lane = threadIdx.x & 63;
-    const int in = (int)s.by_chunks((uint32_t)lane);
-    c = lane - in * s.chunks;
-    group = s.waves == 1 ? wave : s.waves == 2 ? wave >> 1 : 0;
-    row = in < s.wave_rows ? (wave - group * s.waves) * s.wave_rows + in : 1 << 20;
-  }
+  __device__ __forceinline__ explicit Turn(const TurnShape &s) : Place(s, threadIdx.x) {}
   // the angles of this thread's elements, from those of its row
   __device__ __forceinline__ void take(const Rotary &ro, const float2 *angles) {
     const int half = ro.R / 2;
@@ -110,7 +120,7 @@ template <typename T, bool WHOLE> struct Turn {
         float v[2];
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-          const int e = c * W + k + j, from = e < half ? e + half : e < ro.R ? e - half : e;
+          const int from = partner_of(c * W + k + j, ro.R);
           T z;
           __builtin_memcpy(&z, mine + from * sizeof(T), sizeof(T));
           v[j] = (float)z;
