@@ -3,7 +3,8 @@ import numpy as np
 import pytest
 import torch
 
-from cache_helpers import F32, STEP, f64, within
+from cache_helpers import DTYPES, F32, STEP, f64, within
+from oracle import cache as oracle
 from paper_2105_13120_amd import rsa
 
 pytestmark = pytest.mark.gpu
@@ -65,3 +66,25 @@ def test_an_infinite_value_under_a_small_probability(width, sign):
     want = torch.ones(B, Z, 1, A).bfloat16()
     want[..., 5] = sign * float("inf")
     assert torch.equal(got.cpu(), want) and (LSE == 0).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("level", [0.0, 12.0, -100.0, 1000.0, -30000.0])
+def test_joined_weights_go_by_the_differences_alone(dtype, level):
+    """Shares whose LSE lie around any level.  A weight exp(l - l') of a difference below D: the difference and its product by log2(e) are
+    off by a rounding each, 2 D 2^-24 relative, exp by 2^-22; the running maximum moves three times at most, each another such
+    factor of D and 2^-22.  The sums have N terms; LSE is rounded once more, and log adds 2^-22."""
+    N, B, Z, A = 16, 40, 8, 64
+    rng = np.random.default_rng(34)
+    Op = torch.from_numpy(rng.standard_normal((N, B, Z, 1, A))).to(DTYPES[dtype])
+    LSEp = torch.from_numpy(rng.standard_normal((N, B, Z, 1)) * 2 + level).float()
+    O, LSE = oracle.join(f64(Op), f64(LSEp))
+    D = float(LSEp.max(0).values.sub(LSEp.min(0).values).max())
+    assert D < 16
+    rel = 2 * 4 * (2 * D * F32 + 2.0 ** -22) + 2 * N * F32             # (of the weights and of their sum)
+    w = np.exp(f64(LSEp) - LSE)
+    size = (w[..., None] * np.abs(f64(Op))).sum(0)
+    pool, table = torch.zeros(1, Z, 16, A, dtype=DTYPES[dtype], device="cuda"), torch.zeros(B, 1, dtype=torch.int32, device="cuda")
+    got = rsa.cache_join(rsa.make_cache_desc(pool, table, Z), Op.cuda(), LSEp.cuda())
+    within(got[0], O, rel * size + STEP[dtype] * np.abs(O), "O")
+    within(got[1], LSE, rel + 2.0 ** -22 + F32 * np.abs(LSE), "LSE")
