@@ -727,7 +727,15 @@ __global__ __launch_bounds__((64 * Attend<T, A, NQ>::kWaves), (Attend<T, A, NQ>:
     in = 0;
     if (unit < end && ++head == heads) {
       head = 0;
-      do len = __builtin_amdgcn_readfirstlane(length_of(args, ++b)); while (len == 0);  // (units are left: there is such a sequence)
+      // the next sequence that is not empty, of 64 at a time (one by one, 2000 empty ones took 150 us)
+      for (++b; b < args.B; b += 64) {
+        const uint32_t x = b + at.lane < args.B ? length_of(args, b + at.lane) : 0u;
+        const uint64_t some = __ballot(x > 0);
+        if (some == 0) continue;
+        b += __builtin_ctzll(some);
+        len = __builtin_amdgcn_readlane(x, __builtin_ctzll(some));
+        break;
+      }
       n = (len + At::kUnit - 1) / At::kUnit;
     }
   }
