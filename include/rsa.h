@@ -327,6 +327,8 @@ int rsa_rotate_bwd(const rsa_desc *d, int32_t R, int32_t adjacent, const float *
  * captured graph replays with new contents.  Key head h serves query heads [h Z/Zkv, (h+1) Z/Zkv).
  * bf16 (fp32 sums, softmax and probabilities, one rounding per stored element) or fp32 (fp32
  * multiply-adds), A a multiple of 64 up to 256, any page size, B below 2^16, B * Z below 2^24, width * page below 2^31, pages * Zkv * page below 2^32.
+ * Results over other tensors of a call, where it does not allow that, are refused (RSA_ERR_UNSUPPORTED) if neither has gaps; in the gaps of
+ * strided ones another may lie, and what overlaps there is for the caller to see.
  */
 typedef struct {
   int32_t B;          /* sequences of a call (rows of the table)               */

@@ -102,6 +102,27 @@ int check_rank_chunk(const Dims &d, int n, int j) {
   return RSA_OK;
 }
 
+// Memory of a tensor: n bytes in one piece; 0 of one that is not given, or whose strides leave gaps (another may lie there).
+struct Piece {
+  const void *p;
+  size_t n;
+  Piece(const void *p_, size_t n_) : p(p_), n(p_ ? n_ : 0) {}
+};
+Piece rows_of(const rsa::CacheDims &d, const void *p, const int64_t *st, int64_t heads, int64_t tokens) {
+  const bool dense = st[0] == heads * tokens * d.A && st[1] == tokens * d.A && st[2] == d.A;
+  return {p, dense ? (size_t)d.B * heads * tokens * d.A * (d.dtype == RSA_BF16 ? 2 : 4) : 0};
+}
+Piece pool_of(const rsa::CacheDims &d, const void *p) {
+  return {p, (size_t)d.pages * d.Zkv * d.page * d.A * (d.dtype == RSA_BF16 ? 2 : 4)};
+}
+Piece words_of(const void *p, int64_t n) { return {p, (size_t)n * 4}; }
+// whether a result lies over another tensor of the call (elsewhere kernels would read what they or others have written)
+bool lies_over(const Piece &out, std::initializer_list<Piece> others) {
+  for (const Piece &x : others)
+    if (out.n && x.n && rsa::overlap(out.p, out.n, x.p, x.n)) return true;
+  return false;
+}
+
 }  // namespace
 
 extern "C" {
@@ -523,9 +544,6 @@ int cache_validate(const rsa_cache_desc *d, int32_t tokens, rsa::CacheDims *out)
   }
   return RSA_OK;
 }
-size_t pool_bytes(const rsa::CacheDims &d) {
-  return (size_t)d.pages * d.Zkv * d.page * d.A * (d.dtype == RSA_BF16 ? 2 : 4);
-}
 }  // namespace
 
 #define RSA_CACHE_PROLOGUE(tokens, ptr_ok, ...)                   \
@@ -552,7 +570,14 @@ int rsa_cache_append(const rsa_cache_desc *d, int32_t T, const void *Q, const vo
   if (!words({table, lengths, counts, first, inv_freq})) return RSA_ERR_UNSUPPORTED;
   if (!inv_freq) R = 0;
   if (inv_freq && (R < 2 || R > dm.A)) return RSA_ERR_SHAPE;
-  if (R % 2 != 0 || rsa::overlap(Kc, pool_bytes(dm), Vc, pool_bytes(dm))) return RSA_ERR_UNSUPPORTED;
+  if (R % 2 != 0) return RSA_ERR_UNSUPPORTED;
+  const Piece k = rows_of(dm, K, dm.ks, dm.Zkv, T), v = rows_of(dm, V, dm.ks, dm.Zkv, T), q = rows_of(dm, Q, dm.qs, dm.Z, T);
+  const Piece qr = rows_of(dm, Qr, dm.qs, dm.Z, T), keys = pool_of(dm, Kc), values = pool_of(dm, Vc);
+  const Piece t = words_of(table, (int64_t)dm.B * dm.width), n = words_of(lengths, dm.B), c = words_of(counts, dm.B);
+  const Piece f = words_of(first, dm.B), w = words_of(inv_freq, R / 2);
+  if (lies_over(keys, {values, k, v, q, qr, t, n, c, f, w}) || lies_over(values, {k, v, q, qr, t, n, c, f, w}) ||
+      lies_over(qr, {k, v, t, n, c, f, w}) || (Qr != Q && lies_over(qr, {q})))
+    return RSA_ERR_UNSUPPORTED;
   return hip_status(rsa::cache_append(dm, T, R, adjacent != 0, inv_freq, Q, K, V, table, lengths, counts, first, Qr, Kc, Vc, st));
 }
 
@@ -567,6 +592,11 @@ int rsa_cache_attend(const rsa_cache_desc *d, const void *Q, const void *Kc, con
   if (!words({table, lengths, LSE})) return RSA_ERR_UNSUPPORTED;
   const size_t need = rsa::cache_workspace_bytes(dm);
   if (need > 0 && (!ws || ws_bytes < need)) return RSA_ERR_WORKSPACE;
+  const Piece q = rows_of(dm, Q, dm.qs, dm.Z, 1), keys = pool_of(dm, Kc), values = pool_of(dm, Vc);
+  const Piece t = words_of(table, (int64_t)dm.B * dm.width), n = words_of(lengths, dm.B);
+  const Piece o = rows_of(dm, O, dm.os, dm.Z, 1), l = words_of(LSE, (int64_t)dm.B * dm.Z), w(ws, need);
+  if (lies_over(o, {q, keys, values, t, n, l, w}) || lies_over(l, {q, keys, values, t, n, w}) || lies_over(w, {q, keys, values, t, n}))
+    return RSA_ERR_UNSUPPORTED;
   return hip_status(rsa::cache_attend(dm, Q, Kc, Vc, table, lengths, O, LSE, ws, st));
 }
 
@@ -574,9 +604,10 @@ int rsa_cache_join(const rsa_cache_desc *d, int32_t N, const void *Op, const flo
   RSA_CACHE_PROLOGUE(1, Op && LSEp && O && LSE, Op, O);
   if (!words({LSEp, LSE})) return RSA_ERR_UNSUPPORTED;
   if (N < 1) return RSA_ERR_SHAPE;
-  const size_t rows = (size_t)dm.B * dm.Z, es = dm.dtype == RSA_BF16 ? 2 : 4;
-  if (rsa::overlap(LSE, rows * 4, LSEp, N * rows * 4) || rsa::overlap(LSE, rows * 4, Op, N * rows * dm.A * es))
-    return RSA_ERR_UNSUPPORTED;
+  const int64_t rows = (int64_t)dm.B * dm.Z;
+  const Piece op(Op, (size_t)N * rows * dm.A * (dm.dtype == RSA_BF16 ? 2 : 4)), lp = words_of(LSEp, N * rows);
+  const Piece o = rows_of(dm, O, dm.os, dm.Z, 1), l = words_of(LSE, rows);
+  if (lies_over(o, {op, lp, l}) || lies_over(l, {op, lp})) return RSA_ERR_UNSUPPORTED;
   return hip_status(rsa::cache_join(dm, N, Op, LSEp, O, LSE, st));
 }
 
