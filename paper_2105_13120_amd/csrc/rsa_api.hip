@@ -135,8 +135,10 @@ const char *rsa_strerror(int status) {
     case RSA_ERR_NULL: return "a required pointer is NULL";
     case RSA_ERR_SHAPE: return "bad shape: sizes must be positive, L divisible by N, ranks within [0, N), Z by Zkv, 2 <= R <= A";
     case RSA_ERR_UNSUPPORTED:
-      return "unsupported: need a head size of 64 or 128 (staged mode: a multiple of 64 up to 256), L/N "
-             "divisible by 64, 16-byte aligned pointers, bf16 for the fused mode";
+      return "unsupported: pointers and strides need 16-byte alignment (tables, counts, frequencies and LSE of the cache's calls 4), "
+             "flags must be the descriptor's own, sizes within the limits that rsa.h names for the call; calls of the ring need a "
+             "head size of 64 or 128 (staged mode: a multiple of 64 up to 256), L/N divisible by 64, bf16 for the fused mode; "
+             "the rotation an even R; calls on the cache a head size that is a multiple of 64 up to 256, and no result over another tensor";
     case RSA_ERR_WORKSPACE: return "workspace missing or too small";
     case RSA_ERR_HIP: return "a HIP call failed";
     default: return "unknown status";

@@ -85,3 +85,13 @@ def test_slices_of_one_projection_may_lie_between_each_other(rec):
     assert append(rec, at, desc(q_stride=packed, kv_stride=packed)) == 0
     every = (2 * Z * A, 2 * A, A)
     assert attend(rec, {**AT, "O": AT["Q"] + A * 2}, desc(q_stride=every, o_stride=every)) == 0
+
+
+def test_what_a_refusal_says():
+    """One text for all calls: it names what the cache's and the rotation's need, not the ring's limits alone."""
+    said = rsa.strerror(-3)
+    for word in ("even R", "calls on the cache", "strides", "flags", "over another tensor", "calls of the ring", "head size of 64 or 128"):
+        assert word in said, word
+    odd = desc()
+    odd.flags = 1
+    assert rsa.lib().rsa_cache_join(ctypes.byref(odd), 1, None, None, None, None, None) == -3
