@@ -127,7 +127,7 @@ template <typename T, int W> struct Pair {
 // How the 256 threads of a work-group lie over rows and heads: groups of `lanes` threads take one head's `rows` rows,
 // `units` threads a row, 256 / lanes heads at a time.  The rows' R / 2 angles each are shared through LDS by all heads; there are
 // at most lanes * W.
-struct TurnShape {
+struct AppendShape {
   int lanes, rows;
   FastDiv by_lanes, by_units, by_half;  // threads of a group; of a row; R / 2 angles of a row
 };
@@ -137,11 +137,11 @@ int chunk_width(int dtype, int R) {
   return R % 16 == 0 ? 8 : R % 8 == 0 ? 4 : R % 4 == 0 ? 2 : 1;
 }
 // heads of a thread whose loads are in flight
-template <typename T, int W> constexpr int kAhead = W * (int)sizeof(T) >= 8 ? 2 : 4;
+template <typename T, int W> constexpr int kPairsAhead = W * (int)sizeof(T) >= 8 ? 2 : 4;
 // 32 threads a group, or as many more as a row needs
-TurnShape make_turn_shape(int A, int R, int W) {
+AppendShape make_append_shape(int A, int R, int W) {
   const int units = A / (2 * W);
-  TurnShape s;
+  AppendShape s;
   s.lanes = units <= 32 ? 32 : units <= 64 ? 64 : 128;
   s.rows = s.lanes / units;
   s.by_lanes = make_fast_div(s.lanes); s.by_units = make_fast_div(units); s.by_half = make_fast_div(R > 1 ? R / 2 : 1);
@@ -154,7 +154,7 @@ struct AppendArgs {
   const int32_t *table, *lengths, *counts, *first;
   int64_t qs[3], ks[3];
   Rotary ro;
-  TurnShape shape;
+  AppendShape shape;
   FastDiv by_T, by_page, by_split;  // by_split: work-groups that share a tile's heads
   int B, Zq, Zkv, A, pages, width;  // Zq: 0 without queries
   uint32_t tokens;                  // B T
@@ -177,12 +177,12 @@ __device__ __forceinline__ Token token_of(const AppendArgs &a, uint32_t b, uint3
 
 // A work-group takes a few tokens, works out their angles (one a thread), turns their heads of Q and K and moves those of V.
 // Where sequences have uneven numbers of tokens, every wave counts the tiles that there are and the work-groups take them in
-// turn (work-groups for all B T tokens: of 16384 tokens 6700 there, the other tiles' work-groups took 10 us).
+// turn (work-groups for all B T tokens: of 16384 tokens 7144 there, the other tiles' work-groups took 10 us).
 template <typename T, int W>
 __global__ __launch_bounds__(256, 4) void append_kernel(AppendArgs args) {
-  constexpr int ahead = kAhead<T, W>;
+  constexpr int ahead = kPairsAhead<T, W>;
   __shared__ float2 angles[256];
-  const TurnShape &sh = args.shape;
+  const AppendShape &sh = args.shape;
   const uint32_t tid = threadIdx.x, head0 = sh.by_lanes(tid), lane = tid - head0 * sh.lanes, rr = sh.by_units(lane), rows = sh.rows;
   const int u = (int)(lane - rr * sh.by_units.d), heads = 256 / sh.lanes, half = args.ro.R / 2;
   const int2 at = Pair<T, W>::place(args.ro, u);
@@ -304,7 +304,7 @@ struct AttendArgs {
   FastDiv by_page, by_tiles;  // by_tiles: query tiles of a key head
   int B, Z, Zkv, group, pages, width, per;  // per: sequences a lane counts
   float c;           // scale log2(e)
-  float *part;       // partial results, nullptr: whole segments
+  float *part;       // partial results of divided segments (whole segments have none)
   int4 *joins;
   int by_segment;    // one note a segment, else one a share
 };
@@ -885,7 +885,7 @@ hipError_t cache_append(const CacheDims &d, int T, int R, int adjacent, const fl
   for (int k = 0; k < 3; ++k) { a.qs[k] = d.qs[k]; a.ks[k] = d.ks[k]; }
   const int W = chunk_width(d.dtype, R);
   a.ro = {R, adjacent, inv_freq, 1.f};
-  a.shape = make_turn_shape(d.A, R, W);
+  a.shape = make_append_shape(d.A, R, W);
   a.by_T = make_fast_div(T); a.by_page = make_fast_div(d.page);
   a.B = d.B; a.Zq = Q ? d.Z : 0; a.Zkv = d.Zkv; a.A = d.A; a.pages = d.pages; a.width = d.width;
   a.tokens = (uint32_t)((int64_t)d.B * T);
@@ -914,7 +914,9 @@ struct AttendPlan {
 // every 256 slots of 64 elements; shares and their join take 2.5 us more at the least, but no longer for longer sequences.  us,
 // shares and whole segments: 16 key heads of 64 with 768 slots 7.8 and 7.0, with 1024 7.8 and 9.1; 8 of 128, four queries each, 384
 // slots 8.1 and 6.4, 768 8.8 and 9.8; four of 256, 192 slots 10.3 and 8.0, 384 10.8 and 12.1; fp32, 48 of 64, 384 slots 8.3 and 8.9.
-// Shares: up to three a CU for heads of 64, two, or with heads of 256 one, as registers leave room.
+// Shares: up to three a CU for heads of 64, two, or with heads of 256 one, as registers leave room.  More than 4096 sequences (a lane
+// counts 64) or 2^31 units go by whole segments whatever their length: one sequence of 131072 slots among 4095 of 64 takes 122 us, among
+// 4096 of them 1730.
 AttendPlan attend_plan(const CacheDims &d) {
   AttendPlan p;
   const int group = d.Z / d.Zkv, unit = 64;  // (of at least that many slots)

@@ -10,8 +10,8 @@ namespace rsa {
 namespace {
 
 // 16 bytes of a row.
-template <typename T> struct Chunk;
-template <> struct Chunk<bf16_t> {
+template <typename T> struct RowChunk;
+template <> struct RowChunk<bf16_t> {
   static constexpr int W = 8;
   u32x4 r;
   __device__ __forceinline__ float get(int k) const {
@@ -19,14 +19,14 @@ template <> struct Chunk<bf16_t> {
   }
   __device__ __forceinline__ void set2(int k, float x, float y) { r[k >> 1] = pack_bf16(x, y); }
   // neighbours in exchanged places
-  __device__ __forceinline__ Chunk swapped() const {
-    Chunk c;
+  __device__ __forceinline__ RowChunk swapped() const {
+    RowChunk c;
 #pragma unroll
     for (int i = 0; i < 4; ++i) c.r[i] = (r[i] >> 16) | (r[i] << 16);
     return c;
   }
 };
-template <> struct Chunk<float> {
+template <> struct RowChunk<float> {
   static constexpr int W = 4;
   u32x4 r;
   __device__ __forceinline__ float get(int k) const {
@@ -37,8 +37,8 @@ template <> struct Chunk<float> {
     r[k] = __builtin_bit_cast(uint32_t, x);
     r[k + 1] = __builtin_bit_cast(uint32_t, y);
   }
-  __device__ __forceinline__ Chunk swapped() const {
-    Chunk c;
+  __device__ __forceinline__ RowChunk swapped() const {
+    RowChunk c;
     c.r = u32x4{r[1], r[0], r[3], r[2]};
     return c;
   }
@@ -85,7 +85,7 @@ bool whole_chunks(int dtype, int R, int adjacent) {
   return R % (adjacent ? w : 2 * w) == 0;
 }
 template <typename T, bool WHOLE> struct Turn : Place {
-  static constexpr int W = Chunk<T>::W;
+  static constexpr int W = RowChunk<T>::W;
   float co[W], si[W];
 
   __device__ __forceinline__ explicit Turn(const TurnShape &s) : Place(s, threadIdx.x) {}
@@ -102,9 +102,9 @@ template <typename T, bool WHOLE> struct Turn : Place {
     }
   }
   // The turned chunk.  All lanes of the wave have to come here; scratch: 1 KB of LDS of this wave's own (not WHOLE).
-  __device__ __forceinline__ Chunk<T> turned(const Rotary &ro, const Chunk<T> &x, u32x4 *scratch) const {
+  __device__ __forceinline__ RowChunk<T> turned(const Rotary &ro, const RowChunk<T> &x, u32x4 *scratch) const {
     const int half = ro.R / 2;
-    Chunk<T> p, y;
+    RowChunk<T> p, y;
     if (ro.adjacent) {
       p = x.swapped();
     } else if (WHOLE) {
@@ -174,7 +174,7 @@ __global__ __launch_bounds__(256) void rotate_kernel(RotateArgs args) {
   const int64_t at = (int64_t)n * s.st[2] + turn.c * turn.W;
   const auto offset = [&](int h) { return head_offset((uint32_t)h, args.by_Z, s.st) + at; };
   const int groups = 4 / sh.waves, h = (int)blockIdx.y * kAhead * groups + turn.group;
-  Chunk<T> x[kAhead] = {};
+  RowChunk<T> x[kAhead] = {};
 #pragma unroll
   for (int k = 0; k < kAhead; ++k)
     if (have && h + k * groups < args.heads) x[k].r = *reinterpret_cast<const u32x4 *>(static_cast<const T *>(s.x) + offset(h + k * groups));
@@ -189,7 +189,7 @@ __global__ __launch_bounds__(256) void rotate_kernel(RotateArgs args) {
   turn.take(args.ro, angles + (have ? turn.row * (int)sh.by_half.d : 0));
 #pragma unroll
   for (int k = 0; k < kAhead; ++k) {
-    const Chunk<T> y = turn.turned(args.ro, x[k], scratch + (WHOLE ? 0 : threadIdx.x & 192));
+    const RowChunk<T> y = turn.turned(args.ro, x[k], scratch + (WHOLE ? 0 : threadIdx.x & 192));
     if (have && h + k * groups < args.heads) {
       u32x4 *to = reinterpret_cast<u32x4 *>(static_cast<T *>(s.y) + offset(h + k * groups));
       if constexpr (PAST) __builtin_nontemporal_store(y.r, to);
