@@ -490,8 +490,8 @@ struct Attend {
       // The matrix core takes bf16: a probability goes to it as three, its first eight bits, the next eight and the rest, all 24 of
       // it (as two, 2^-16 of it is lost, which shows where values cancel.  Long walks from HBM take the same, whose matrix cores wait for
       // memory; one of 200 slots 5.2 and 5.3 us, 16 of 8192 from the infinity cache with 32 queries a key head 21.3 and 22.3).  No part is
-      // 0 where the probability is not (exp2 gives none below 2^-126): times an infinite value that were NaN.  The later ones are
-      // 2^-100 at least, or the first if that is less: below every sum's rounding.
+      // 0 where the probability is not (exp2 gives none below 2^-126): times an infinite value that were NaN.  The later ones are at
+      // least the smallest number that bf16 has, 2^-133, which the matrix cores take as it is: less than 2^-24 of a probability of 2^-108.
       bf16x8 pb[NQ][3];
 #pragma unroll
       for (int x = 0; x < NQ; ++x) {
@@ -503,8 +503,8 @@ struct Attend {
           for (int e = 0; e < 2; ++e) {
             const float y = p[x][k >> 1 ? KT - 1 : 0][2 * (k & 1) + e], r = y - first_bits(y);
             part[0][e] = y;
-            part[1][e] = __builtin_amdgcn_fmed3f(r, 0x1p-100f, y);
-            part[2][e] = __builtin_amdgcn_fmed3f(r - first_bits(r), 0x1p-100f, y);
+            part[1][e] = __builtin_amdgcn_fmed3f(r, 0x1p-133f, y);
+            part[2][e] = __builtin_amdgcn_fmed3f(r - first_bits(r), 0x1p-133f, y);
           }
 #pragma unroll
           for (int i = 0; i < 3; ++i)

@@ -88,3 +88,23 @@ def test_joined_weights_go_by_the_differences_alone(dtype, level):
     got = rsa.cache_join(rsa.make_cache_desc(pool, table, Z), Op.cuda(), LSEp.cuda())
     within(got[0], O, rel * size + STEP[dtype] * np.abs(O), "O")
     within(got[1], LSE, rel + 2.0 ** -22 + F32 * np.abs(LSE), "LSE")
+
+
+@pytest.mark.parametrize("width", [1, 1000])
+def test_a_large_value_under_a_small_probability(width):
+    """Values of 2^120 under probabilities p of 2^-125 to 2^-87 of the row's largest, where they decide.  A score is a single product; p is off by
+    4 roundings of its exponent and exp's 2^-22; its parts are multiples of 2^-133, one cut off and two that may be raised to it."""
+    B, Z, A = 64, 16, 64
+    rng = np.random.default_rng(35)
+    Q, K, V = torch.zeros(B, Z, 1, A).bfloat16(), torch.zeros(B, 1, 30, A).bfloat16(), torch.ones(B, 1, 30, A).bfloat16()
+    Q[..., 0, 0] = torch.from_numpy(rng.uniform(60, 87, (B, Z))).bfloat16()
+    K[:, 0, 1, 0], K[:, 0, 2:, 0] = -1.0, -30000.0
+    V[:, 0, 1, :8], V[:, 0, 1, 8:16] = 2.0 ** 120, -1.75 * 2.0 ** 120
+    V[:, 0, 2:, 16:] = 2.0 ** 127                               # (under probabilities of 0: no part of any result)
+    Kc, Vc, table, lengths = one_page(K, V, width)
+    got, _ = rsa.cache_attend(rsa.make_cache_desc(Kc, table, Z, scale=1.0), Q.cuda(), Kc, Vc, table, lengths)
+    p = torch.exp(-Q[..., 0].double())
+    O = 1.0 + p[..., None] * (V[:, :1, 1:2].double() - 1)
+    off = (4 * F32 * 87 + 2.0 ** -22) * p[..., None] + 3 * 2.0 ** -133
+    bound = off * V[:, :1, 1:2].double().abs() + 8 * F32
+    within(got, O.numpy(), bound.numpy() + STEP["bf16"] * O.abs().numpy(), "O")
