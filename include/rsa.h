@@ -340,7 +340,7 @@ typedef struct {
   float scale;        /* 0 selects 1/sqrt(A)                                   */
   uint32_t flags;     /* 0                                                     */
   /* Strides in elements of the batch, head and token index: q_stride for Q and Qr, kv_stride for
-   * the new K and V, o_stride for O.  All three zero = dense (B, heads, tokens, A).
+   * the new K and V and those read, o_stride for O.  All three zero = dense (B, heads, tokens, A).
    * Positive multiples of 16 bytes otherwise. */
   int64_t q_stride[3], kv_stride[3], o_stride[3];
 } rsa_cache_desc;
@@ -369,6 +369,44 @@ size_t rsa_cache_workspace_bytes(const rsa_cache_desc *d);
 int rsa_cache_attend(const rsa_cache_desc *d, const void *Q, const void *Kc, const void *Vc,
                      const int32_t *table, const int32_t *lengths, void *O, float *LSE, void *ws,
                      size_t ws_bytes, void *stream);
+
+/*
+ * The cache in 8 bits: pools of e4m3 numbers, Kc and Vc as above with one byte an element, and a power of two for each row (a token's
+ * head), Ks and Vs, (pages, Zkv, page) bytes: the row's elements stand for e4m3 * 2^(byte - 127), which bf16 holds exactly.  For calls in bf16.
+ *  rsa_cache_append8: rsa_cache_append to such pools.  Of a row of keys (after its rotation) or values, 2^e is the least power,
+ *    -64 <= e <= 120, with no finite element beyond 448 2^e; element x is stored as the e4m3 number nearest to x 2^-e (ties to even), rounded once
+ *    from the exact rotation.  Infinite and NaN elements are stored as NaN.
+ *  rsa_cache_attend8: rsa_cache_attend to such pools, of the same workspace; any bytes in Ks and Vs but 255.
+ */
+int rsa_cache_append8(const rsa_cache_desc *d, int32_t T, const void *Q, const void *K, const void *V,
+                      const int32_t *table, const int32_t *lengths, const int32_t *counts,
+                      const int32_t *first, int32_t R, int32_t adjacent, const float *inv_freq,
+                      void *Qr, void *Kc, void *Vc, uint8_t *Ks, uint8_t *Vs, void *stream);
+int rsa_cache_attend8(const rsa_cache_desc *d, const void *Q, const void *Kc, const void *Vc, const uint8_t *Ks,
+                      const uint8_t *Vs, const int32_t *table, const int32_t *lengths, void *O, float *LSE,
+                      void *ws, size_t ws_bytes, void *stream);
+
+/* The tokens of a cache as dense tensors: K, V (B, Zkv, T, A), strides kv_stride.  Of sequence b the last counts[b] slots (NULL, or
+ * above T: T; below 0: 0) are read, token t from slot lengths[b] - counts[b] + t; zeros where that is not held.  Rows of
+ * other tokens are left as they are.  Ks, Vs: of pools in e4m3, of which the results have the exact values, else both NULL. */
+int rsa_cache_read(const rsa_cache_desc *d, int32_t T, const void *Kc, const void *Vc, const uint8_t *Ks,
+                   const uint8_t *Vs, const int32_t *table, const int32_t *lengths, const int32_t *counts,
+                   void *K, void *V, void *stream);
+
+/* Attention of several new tokens of every sequence to the cache, to which they have been appended: a prompt, a piece of one, guesses to be checked.
+ * Q and O are (B, Z, T, A), LSE (B, Z, T) fp32.  Of sequence b the first counts[b] tokens (as in rsa_cache_append) are there; token t
+ * is that of slot lengths[b] - counts[b] + t and sees the slots that are held up to its own or, without `causal`, all that are held (a rank
+ * whose share of the cache lies in front of the tokens).  A row that sees no key gets O = 0 and LSE = -inf, rows of tokens that are not there
+ * are left as they are.  Pool memory outside the slots that a row sees does not reach its result, whatever it holds: not one of an infinite or
+ * NaN key or value either.  Ks, Vs as in rsa_cache_read.  fp32, and bf16 up to 32 rows of a key head (T Z/Zkv), as rsa_cache_attend; beyond that P is
+ * rounded to bf16 once, as in rsa_forward.  T * Z must be below 2^31, B * Z * T * A at most 2^34.  ws:
+ * rsa_cache_chunk_workspace_bytes(d, T) bytes, as for rsa_cache_attend.
+ * Results of shares are joined by rsa_cache_join with Z * T for Z: rows are rows. */
+size_t rsa_cache_chunk_workspace_bytes(const rsa_cache_desc *d, int32_t T);
+int rsa_cache_attend_chunk(const rsa_cache_desc *d, int32_t T, int32_t causal, const void *Q, const void *Kc,
+                           const void *Vc, const uint8_t *Ks, const uint8_t *Vs, const int32_t *table,
+                           const int32_t *lengths, const int32_t *counts, void *O, float *LSE, void *ws,
+                           size_t ws_bytes, void *stream);
 
 /* Joins the results of N shares of a cache (each of N ranks holds some of the tokens and attends
  * to those): Op (N, B, Z, 1, A) and LSEp (N, B, Z, 1), dense, as rsa_cache_attend wrote

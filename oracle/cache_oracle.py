@@ -98,3 +98,81 @@ def join(Op, LSEp):
         LSE = np.log(total) + ref
     part = np.where(w[..., None] > 0, Op, 0.0) * w[..., None]
     return part.sum(0) / np.where(total > 0, total, 1.0)[..., None], LSE
+
+
+# ---- the cache in 8 bits ----
+# What the 127 bytes from 0 up to the largest number of e4m3 stand for, in ascending order: four bits of an exponent, three of a fraction.
+E4M3 = np.array([(b & 7) * 2.0 ** -9 if b < 8 else (8 + (b & 7)) * 2.0 ** ((b >> 3) - 10) for b in range(127)])
+
+
+def from_e4m3(byte):
+    byte = np.asarray(byte, np.int64)
+    v = np.append(E4M3, np.nan)[byte & 127]
+    return np.where(byte & 128, -v, v)
+
+
+def to_e4m3(x):
+    """Rows (..., A) -> bytes, and the rows' exponents + 127: the least power of two, from 2^-64 on, under which no finite element
+    passes 448, and the nearest number, of two the one with an even byte."""
+    x = np.asarray(x, np.float64)
+    top = np.where(np.isfinite(x), np.abs(x), 0.0).max(-1)
+    e = np.full(top.shape, -64)
+    while (top > 448.0 * 2.0 ** e).any():
+        e += top > 448.0 * 2.0 ** e
+    y = np.abs(x) / 2.0 ** e[..., None]
+    hi = np.clip(np.searchsorted(E4M3, np.nan_to_num(y)), 1, 126)
+    below, above = y - E4M3[hi - 1], E4M3[hi] - y
+    byte = np.where((above < below) | ((above == below) & (hi % 2 == 0)), hi, hi - 1)
+    byte = np.where(np.isfinite(x), byte, 127)
+    return np.where(np.signbit(x) & np.isfinite(x), byte + 128, byte), e + 127
+
+
+def append8(K, V, Kc, Vc, Ks, Vs, table, lengths, counts=None, first=None, inv_freq=None, adjacent=False, Q=None, Qr=None):
+    """... to pools of bytes with exponents.  Returns (Qr, Kc, Vc, Ks, Vs)."""
+    Kc, Vc, Ks, Vs = (np.array(x, np.int64) for x in (Kc, Vc, Ks, Vs))
+    pages, _, page, _ = Kc.shape
+    T = K.shape[2]
+    mark = np.full(Kc.shape, np.nan)
+    Qr, turned, moved = append(K, V, mark, mark, table, lengths, counts, first, inv_freq, adjacent, Q, Qr)
+    for b in range(len(lengths)):
+        count = T if counts is None else min(T, int(counts[b]))
+        for slot in range(int(lengths[b]) - count, int(lengths[b])):
+            at = place(table, b, slot, pages, page)
+            if at is not None:
+                Kc[at[0], :, at[1]], Ks[at[0], :, at[1]] = to_e4m3(turned[at[0], :, at[1]])
+                Vc[at[0], :, at[1]], Vs[at[0], :, at[1]] = to_e4m3(moved[at[0], :, at[1]])
+    return Qr, Kc, Vc, Ks, Vs
+
+
+def read(pool, table, lengths, T, counts=None, start=None):
+    """The last tokens of every sequence, (B, Zkv, T, A); rows of no token from the given ones (zero)."""
+    pages, Zkv, page, A = pool.shape
+    out = np.zeros((len(lengths), Zkv, T, A)) if start is None else np.array(start, np.float64)
+    for b in range(len(lengths)):
+        count = T if counts is None else min(T, int(counts[b]))
+        for t in range(count):
+            at = place(table, b, int(lengths[b]) - count + t, pages, page)
+            out[b, :, t] = 0.0 if at is None else pool[at[0], :, at[1]]
+    return out
+
+
+# ---- several new tokens at a time ----
+def seen_by(table, lengths, T, counts, causal, page):
+    """Slots that token t of sequence b sees (from 0 on, those that are not held among them), -1 for a token that is not there."""
+    n = np.full((len(lengths), T), -1)
+    for b in range(len(lengths)):
+        count = T if counts is None else max(0, min(T, int(counts[b])))
+        most = max(0, min(int(lengths[b]), table.shape[1] * page))
+        for t in range(count):
+            n[b, t] = most if not causal else max(0, min(int(lengths[b]) - count + t + 1, most))
+    return n
+
+
+def attend_chunk(Q, Kc, Vc, table, lengths, counts=None, causal=True, scale=None):
+    """Q (B, Z, T, A) -> O, LSE (B, Z, T), token by token; 0 and -inf for tokens that are not there."""
+    Q = np.asarray(Q, np.float64)
+    O, LSE = np.zeros(Q.shape), np.full(Q.shape[:3], -np.inf)
+    n = seen_by(table, lengths, Q.shape[2], counts, causal, Kc.shape[2])
+    for t in range(Q.shape[2]):
+        O[:, :, t:t + 1], LSE[:, :, t:t + 1] = attend(Q[:, :, t:t + 1], Kc, Vc, table, n[:, t], scale)
+    return O, LSE

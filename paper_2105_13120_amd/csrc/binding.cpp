@@ -9,12 +9,15 @@
 
 #include <ATen/ops/empty.h>
 #include <ATen/ops/empty_like.h>
+#include <ATen/ops/full.h>
+#include <ATen/ops/zeros.h>
 #include <ATen/ops/zeros_like.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <array>
+#include <cmath>
 
 #include "rsa.h"
 
@@ -345,21 +348,42 @@ const int32_t *int32s(const Call &c, int i, at::IntArrayRef shape) {
   check(i, c.tensor(i), at::kInt, shape);
   return static_cast<const int32_t *>(ptr(c.tensor(i)));
 }
-void check_pools(const Call &c, int i) {
+// Pools at i and i + 1 and, where they are in e4m3, their rows' exponents at k and k + 1
+bool check_pools(const Call &c, int i, int k) {
   const rsa_cache_desc &d = *c.cd;
-  for (int k = i; k < i + 2; ++k) check(k, c.tensor(k), type_of(d.dtype), {d.pages, d.Zkv, d.page, d.A});
+  const bool eight = c.tensor(i).scalar_type() == at::kFloat8_e4m3fn;
+  for (int n = 0; n < 2; ++n) {
+    check(i + n, c.tensor(i + n), eight ? at::kFloat8_e4m3fn : type_of(d.dtype), {d.pages, d.Zkv, d.page, d.A});
+    if (c.given(k + n) != eight) refuse(k + n, eight ? "exponents of a pool in e4m3 expected" : "exponents belong to pools in e4m3");
+    if (eight) check(k + n, c.tensor(k + n), at::kByte, {d.pages, d.Zkv, d.page});
+  }
+  return eight;
+}
+uint8_t *exponents(const Call &c, int i) { return c.given(i) ? static_cast<uint8_t *>(ptr(c.tensor(i))) : nullptr; }
+void check_places(const Call &c, int i, const int32_t *&table, const int32_t *&lengths) {
+  if (!c.given(i) || !c.given(i + 1)) refuse(c.given(i) ? i + 1 : i, "a tensor expected");
+  table = int32s(c, i, {c.cd->B, c.cd->width});
+  lengths = int32s(c, i + 1, {c.cd->B});
+}
+at::Tensor cache_workspace(const Call &c, int i, size_t need, const at::Tensor &like, size_t &n) {
+  n = need;
+  if (!c.given(i)) return need ? bytes(need, like) : at::Tensor();
+  if (!c.tensor(i).is_contiguous()) refuse(i, "a workspace without gaps expected");
+  n = c.tensor(i).nbytes();
+  return c.tensor(i);
 }
 
-// desc, K, V, Kc, Vc, table, lengths, counts, first, inv_freq, adjacent, Q, Qr
+// desc, K, V, Kc, Vc, table, lengths, counts, first, inv_freq, adjacent, Q, Qr, Ks, Vs
 PyObject *cache_append(Call &c) {
   const rsa_cache_desc &d = *c.cd;
   const at::Tensor &K = c.tensor(1), &V = c.tensor(2), &Kc = c.tensor(3), &Vc = c.tensor(4);
   if (K.dim() != 4 || K.size(2) < 1 || K.size(2) > INT32_MAX) refuse(1, "(B, Zkv, T, A) expected");
   const int64_t T = K.size(2);
   for (int i = 1; i < 3; ++i) check(i, c.tensor(i), type_of(d.dtype), {d.B, d.Zkv, T, d.A}, d.kv_stride);
-  check_pools(c, 3);
-  if (!c.given(5) || !c.given(6)) refuse(c.given(5) ? 6 : 5, "a tensor expected");
-  const int32_t *table = int32s(c, 5, {d.B, d.width}), *lengths = int32s(c, 6, {d.B}), *counts = int32s(c, 7, {d.B});
+  const bool eight = check_pools(c, 3, 13);
+  const int32_t *table, *lengths;
+  check_places(c, 5, table, lengths);
+  const int32_t *counts = int32s(c, 7, {d.B});
   const int32_t *first = int32s(c, 8, {d.B}), R = c.given(9) ? check_frequencies(c, 9) : 0, adjacent = truth(c, 10);
   const float *freq = c.given(9) ? static_cast<const float *>(ptr(c.tensor(9))) : nullptr;
   at::Tensor Q, Qr;
@@ -371,8 +395,11 @@ PyObject *cache_append(Call &c) {
   } else if (c.given(12)) {
     refuse(12, "a result without its input");
   }
-  check_device(c, 13);
+  check_device(c, 15);
   const auto call = [&](void *st) {
+    if (eight)
+      return rsa_cache_append8(&d, (int32_t)T, ptr(Q), ptr(K), ptr(V), table, lengths, counts, first, R, adjacent, freq, ptr(Qr), ptr(Kc),
+                               ptr(Vc), exponents(c, 13), exponents(c, 14), st);
     return rsa_cache_append(&d, (int32_t)T, ptr(Q), ptr(K), ptr(V), table, lengths, counts, first, R, adjacent, freq, ptr(Qr), ptr(Kc),
                             ptr(Vc), st); };
   if (Q.defined()) return finish(call, {Qr});
@@ -382,32 +409,84 @@ PyObject *cache_append(Call &c) {
   Py_RETURN_NONE;
 }
 
-// desc, Q, Kc, Vc, table, lengths, O, LSE, ws
+// desc, T, Kc, Vc, table, lengths, counts, K, V, Ks, Vs
+PyObject *cache_read(Call &c) {
+  const rsa_cache_desc &d = *c.cd;
+  const long long T = PyLong_AsLongLong(c.args[1]);
+  if (T == -1 && PyErr_Occurred()) throw Refused{};
+  if (T < 1 || T > INT32_MAX) refuse(1, "a number of tokens expected");
+  check_pools(c, 2, 9);
+  const int32_t *table, *lengths;
+  check_places(c, 4, table, lengths);
+  const int32_t *counts = int32s(c, 6, {d.B});
+  const std::array<int64_t, 4> shape{d.B, d.Zkv, T, d.A};
+  at::Tensor out[2];
+  for (int i = 0; i < 2; ++i) {
+    if (!c.given(7 + i)) {
+      for (int k = 0; k < 3; ++k)
+        if (d.kv_stride[k] != 0) refuse(7 + i, "a result with strides has to be given");
+      const auto o = c.tensor(2).options().dtype(type_of(d.dtype));
+      out[i] = counts ? at::zeros(shape, o) : at::empty(shape, o);
+    } else {
+      out[i] = c.tensor(7 + i);
+    }
+    check(7 + i, out[i], type_of(d.dtype), shape, d.kv_stride);
+  }
+  check_device(c, 11);
+  return finish([&](void *st) {
+    return rsa_cache_read(&d, (int32_t)T, ptr(c.tensor(2)), ptr(c.tensor(3)), exponents(c, 9), exponents(c, 10), table, lengths, counts,
+                          ptr(out[0]), ptr(out[1]), st); }, {out[0], out[1]});
+}
+
+// desc, Q, Kc, Vc, table, lengths, O, LSE, ws, Ks, Vs
 PyObject *cache_attend(Call &c) {
   const rsa_cache_desc &d = *c.cd;
   const at::Tensor &Q = c.tensor(1), &Kc = c.tensor(2), &Vc = c.tensor(3);
   const std::array<int64_t, 4> shape{d.B, d.Z, 1, d.A};
   check(1, Q, type_of(d.dtype), shape, d.q_stride);
-  check_pools(c, 2);
-  if (!c.given(4) || !c.given(5)) refuse(c.given(4) ? 5 : 4, "a tensor expected");
-  const int32_t *table = int32s(c, 4, {d.B, d.width}), *lengths = int32s(c, 5, {d.B});
+  const bool eight = check_pools(c, 2, 9);
+  const int32_t *table, *lengths;
+  check_places(c, 4, table, lengths);
   const at::Tensor O = c.tensor_or(6, [&] { return at::empty(shape, Q.options()); });
   check(6, O, type_of(d.dtype), shape, d.o_stride);
   const at::Tensor LSE = c.tensor_or(7, [&] { return at::empty({d.B, d.Z, 1}, Q.options().dtype(at::kFloat)); });
   check(7, LSE, at::kFloat, {d.B, d.Z, 1});
-  check_device(c, 9);
+  check_device(c, 11);
   size_t n = 0;
-  at::Tensor ws;
-  if (c.given(8)) {
-    ws = c.tensor(8);
-    if (!ws.is_contiguous()) refuse(8, "a workspace without gaps expected");
-    n = ws.nbytes();
-  } else if ((n = rsa_cache_workspace_bytes(&d)) > 0) {
-    ws = bytes(n, Q);
-  }
+  const at::Tensor ws = cache_workspace(c, 8, c.given(8) ? 0 : rsa_cache_workspace_bytes(&d), Q, n);
   return finish([&](void *st) {
-    return rsa_cache_attend(&d, ptr(Q), ptr(Kc), ptr(Vc), table, lengths, ptr(O), static_cast<float *>(ptr(LSE)), ptr(ws), n, st); },
-    {O, LSE});
+    float *l = static_cast<float *>(ptr(LSE));
+    if (eight)
+      return rsa_cache_attend8(&d, ptr(Q), ptr(Kc), ptr(Vc), exponents(c, 9), exponents(c, 10), table, lengths, ptr(O), l, ptr(ws), n, st);
+    return rsa_cache_attend(&d, ptr(Q), ptr(Kc), ptr(Vc), table, lengths, ptr(O), l, ptr(ws), n, st); }, {O, LSE});
+}
+
+// desc, Q, Kc, Vc, table, lengths, counts, causal, O, LSE, ws, Ks, Vs
+PyObject *cache_attend_chunk(Call &c) {
+  const rsa_cache_desc &d = *c.cd;
+  const at::Tensor &Q = c.tensor(1), &Kc = c.tensor(2), &Vc = c.tensor(3);
+  if (Q.dim() != 4 || Q.size(2) < 1 || Q.size(2) > INT32_MAX) refuse(1, "(B, Z, T, A) expected");
+  const int32_t T = (int32_t)Q.size(2);
+  const std::array<int64_t, 4> shape{d.B, d.Z, T, d.A};
+  check(1, Q, type_of(d.dtype), shape, d.q_stride);
+  check_pools(c, 2, 11);
+  const int32_t *table, *lengths;
+  check_places(c, 4, table, lengths);
+  const int32_t *counts = int32s(c, 6, {d.B}), causal = truth(c, 7);
+  // (rows of tokens that are not there stay as they are)
+  const at::Tensor O = c.tensor_or(8, [&] { return counts ? at::zeros(shape, Q.options()) : at::empty(shape, Q.options()); });
+  check(8, O, type_of(d.dtype), shape, d.o_stride);
+  const at::Tensor LSE = c.tensor_or(9, [&] {
+    const auto o = Q.options().dtype(at::kFloat);
+    return counts ? at::full({d.B, d.Z, T}, -INFINITY, o) : at::empty({d.B, d.Z, T}, o);
+  });
+  check(9, LSE, at::kFloat, {d.B, d.Z, T});
+  check_device(c, 13);
+  size_t n = 0;
+  const at::Tensor ws = cache_workspace(c, 10, c.given(10) ? 0 : rsa_cache_chunk_workspace_bytes(&d, T), Q, n);
+  return finish([&](void *st) {
+    return rsa_cache_attend_chunk(&d, T, causal, ptr(Q), ptr(Kc), ptr(Vc), exponents(c, 11), exponents(c, 12), table, lengths, counts, ptr(O),
+                                  static_cast<float *>(ptr(LSE)), ptr(ws), n, st); }, {O, LSE});
 }
 
 // desc, Op, LSEp, O, LSE
@@ -442,8 +521,9 @@ PyMODINIT_FUNC PyInit__binding(void) {
       method<out_proj, 4>("out_proj"), method<out_proj_bwd, 7>("out_proj_bwd"), method<qkv_proj_bwd, 9>("qkv_proj_bwd"),
       method<linformer_project, 5>("linformer_project"), method<linformer_forward, 6>("linformer_forward"),
       method<linformer_backward, 11>("linformer_backward"), method<linformer_project_bwd, 6>("linformer_project_bwd"),
-      method<rotate, 8>("rotate"), method<cache_append, 13, true>("cache_append"),
-      method<cache_attend, 9, true>("cache_attend"), method<cache_join, 5, true>("cache_join"),
+      method<rotate, 8>("rotate"), method<cache_append, 15, true>("cache_append"), method<cache_read, 11, true>("cache_read"),
+      method<cache_attend, 11, true>("cache_attend"), method<cache_attend_chunk, 13, true>("cache_attend_chunk"),
+      method<cache_join, 5, true>("cache_join"),
       {nullptr, nullptr, 0, nullptr}};
   static PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, table, nullptr, nullptr, nullptr, nullptr};
   return PyModule_Create(&module);

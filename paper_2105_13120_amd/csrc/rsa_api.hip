@@ -115,6 +115,9 @@ Piece rows_of(const rsa::CacheDims &d, const void *p, const int64_t *st, int64_t
 Piece pool_of(const rsa::CacheDims &d, const void *p) {
   return {p, (size_t)d.pages * d.Zkv * d.page * d.A * (d.dtype == RSA_BF16 ? 2 : 4)};
 }
+// ... in e4m3, and the exponents of its rows
+Piece pool8_of(const rsa::CacheDims &d, const void *p) { return {p, (size_t)d.pages * d.Zkv * d.page * d.A}; }
+Piece scales_of(const rsa::CacheDims &d, const void *p) { return {p, (size_t)d.pages * d.Zkv * d.page}; }
 Piece words_of(const void *p, int64_t n) { return {p, (size_t)n * 4}; }
 // whether a result lies over another tensor of the call (elsewhere kernels would read what they or others have written)
 bool lies_over(const Piece &out, std::initializer_list<Piece> others) {
@@ -127,7 +130,7 @@ bool lies_over(const Piece &out, std::initializer_list<Piece> others) {
 
 extern "C" {
 
-int rsa_version(void) { return 120; }
+int rsa_version(void) { return 130; }
 
 const char *rsa_strerror(int status) {
   switch (status) {
@@ -536,7 +539,7 @@ int cache_validate(const rsa_cache_desc *d, int32_t tokens, rsa::CacheDims *out)
   int64_t *st[3] = {out->qs, out->ks, out->os};
   const int unit = d->dtype == RSA_BF16 ? 8 : 4;
   for (int t = 0; t < 3; ++t) {
-    const int64_t heads = t == 1 ? d->Zkv : d->Z, rows = t == 2 ? 1 : tokens, dense[3] = {heads * rows * d->A, rows * d->A, d->A};
+    const int64_t heads = t == 1 ? d->Zkv : d->Z, dense[3] = {heads * tokens * d->A, (int64_t)tokens * d->A, d->A};
     const bool zero = in[t][0] == 0 && in[t][1] == 0 && in[t][2] == 0;
     for (int k = 0; k < 3; ++k) {
       st[t][k] = zero ? dense[k] : in[t][k];
@@ -565,22 +568,58 @@ bool words(std::initializer_list<const void *> ps) {  // whether all are aligned
 }
 }  // namespace
 
-int rsa_cache_append(const rsa_cache_desc *d, int32_t T, const void *Q, const void *K, const void *V, const int32_t *table,
-                     const int32_t *lengths, const int32_t *counts, const int32_t *first, int32_t R, int32_t adjacent,
-                     const float *inv_freq, void *Qr, void *Kc, void *Vc, void *stream) {
-  RSA_CACHE_PROLOGUE(T, K && V && table && lengths && Kc && Vc && !Q == !Qr, Q, K, V, Qr, Kc, Vc);
+namespace {
+// eight: pools in e4m3, with Ks and Vs
+int append_to(const rsa_cache_desc *d, int32_t T, const void *Q, const void *K, const void *V, const int32_t *table,
+              const int32_t *lengths, const int32_t *counts, const int32_t *first, int32_t R, int32_t adjacent,
+              const float *inv_freq, void *Qr, void *Kc, void *Vc, uint8_t *Ks, uint8_t *Vs, bool eight, void *stream) {
+  RSA_CACHE_PROLOGUE(T, K && V && table && lengths && Kc && Vc && !Q == !Qr && (!eight || (Ks && Vs)), Q, K, V, Qr, Kc, Vc);
+  if (eight && d->dtype != RSA_BF16) return RSA_ERR_UNSUPPORTED;
   if (!words({table, lengths, counts, first, inv_freq})) return RSA_ERR_UNSUPPORTED;
   if (!inv_freq) R = 0;
   if (inv_freq && (R < 2 || R > dm.A)) return RSA_ERR_SHAPE;
   if (R % 2 != 0) return RSA_ERR_UNSUPPORTED;
   const Piece k = rows_of(dm, K, dm.ks, dm.Zkv, T), v = rows_of(dm, V, dm.ks, dm.Zkv, T), q = rows_of(dm, Q, dm.qs, dm.Z, T);
-  const Piece qr = rows_of(dm, Qr, dm.qs, dm.Z, T), keys = pool_of(dm, Kc), values = pool_of(dm, Vc);
+  const Piece qr = rows_of(dm, Qr, dm.qs, dm.Z, T), keys = eight ? pool8_of(dm, Kc) : pool_of(dm, Kc);
+  const Piece values = eight ? pool8_of(dm, Vc) : pool_of(dm, Vc), ke = scales_of(dm, Ks), ve = scales_of(dm, Vs);
   const Piece t = words_of(table, (int64_t)dm.B * dm.width), n = words_of(lengths, dm.B), c = words_of(counts, dm.B);
   const Piece f = words_of(first, dm.B), w = words_of(inv_freq, R / 2);
   if (lies_over(keys, {values, k, v, q, qr, t, n, c, f, w}) || lies_over(values, {k, v, q, qr, t, n, c, f, w}) ||
       lies_over(qr, {k, v, t, n, c, f, w}) || (Qr != Q && lies_over(qr, {q})))
     return RSA_ERR_UNSUPPORTED;
+  if (lies_over(ke, {ve, keys, values, k, v, q, qr, t, n, c, f, w}) || lies_over(ve, {keys, values, k, v, q, qr, t, n, c, f, w}))
+    return RSA_ERR_UNSUPPORTED;
+  if (eight)
+    return hip_status(rsa::cache_append8(dm, {Kc, Vc, Ks, Vs}, T, R, adjacent != 0, inv_freq, Q, K, V, table, lengths, counts, first, Qr, st));
   return hip_status(rsa::cache_append(dm, T, R, adjacent != 0, inv_freq, Q, K, V, table, lengths, counts, first, Qr, Kc, Vc, st));
+}
+
+}  // namespace
+
+int rsa_cache_append(const rsa_cache_desc *d, int32_t T, const void *Q, const void *K, const void *V, const int32_t *table,
+                     const int32_t *lengths, const int32_t *counts, const int32_t *first, int32_t R, int32_t adjacent,
+                     const float *inv_freq, void *Qr, void *Kc, void *Vc, void *stream) {
+  return append_to(d, T, Q, K, V, table, lengths, counts, first, R, adjacent, inv_freq, Qr, Kc, Vc, nullptr, nullptr, false, stream);
+}
+
+int rsa_cache_append8(const rsa_cache_desc *d, int32_t T, const void *Q, const void *K, const void *V, const int32_t *table,
+                      const int32_t *lengths, const int32_t *counts, const int32_t *first, int32_t R, int32_t adjacent,
+                      const float *inv_freq, void *Qr, void *Kc, void *Vc, uint8_t *Ks, uint8_t *Vs, void *stream) {
+  return append_to(d, T, Q, K, V, table, lengths, counts, first, R, adjacent, inv_freq, Qr, Kc, Vc, Ks, Vs, true, stream);
+}
+
+int rsa_cache_read(const rsa_cache_desc *d, int32_t T, const void *Kc, const void *Vc, const uint8_t *Ks, const uint8_t *Vs,
+                   const int32_t *table, const int32_t *lengths, const int32_t *counts, void *K, void *V, void *stream) {
+  RSA_CACHE_PROLOGUE(T, Kc && Vc && table && lengths && K && V && !Ks == !Vs, Kc, Vc, K, V);
+  if (!words({table, lengths, counts}) || (Ks && d->dtype != RSA_BF16)) return RSA_ERR_UNSUPPORTED;
+  const Piece keys = Ks ? pool8_of(dm, Kc) : pool_of(dm, Kc), values = Ks ? pool8_of(dm, Vc) : pool_of(dm, Vc);
+  const Piece ke = scales_of(dm, Ks), ve = scales_of(dm, Vs), k = rows_of(dm, K, dm.ks, dm.Zkv, T), v = rows_of(dm, V, dm.ks, dm.Zkv, T);
+  const Piece t = words_of(table, (int64_t)dm.B * dm.width), n = words_of(lengths, dm.B), c = words_of(counts, dm.B);
+  if (K == V || lies_over(k, {v, keys, values, ke, ve, t, n, c}) || lies_over(v, {keys, values, ke, ve, t, n, c}))
+    return RSA_ERR_UNSUPPORTED;
+  // (the kernel writes nothing to the pools)
+  const rsa::CachePools pools = {const_cast<void *>(Kc), const_cast<void *>(Vc), const_cast<uint8_t *>(Ks), const_cast<uint8_t *>(Vs)};
+  return hip_status(rsa::cache_read(dm, pools, T, table, lengths, counts, K, V, st));
 }
 
 size_t rsa_cache_workspace_bytes(const rsa_cache_desc *d) {
@@ -588,18 +627,56 @@ size_t rsa_cache_workspace_bytes(const rsa_cache_desc *d) {
   return cache_validate(d, 1, &dm) == RSA_OK ? rsa::cache_workspace_bytes(dm) : 0;
 }
 
+namespace {
+// What the row numbers of a chunk's kernels hold
+bool chunk_fits(const rsa::CacheDims &d, int64_t T) {
+  return T * d.Z < (1LL << 31) && (int64_t)d.B * d.Z <= (1LL << 34) / d.A / T;
+}
+// T tokens per sequence (chunk), or the one of rsa_cache_attend
+int attend_to(const rsa_cache_desc *d, bool chunk, int32_t T, int32_t causal, const void *Q, const void *Kc, const void *Vc, const uint8_t *Ks,
+              const uint8_t *Vs, const int32_t *table, const int32_t *lengths, const int32_t *counts, void *O, float *LSE, void *ws,
+              size_t ws_bytes, void *stream) {
+  RSA_CACHE_PROLOGUE(T, Q && Kc && Vc && table && lengths && O && LSE && !Ks == !Vs, Q, Kc, Vc, O, ws);
+  if (!words({table, lengths, counts, LSE}) || (Ks && d->dtype != RSA_BF16) || (chunk && !chunk_fits(dm, T))) return RSA_ERR_UNSUPPORTED;
+  const size_t need = chunk ? rsa::chunk_workspace_bytes(dm, T) : rsa::cache_workspace_bytes(dm);
+  if (need > 0 && (!ws || ws_bytes < need)) return RSA_ERR_WORKSPACE;
+  const Piece q = rows_of(dm, Q, dm.qs, dm.Z, T), keys = Ks ? pool8_of(dm, Kc) : pool_of(dm, Kc), values = Ks ? pool8_of(dm, Vc) : pool_of(dm, Vc);
+  const Piece ke = scales_of(dm, Ks), ve = scales_of(dm, Vs);
+  const Piece t = words_of(table, (int64_t)dm.B * dm.width), n = words_of(lengths, dm.B), c = words_of(counts, dm.B);
+  const Piece o = rows_of(dm, O, dm.os, dm.Z, T), l = words_of(LSE, (int64_t)dm.B * dm.Z * T), w(ws, need);
+  if (lies_over(o, {q, keys, values, ke, ve, t, n, c, l, w}) || lies_over(l, {q, keys, values, ke, ve, t, n, c, w}) ||
+      lies_over(w, {q, keys, values, ke, ve, t, n, c}))
+    return RSA_ERR_UNSUPPORTED;
+  // (the kernels write nothing to the pools)
+  const rsa::CachePools pools = {const_cast<void *>(Kc), const_cast<void *>(Vc), const_cast<uint8_t *>(Ks), const_cast<uint8_t *>(Vs)};
+  return hip_status(chunk ? rsa::cache_attend_chunk(dm, pools, T, causal != 0, Q, table, lengths, counts, O, LSE, ws, st)
+                          : rsa::cache_attend(dm, pools, Q, table, lengths, O, LSE, ws, st));
+}
+}  // namespace
+
 int rsa_cache_attend(const rsa_cache_desc *d, const void *Q, const void *Kc, const void *Vc, const int32_t *table,
                      const int32_t *lengths, void *O, float *LSE, void *ws, size_t ws_bytes, void *stream) {
-  RSA_CACHE_PROLOGUE(1, Q && Kc && Vc && table && lengths && O && LSE, Q, Kc, Vc, O, ws);
-  if (!words({table, lengths, LSE})) return RSA_ERR_UNSUPPORTED;
-  const size_t need = rsa::cache_workspace_bytes(dm);
-  if (need > 0 && (!ws || ws_bytes < need)) return RSA_ERR_WORKSPACE;
-  const Piece q = rows_of(dm, Q, dm.qs, dm.Z, 1), keys = pool_of(dm, Kc), values = pool_of(dm, Vc);
-  const Piece t = words_of(table, (int64_t)dm.B * dm.width), n = words_of(lengths, dm.B);
-  const Piece o = rows_of(dm, O, dm.os, dm.Z, 1), l = words_of(LSE, (int64_t)dm.B * dm.Z), w(ws, need);
-  if (lies_over(o, {q, keys, values, t, n, l, w}) || lies_over(l, {q, keys, values, t, n, w}) || lies_over(w, {q, keys, values, t, n}))
-    return RSA_ERR_UNSUPPORTED;
-  return hip_status(rsa::cache_attend(dm, Q, Kc, Vc, table, lengths, O, LSE, ws, st));
+  return attend_to(d, false, 1, 1, Q, Kc, Vc, nullptr, nullptr, table, lengths, nullptr, O, LSE, ws, ws_bytes, stream);
+}
+
+int rsa_cache_attend8(const rsa_cache_desc *d, const void *Q, const void *Kc, const void *Vc, const uint8_t *Ks, const uint8_t *Vs,
+                      const int32_t *table, const int32_t *lengths, void *O, float *LSE, void *ws, size_t ws_bytes, void *stream) {
+  rsa::CacheDims dm;
+  const int rc = cache_validate(d, 1, &dm);
+  if (rc != RSA_OK) return rc;
+  if (!Ks || !Vs) return RSA_ERR_NULL;
+  return attend_to(d, false, 1, 1, Q, Kc, Vc, Ks, Vs, table, lengths, nullptr, O, LSE, ws, ws_bytes, stream);
+}
+
+size_t rsa_cache_chunk_workspace_bytes(const rsa_cache_desc *d, int32_t T) {
+  rsa::CacheDims dm;
+  return cache_validate(d, T, &dm) == RSA_OK && chunk_fits(dm, T) ? rsa::chunk_workspace_bytes(dm, T) : 0;
+}
+
+int rsa_cache_attend_chunk(const rsa_cache_desc *d, int32_t T, int32_t causal, const void *Q, const void *Kc, const void *Vc,
+                           const uint8_t *Ks, const uint8_t *Vs, const int32_t *table, const int32_t *lengths, const int32_t *counts,
+                           void *O, float *LSE, void *ws, size_t ws_bytes, void *stream) {
+  return attend_to(d, true, T, causal, Q, Kc, Vc, Ks, Vs, table, lengths, counts, O, LSE, ws, ws_bytes, stream);
 }
 
 int rsa_cache_join(const rsa_cache_desc *d, int32_t N, const void *Op, const float *LSEp, void *O, float *LSE, void *stream) {

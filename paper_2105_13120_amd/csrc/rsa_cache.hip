@@ -1,49 +1,11 @@
 // The paged cache of keys and values: appending to it, attention of one new token per sequence to it, and the join of
 // results over shares of it (rsa_cache_append, rsa_cache_attend, rsa_cache_join).
+#include "rsa_cache_tokens.h"
 #include "rsa_kernels.h"
 #include "rsa_rotary.h"
 
 namespace rsa {
 namespace {
-
-constexpr int kCUs = 256;
-
-// Uneven sequences, each of some items of work (none for b outside [0, B)), as every wave counts them for itself: lane l has
-// sequences [l per, (l + 1) per), per <= 64.
-struct Count {
-  uint32_t mine, upto;  // items of this lane's sequences; of theirs and all before
-  __device__ __forceinline__ static uint32_t scan(uint32_t x) {
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const uint32_t y = __shfl_up(x, o);
-      if ((int)(threadIdx.x & 63) >= o) x += y;
-    }
-    return x;
-  }
-  template <class F> __device__ __forceinline__ Count(int B, int per, F items) : mine(0) {
-    const int b0 = (int)(threadIdx.x & 63) * per, b1 = b0 + per < B ? b0 + per : B;
-    if (per == 1) mine = b0 < b1 ? items(b0) : 0u;
-    else for (int b = b0; b < b1; b += 8) {  // (eight loads on their way at a time)
-      uint32_t n[8];
-#pragma unroll
-      for (int k = 0; k < 8; ++k) n[k] = items(b + k < b1 ? b + k : b);
-#pragma unroll
-      for (int k = 0; k < 8; ++k) mine += b + k < b1 ? n[k] : 0u;
-    }
-    upto = scan(mine);
-  }
-  __device__ __forceinline__ uint32_t all() const { return __builtin_amdgcn_readlane(upto, 63); }
-  // The sequence of item x < all(), and the items before it
-  template <class F> __device__ __forceinline__ int find(uint32_t x, int B, int per, F items, uint32_t &before) const {
-    const int l = __builtin_ctzll(__ballot(x < upto)), lane = (int)(threadIdx.x & 63), b = l * per + lane;
-    before = __builtin_amdgcn_readlane(upto - mine, l);
-    if (per == 1) return l;
-    const uint32_t n = lane < per && b < B ? items(b) : 0u, s = scan(n);
-    const int k = __builtin_ctzll(__ballot(x < before + s));
-    before += __builtin_amdgcn_readlane(s - n, k);
-    return l * per + k;
-  }
-};
 
 // ---------------------------------------------------------------- append ----
 // W consecutive elements in fp32.
@@ -295,14 +257,23 @@ void launch_append(const AppendArgs &a, int W, uint32_t grid, hipStream_t st) {
 //                 byte permutes, half an instruction an element.
 // Every accumulator of a lane belongs to its query l % 16: the rescaling by the running maximum is a product by one number.
 // Query heads of one key head are the 16 (or 32) columns; a lone one pays for the unused ones nothing that counts.
+//
+// KIND kChunk: T new tokens per sequence, those that are there (counts) at its last slots.  The columns are then the rows of a key head,
+// token by token, the group's heads of a token side by side; each has a limit of its own, the first slot that it does not see.
+// KIND kEight: pools in e4m3, a power of two per row (Ks, Vs: its exponent + 127).  What a row stands for is exact in bf16 and formed by one
+// instruction per two elements, the power among it: the products are those of a bf16 cache, of half the bytes.
+enum AttendKind { kPlain = 0, kEight = 1, kChunk = 2 };
+
 struct AttendArgs {
   const void *Q, *Kc, *Vc;
-  const int32_t *table, *lengths;
+  const uint8_t *Ks, *Vs;
+  const int32_t *table, *lengths, *counts;
   void *O;
   float *LSE;
   int64_t qs[3], os[3];
-  FastDiv by_page, by_tiles;  // by_tiles: query tiles of a key head
+  FastDiv by_page, by_tiles, by_group;  // by_tiles: query tiles of a key head
   int B, Z, Zkv, group, pages, width, per;  // per: sequences a lane counts
+  int T, rows, causal;  // tokens of a sequence (at most), rows of a key head: T group
   float c;           // scale log2(e)
   float *part;       // partial results of divided segments (whole segments have none)
   int4 *joins;
@@ -336,21 +307,38 @@ __device__ __forceinline__ float first_bits(float x) {
   return __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, x) & 0xffff0000u);
 }
 
-template <typename T, int A, int NQ>
-struct Attend {
+__device__ __forceinline__ uint32_t length_of(const AttendArgs &args, int b) {
+  const int n = args.lengths[b], most = args.width * (int)args.by_page.d;
+  return (uint32_t)(n < 0 ? 0 : n < most ? n : most);
+}
+// tokens of sequence b that are there
+__device__ __forceinline__ int tokens_of(const AttendArgs &args, int b) {
+  const int n = args.counts ? args.counts[b] : args.T;
+  return n < 0 ? 0 : n < args.T ? n : args.T;
+}
+
+// (the rows of a sequence in registers, of chunks alone)
+template <int KIND, int NQ> struct ChunkRows {};
+template <int NQ> struct ChunkRows<kEight | kChunk, NQ> { int rows; int64_t slot0; uint32_t lim[NQ], least; };
+template <int NQ> struct ChunkRows<kChunk, NQ> : ChunkRows<kEight | kChunk, NQ> {};
+
+template <typename T, int A, int NQ, int KIND>
+struct Attend : ChunkRows<KIND, NQ> {
   static constexpr int kKeys = AttendShape<T>::kKeys;
-  static constexpr bool kHalf = sizeof(T) == 2;
+  static constexpr bool kHalf = sizeof(T) == 2, k8 = KIND & kEight, kRows = KIND & kChunk;
   static constexpr int VW = kHalf && A % 128 == 0 ? 8 : 4;      // columns of a lane
   static constexpr int NB = A / (16 * VW);                      // blocks of 16 lanes' columns
   static constexpr int KT = kHalf ? 2 : 1;                      // 16-key tiles
-  static constexpr int KF = kHalf ? A / 32 : A / 16;            // 16-byte pieces of a key
+  static constexpr int KF = kHalf ? A / 32 : A / 16;            // 16-byte pieces of a query
+  static constexpr int KP = k8 ? KF / 2 : KF;                   // ... of a stored key
   static constexpr int VR = kHalf ? 8 : 4;                      // rows of V of a lane
-  static constexpr int kDw = kHalf ? VW / 2 : VW;               // dwords of a row of V
+  static constexpr int kDw = k8 ? VW / 4 : kHalf ? VW / 2 : VW; // dwords of a stored row of V
+  static constexpr int kRowBytes = k8 ? A : A * (int)sizeof(T);
   static constexpr int kRow = A + 4;                            // floats of a row in LDS
   typedef __attribute__((__vector_size__(kDw * sizeof(uint32_t)))) uint32_t VReg;
 
   // registers: tile, operands and accumulators, and about 60 more; of 512 a SIMD has room for these waves
-  static constexpr int kRegs = 4 * (KT * KF + NQ * KF + NQ * NB * VW) + VR * NB * kDw + 60;
+  static constexpr int kRegs = 4 * (KT * KP + NQ * KF + NQ * NB * VW) + VR * NB * kDw + 60 + (k8 ? 8 * NQ : 0) + (kRows ? 8 * NQ : 0);
   static constexpr int kSimd = kRegs <= 128 ? 4 : kRegs <= 256 ? 2 : 1;
   static constexpr int kWaves = 4, kTiles = kWaves, kUnit = kKeys * kTiles;
 
@@ -366,8 +354,9 @@ struct Attend {
   u32x4 q[NQ][KF];
   f32x4 acc[NQ][NB * VW];
   float m[NQ], l[NQ];
-  u32x4 kr[KT][KF];
+  u32x4 kr[KT][KP];
   VReg vr[VR][NB];
+  uint32_t ks, vs;  // exponents of this lane's slot's rows (e4m3)
 
   __device__ __forceinline__ Attend(const AttendArgs &a, Lds &s)
       : args(a), lds(s), lane(threadIdx.x & 63), wave(threadIdx.x >> 6), g(lane >> 4), n16(lane & 15) {}
@@ -394,10 +383,11 @@ struct Attend {
     __builtin_amdgcn_sched_barrier(0);  // (one wait for all of them)
 #pragma unroll
     for (int t = 0; t < KT; ++t) {
-      const u32x4 *p = reinterpret_cast<const u32x4 *>(static_cast<const T *>(args.Kc) + (uint64_t)row[t] * A) + g;
+      const u32x4 *p = reinterpret_cast<const u32x4 *>(static_cast<const char *>(args.Kc) + (uint64_t)row[t] * kRowBytes) + g;
 #pragma unroll
-      for (int i = 0; i < KF; ++i) kr[t][i] = __builtin_nontemporal_load(p + 4 * i);
+      for (int i = 0; i < KP; ++i) kr[t][i] = __builtin_nontemporal_load(p + 4 * i);
     }
+    if constexpr (k8) ks = args.Ks[r.row];
   }
   __device__ __forceinline__ int key_of(int j) const { return 16 * (j >> 2) + 4 * g + (j & 3); }
   __device__ __forceinline__ void load_v(const Rows &r) {
@@ -407,24 +397,76 @@ struct Attend {
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int j = 0; j < VR; ++j) {
-      const VReg *p = reinterpret_cast<const VReg *>(static_cast<const T *>(args.Vc) + (uint64_t)row[j] * A) + n16;
+      const VReg *p = reinterpret_cast<const VReg *>(static_cast<const char *>(args.Vc) + (uint64_t)row[j] * kRowBytes) + n16;
 #pragma unroll
       for (int b = 0; b < NB; ++b) vr[j][b] = __builtin_nontemporal_load(p + 16 * b);
     }
+    if constexpr (k8) vs = args.Vs[r.row];
+  }
+  // Rows of a key head of sequence b
+  __device__ __forceinline__ int rows_here() const {
+    if constexpr (kRows) return this->rows;
+    else return args.group;
+  }
+  __device__ __forceinline__ void begin(int b) {
+    if constexpr (kRows) {
+      const int n = tokens_of(args, b);
+      this->rows = n * args.group;
+      this->slot0 = (int64_t)args.lengths[b] - n;
+    }
+  }
+  // Row `in` of key head h: its token and query head
+  __device__ __forceinline__ void place(int h, int in, int &token, int &z) const {
+    token = kRows ? (int)args.by_group((uint32_t)in) : 0;
+    z = h * args.group + in - token * args.group;
+  }
+  // The first slot that row `in` does not see
+  __device__ __forceinline__ uint32_t limit_of(int in, uint32_t len) const {
+    if constexpr (kRows) {
+      const int64_t n = this->slot0 + (int)args.by_group((uint32_t)in) + 1;
+      return !args.causal ? len : n < 0 ? 0u : n < (int64_t)len ? (uint32_t)n : len;
+    }
+    return len;
   }
   __device__ __forceinline__ void load_q(int b, int h, int tile) {
 #pragma unroll
     for (int x = 0; x < NQ; ++x) {
       const int in = (tile * NQ + x) * 16 + n16;
-      const u32x4 *p = reinterpret_cast<const u32x4 *>(static_cast<const T *>(args.Q) + (int64_t)b * args.qs[0] +
-                                                       (int64_t)(h * args.group + in) * args.qs[1]) + g;
+      int token, z;
+      place(h, in, token, z);
+      const u32x4 *p = reinterpret_cast<const u32x4 *>(static_cast<const T *>(args.Q) + (int64_t)b * args.qs[0] + (int64_t)z * args.qs[1] +
+                                                       (kRows ? (int64_t)token * args.qs[2] : 0));
+      // (a 16-byte piece of e4m3 has the elements of two of a query's, side by side)
 #pragma unroll
-      for (int i = 0; i < KF; ++i) q[x][i] = in < args.group ? p[4 * i] : u32x4{0, 0, 0, 0};
+      for (int i = 0; i < KF; ++i) q[x][i] = in < rows_here() ? p[k8 ? 8 * (i >> 1) + 2 * g + (i & 1) : 4 * i + g] : u32x4{0, 0, 0, 0};
     }
+  }
+  // (of a slot that is not seen: 1, not what lies there)
+  __device__ __forceinline__ float power_of(uint32_t e, uint32_t seen) const {
+    return __builtin_bit_cast(float, ((seen >> (lane & (kKeys - 1))) & 1 ? e : 127u) << 23);
   }
 
   // Scores of the tile in kr: s[x][j] is key key_of(j)'s
-  __device__ __forceinline__ void scores(f32x4 (&s)[NQ][KT]) {
+  __device__ __forceinline__ void scores(f32x4 (&s)[NQ][KT], uint32_t seen) {
+    if constexpr (k8) {
+      const float power = power_of(ks, seen);
+#pragma unroll
+      for (int t = 0; t < KT; ++t) {
+        const float f = __shfl(power, 16 * t + n16);
+#pragma unroll
+        for (int x = 0; x < NQ; ++x) s[x][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < KP; ++i)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const bf16x8 k = __builtin_bit_cast(bf16x8, widened8(kr[t][i][2 * e], kr[t][i][2 * e + 1], f));
+#pragma unroll
+            for (int x = 0; x < NQ; ++x)
+              s[x][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, __builtin_bit_cast(bf16x8, q[x][2 * i + e]), s[x][t], 0, 0, 0);
+          }
+      }
+      return;
+    }
 #pragma unroll
     for (int x = 0; x < NQ; ++x)
 #pragma unroll
@@ -433,9 +475,9 @@ struct Attend {
 #pragma unroll
         for (int i = 0; i < KF; ++i) {
           if constexpr (kHalf) {
-            a = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kr[t][i]), __builtin_bit_cast(bf16x8, q[x][i]), a, 0, 0, 0);
+            a = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kr[t][i % KP]), __builtin_bit_cast(bf16x8, q[x][i]), a, 0, 0, 0);
           } else {
-            const f32x4 kf = __builtin_bit_cast(f32x4, kr[t][i]), qf = __builtin_bit_cast(f32x4, q[x][i]);
+            const f32x4 kf = __builtin_bit_cast(f32x4, kr[t][i % KP]), qf = __builtin_bit_cast(f32x4, q[x][i]);
 #pragma unroll
             for (int e = 0; e < 4; ++e) a = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[e], qf[e], a, 0, 0, 0);
           }
@@ -444,11 +486,26 @@ struct Attend {
       }
   }
   // The running maximum, and s to probabilities relative to it
-  __device__ __forceinline__ void softmax(f32x4 (&s)[NQ][KT], uint32_t seen) {
-    const bool all = seen == (kKeys == 32 ? ~0u : 0xffffu);
+  // Whether all rows of the query tile see all slots of a tile
+  __device__ __forceinline__ bool whole(uint32_t seen, uint32_t tile) const {
+    bool all = seen == (kKeys == 32 ? ~0u : 0xffffu);
+    if constexpr (kRows) all = all && (tile + 1) * kKeys <= this->least;
+    return all;
+  }
+  __device__ __forceinline__ void softmax(f32x4 (&s)[NQ][KT], uint32_t seen, uint32_t tile) {
+    const bool all = whole(seen, tile);
 #pragma unroll
     for (int x = 0; x < NQ; ++x) {
-      if (!all) {
+      if constexpr (kRows) {
+        if (!all) {
+          const int n = (int)this->lim[x] - (int)(tile * kKeys);
+          const uint32_t mine = seen & low_bits(n);
+#pragma unroll
+          for (int t = 0; t < KT; ++t)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) s[x][t][r] = (mine >> (16 * t + 4 * g + r)) & 1 ? s[x][t][r] : -INFINITY;
+        }
+      } else if (!all) {
 #pragma unroll
         for (int t = 0; t < KT; ++t)
 #pragma unroll
@@ -476,7 +533,7 @@ struct Attend {
         }
     }
   }
-  __device__ __forceinline__ void add_values(const f32x4 (&p)[NQ][KT], uint32_t seen) {
+  __device__ __forceinline__ void add_values(const f32x4 (&p)[NQ][KT], uint32_t seen, uint32_t tile) {
     // (0 times what lies in a slot that is not seen could be NaN)
     if (seen != (kKeys == 32 ? ~0u : 0xffffu)) {
 #pragma unroll
@@ -486,6 +543,100 @@ struct Attend {
 #pragma unroll
           for (int e = 0; e < kDw; ++e) vr[j][b][e] = (seen >> key_of(j)) & 1 ? vr[j][b][e] : 0u;
     }
+    if constexpr (kRows) {
+      // ... and so could 0 times an infinite or NaN value that other rows see: such values go by themselves.
+      if (!whole(seen, tile) && any_special()) take_special(seen, tile);
+    }
+    products(p, seen);
+  }
+  // Whether a value of the tile is infinite or NaN
+  __device__ __forceinline__ bool any_special() const {
+    uint32_t any = 0;
+#pragma unroll
+    for (int j = 0; j < VR; ++j)
+#pragma unroll
+      for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int e = 0; e < kDw; ++e) any |= specials(vr[j][b][e]);
+    return __any(any != 0);
+  }
+  // All bits of the elements of a dword of V that are infinite or NaN
+  __device__ __forceinline__ static uint32_t specials(uint32_t w) {
+    if constexpr (k8) {  // a byte 0x7f or 0xff: with the signs cleared, the only one that a 1 carries into the sign
+      const uint32_t top = ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
+      return (top - (top >> 7)) | top;
+    }
+    const uint32_t hi = (w & 0x7f800000u) == 0x7f800000u ? (kHalf ? 0xffff0000u : ~0u) : 0u;
+    return !kHalf ? hi : hi | ((w & 0x7f80u) == 0x7f80u ? 0xffffu : 0u);
+  }
+  // The infinite and NaN values of a tile to the rows that see them, and out of the tile.  What kinds of them a row's element
+  // gets is counted by a matrix product of ones (the row sees the slot) and 1, 2^10, 2^20 (infinite, -infinite, NaN).
+  __device__ __forceinline__ void take_special(uint32_t seen, uint32_t tile) {
+    uint32_t sees[NQ];  // bit j: slot key_of(j)
+#pragma unroll
+    for (int x = 0; x < NQ; ++x) {
+      sees[x] = 0;
+#pragma unroll
+      for (int j = 0; j < VR; ++j)
+        sees[x] |= (((seen >> key_of(j)) & 1) && tile * kKeys + key_of(j) < this->lim[x] ? 1u : 0u) << j;
+    }
+    const auto kind = [](uint32_t h) __attribute__((always_inline)) {  // of a bf16 number, as one
+      return (h & 0x7f80u) != 0x7f80u ? 0u : h & 0x7fu ? 0x4980u : h & 0x8000u ? 0x4480u : 0x3f80u;
+    };
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+      for (int i = 0; i < VW; ++i) {
+        __builtin_amdgcn_sched_barrier(0);  // (one at a time: all their comparisons at once fill the scalar registers)
+        f32x4 n[NQ];
+#pragma unroll
+        for (int x = 0; x < NQ; ++x) n[x] = f32x4{0.f, 0.f, 0.f, 0.f};
+        if constexpr (kHalf) {
+          u32x4 w;
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            uint32_t h[2];
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              const uint32_t v = vr[(2 * k + e) % VR][b][(k8 ? i >> 2 : i >> 1) % kDw];
+              if constexpr (k8) h[e] = ((v >> (8 * (i & 3))) & 0x7fu) == 0x7fu ? 0x4980u : 0u;
+              else h[e] = kind(i & 1 ? v >> 16 : v & 0xffffu);
+            }
+            w[k] = h[0] | h[1] << 16;
+          }
+#pragma unroll
+          for (int x = 0; x < NQ; ++x) {
+            u32x4 o;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) o[k] = ((sees[x] >> (2 * k)) & 1 ? 0x3f80u : 0u) | ((sees[x] >> (2 * k + 1)) & 1 ? 0x3f800000u : 0u);
+            n[x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, w), __builtin_bit_cast(bf16x8, o), n[x], 0, 0, 0);
+          }
+        } else {
+#pragma unroll
+          for (int x = 0; x < NQ; ++x)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+              const u32x4 v = __builtin_bit_cast(u32x4, vr[r][b]);
+              const uint32_t w = v[i % 4], h = w >> 16 | ((w & 0xffffu) != 0);  // (a NaN stays one)
+              n[x] = __builtin_amdgcn_mfma_f32_16x16x4f32(__builtin_bit_cast(float, kind(h) << 16), (sees[x] >> r) & 1 ? 1.f : 0.f, n[x], 0, 0, 0);
+            }
+        }
+#pragma unroll
+        for (int x = 0; x < NQ; ++x)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const uint32_t c = (uint32_t)n[x][r];
+            if (c) acc[x][b * VW + i][r] += c >= (1u << 20) || ((c & 1023u) && c >= 1024u) ? __builtin_nanf("") : c >= 1024u ? -INFINITY : INFINITY;
+          }
+      }
+#pragma unroll
+    for (int j = 0; j < VR; ++j)
+#pragma unroll
+      for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int e = 0; e < kDw; ++e) vr[j][b][e] &= ~specials(vr[j][b][e]);
+  }
+  __device__ __forceinline__ void products(const f32x4 (&p)[NQ][KT], uint32_t seen) {
     if constexpr (kHalf) {
       // The matrix core takes bf16: a probability goes to it as three, its first eight bits, the next eight and the rest, all 24 of
       // it (as two, 2^-16 of it is lost, which shows where values cancel.  Long walks from HBM take the same, whose matrix cores wait for
@@ -513,15 +664,29 @@ struct Attend {
 #pragma unroll
         for (int i = 0; i < 3; ++i) pb[x][i] = __builtin_bit_cast(bf16x8, w[i]);
       }
+      float power[k8 ? VR : 1];
+      if constexpr (k8) {
+        const float mine = power_of(vs, seen);
+#pragma unroll
+        for (int j = 0; j < VR; ++j) power[j] = __shfl(mine, key_of(j));
+      }
 #pragma unroll
       for (int b = 0; b < NB; ++b)
 #pragma unroll
         for (int i = 0; i < VW; ++i) {
           u32x4 w;
 #pragma unroll
-          for (int k = 0; k < 4; ++k)
-            w[k] = __builtin_amdgcn_perm(vr[(2 * k + 1) % VR][b][(i >> 1) % kDw], vr[(2 * k) % VR][b][(i >> 1) % kDw],
-                                         i & 1 ? 0x07060302u : 0x05040100u);
+          for (int k = 0; k < 4; ++k) {
+            uint32_t lo, hi;  // columns i and i ^ 1 of two rows
+            if constexpr (k8) {
+              lo = widened2(vr[2 * k][b][i >> 2], power[2 * k], (i >> 1) & 1);
+              hi = widened2(vr[2 * k + 1][b][i >> 2], power[2 * k + 1], (i >> 1) & 1);
+            } else {
+              lo = vr[(2 * k) % VR][b][(i >> 1) % kDw];
+              hi = vr[(2 * k + 1) % VR][b][(i >> 1) % kDw];
+            }
+            w[k] = __builtin_amdgcn_perm(hi, lo, i & 1 ? 0x07060302u : 0x05040100u);
+          }
 #pragma unroll
           for (int x = 0; x < NQ; ++x)
 #pragma unroll
@@ -549,7 +714,19 @@ struct Attend {
   __device__ __forceinline__ void walk(int b, int h, int tile, uint32_t len, uint32_t t, uint32_t end) {
     const int32_t *table = args.table + (int64_t)b * args.width;
     t += wave;
+    begin(b);
     load_q(b, h, tile);
+    if constexpr (kRows) {
+      const int first = tile * NQ * 16, last = (first + NQ * 16 < this->rows ? first + NQ * 16 : this->rows) - 1;
+      this->least = limit_of(first, len);
+      const uint32_t most = (limit_of(last < first ? first : last, len) + kKeys - 1) / kKeys;
+      end = first >= this->rows ? 0u : end < most ? end : most;
+#pragma unroll
+      for (int x = 0; x < NQ; ++x) {
+        const int in = first + x * 16 + n16;
+        this->lim[x] = in < this->rows ? limit_of(in, len) : 0u;
+      }
+    }
 #pragma unroll
     for (int x = 0; x < NQ; ++x) {
       m[x] = -INFINITY;
@@ -567,18 +744,18 @@ struct Attend {
     __builtin_amdgcn_sched_barrier(0);
     f32x4 s[NQ][KT];
     for (; t + kWaves < end; t += kWaves) {  // (the last tile behind the loop: in it, no wait counts loads that may be missing)
-      scores(s);
+      scores(s, now.seen);
       const Rows next = rows_of(id, len, h, t + kWaves);
       load_k(next);
       id = page_of(table, len, t + 2 * kWaves);
-      softmax(s, now.seen);
-      add_values(s, now.seen);
+      softmax(s, now.seen, t);
+      add_values(s, now.seen, t);
       load_v(next);
       now = next;
     }
-    scores(s);
-    softmax(s, now.seen);
-    add_values(s, now.seen);
+    scores(s, now.seen);
+    softmax(s, now.seen, t);
+    add_values(s, now.seen, t);
 #pragma unroll
     for (int x = 0; x < NQ; ++x) {
       l[x] += __shfl_xor(l[x], 16);
@@ -590,7 +767,7 @@ struct Attend {
   __device__ __forceinline__ void finish(int b, int h, int tile, float *part) {
 #pragma unroll
     for (int x = 0; x < NQ; ++x) {
-      const int rows = args.group - (tile * NQ + x) * 16;  // of this tile
+      const int rows = rows_here() - (tile * NQ + x) * 16;  // of this tile
       __syncthreads();                                     // (LDS is read to the end)
       if (rows <= 0) break;
       if (n16 < rows) {
@@ -626,43 +803,53 @@ struct Attend {
           *reinterpret_cast<f32x4 *>(p + col) = o;
           if (col == 0) *reinterpret_cast<float2 *>(p + A) = make_float2(top, sum);
         } else {
-          store_row(args, b, h * args.group + (tile * NQ + x) * 16 + row, col, o, top, sum);
+          int token, z;
+          place(h, (tile * NQ + x) * 16 + row, token, z);
+          store_row(args, b, z, token, col, o, top, sum);
         }
       }
     }
   }
 
   // Four columns of a row's result from sums relative to 2^top, and its LSE.
-  static __device__ __forceinline__ void store_row(const AttendArgs &args, int b, int z, int col, f32x4 o, float top, float sum) {
+  static __device__ __forceinline__ void store_row(const AttendArgs &args, int b, int z, int token, int col, f32x4 o, float top, float sum) {
     const float inv = sum != 0.f ? 1.f / sum : 0.f;
     T *y = static_cast<T *>(args.O) + (int64_t)b * args.os[0] + (int64_t)z * args.os[1] + col;
+    if constexpr (kRows) y += (int64_t)token * args.os[2];
     if constexpr (kHalf) {
       *reinterpret_cast<u32x2 *>(y) = u32x2{pack_bf16(o[0] * inv, o[1] * inv), pack_bf16(o[2] * inv, o[3] * inv)};
     } else {
       *reinterpret_cast<f32x4 *>(y) = o * inv;
     }
-    if (col == 0) args.LSE[(int64_t)b * args.Z + z] = sum != 0.f ? (top + __builtin_amdgcn_logf(sum)) * kLn2 : -INFINITY;
+    if (col == 0) {
+      const int64_t row = kRows ? ((int64_t)b * args.Z + z) * args.T + token : (int64_t)b * args.Z + z;
+      args.LSE[row] = sum != 0.f ? (top + __builtin_amdgcn_logf(sum)) * kLn2 : -INFINITY;
+    }
   }
 };
 
-__device__ __forceinline__ uint32_t length_of(const AttendArgs &args, int b) {
-  const int n = args.lengths[b], most = args.width * (int)args.by_page.d;
-  return (uint32_t)(n < 0 ? 0 : n < most ? n : most);
-}
-
 // A sequence with no key.
-template <typename T, int A, int NQ> __device__ __forceinline__ void store_empty(const AttendArgs &args, int b) {
-  for (int e = threadIdx.x; e < args.Z * (A / 4); e += 64 * Attend<T, A, NQ>::kWaves)
-    Attend<T, A, NQ>::store_row(args, b, e / (A / 4), e % (A / 4) * 4, f32x4{0.f, 0.f, 0.f, 0.f}, -INFINITY, 0.f);
+template <typename T, int A, int NQ, int KIND> __device__ __forceinline__ void store_empty(const AttendArgs &args, int b) {
+  const int tokens = KIND & kChunk ? tokens_of(args, b) : 1;
+  for (int t = 0; t < tokens; ++t)
+    for (int e = threadIdx.x; e < args.Z * (A / 4); e += 64 * Attend<T, A, NQ, KIND>::kWaves)
+      Attend<T, A, NQ, KIND>::store_row(args, b, e / (A / 4), t, e % (A / 4) * 4, f32x4{0.f, 0.f, 0.f, 0.f}, -INFINITY, 0.f);
+}
+// The slots of sequence b that its rows walk
+template <int KIND> __device__ __forceinline__ uint32_t walk_of(const AttendArgs &args, int b) {
+  if constexpr (KIND & kChunk) return tokens_of(args, b) > 0 ? length_of(args, b) : 0u;
+  return length_of(args, b);
 }
 
 // One work-group a segment: a sequence's key head and query tile.
-template <typename T, int A, int NQ>
-__global__ __launch_bounds__((64 * Attend<T, A, NQ>::kWaves), (Attend<T, A, NQ>::kSimd)) void attend_whole_kernel(AttendArgs args) {
-  typedef Attend<T, A, NQ> At;
+template <typename T, int A, int NQ, int KIND>
+__global__ __launch_bounds__((64 * Attend<T, A, NQ, KIND>::kWaves), (Attend<T, A, NQ, KIND>::kSimd)) void attend_whole_kernel(AttendArgs args) {
+  typedef Attend<T, A, NQ, KIND> At;
   __shared__ typename At::Lds lds;
   At at(args, lds);
-  const uint32_t head = args.by_tiles(blockIdx.x), tile = blockIdx.x - head * args.by_tiles.d, b = head / (uint32_t)args.Zkv, h = head - b * args.Zkv;
+  const uint32_t head = args.by_tiles(blockIdx.x), b = head / (uint32_t)args.Zkv, h = head - b * args.Zkv;
+  uint32_t tile = blockIdx.x - head * args.by_tiles.d;
+  if constexpr (KIND & kChunk) tile = args.by_tiles.d - 1 - tile;  // (the longest walks first)
   const uint32_t len = length_of(args, b);
   at.walk(b, h, tile, len, 0, (len + At::kKeys - 1) / At::kKeys);
   at.finish(b, h, tile, nullptr);
@@ -673,16 +860,16 @@ __global__ __launch_bounds__((64 * Attend<T, A, NQ>::kWaves), (Attend<T, A, NQ>:
 // work-group that has a divided segment's beginning writes down for the join where its parts lie: in the place of the segment or, if
 // there are more segments than shares, in its own (a share begins one divided segment at most).  Every place gets a note, if only that
 // there is nothing to do.
-template <typename T, int A, int NQ>
-__global__ __launch_bounds__((64 * Attend<T, A, NQ>::kWaves), (Attend<T, A, NQ>::kSimd)) void attend_shares_kernel(AttendArgs args) {
-  typedef Attend<T, A, NQ> At;
+template <typename T, int A, int NQ, int KIND>
+__global__ __launch_bounds__((64 * Attend<T, A, NQ, KIND>::kWaves), (Attend<T, A, NQ, KIND>::kSimd)) void attend_shares_kernel(AttendArgs args) {
+  typedef Attend<T, A, NQ, KIND> At;
   __shared__ typename At::Lds lds;
   At at(args, lds);
   const uint32_t heads = args.Zkv * args.by_tiles.d, w = blockIdx.x;
   const int4 nothing = make_int4(-1, 0, 0, 0);
   bool empty = false;
   const auto units_of = [&](int b) {
-    const uint32_t len = length_of(args, b);
+    const uint32_t len = walk_of<KIND>(args, b);
     empty |= len == 0;
     return (len + At::kUnit - 1) / At::kUnit;
   };
@@ -690,8 +877,8 @@ __global__ __launch_bounds__((64 * Attend<T, A, NQ>::kWaves), (Attend<T, A, NQ>:
   const uint32_t units = count.all() * heads;
   if (__any(empty))
     for (int b = w; b < args.B; b += gridDim.x)
-      if (length_of(args, b) == 0) {
-        store_empty<T, A, NQ>(args, b);
+      if (walk_of<KIND>(args, b) == 0) {
+        store_empty<T, A, NQ, KIND>(args, b);
         if (args.by_segment)
           for (uint32_t k = threadIdx.x; k < heads; k += 64 * At::kWaves) args.joins[b * heads + k] = nothing;
       }
@@ -709,10 +896,10 @@ __global__ __launch_bounds__((64 * Attend<T, A, NQ>::kWaves), (Attend<T, A, NQ>:
   // where the first unit is
   uint32_t before;
   int b = count.find(unit / heads, args.B, args.per, units_of, before);
-  uint32_t len = __builtin_amdgcn_readfirstlane(length_of(args, b)), n = (len + At::kUnit - 1) / At::kUnit;
+  uint32_t len = __builtin_amdgcn_readfirstlane(walk_of<KIND>(args, b)), n = (len + At::kUnit - 1) / At::kUnit;
   uint32_t rest = unit - before * heads, head = rest / n, in = rest - head * n;
   int4 join = nothing;
-  const size_t place = (size_t)(args.group < 16 * NQ ? args.group : 16 * NQ) * (A + 4);
+  const size_t place = (size_t)(args.rows < 16 * NQ ? args.rows : 16 * NQ) * (A + 4);
   for (bool begun = false; unit < end; begun = true) {
     const uint32_t left = end - unit, take = n - in < left ? n - in : left;
     const uint32_t h = args.by_tiles(head), tile = head - h * args.by_tiles.d;
@@ -729,7 +916,7 @@ __global__ __launch_bounds__((64 * Attend<T, A, NQ>::kWaves), (Attend<T, A, NQ>:
       head = 0;
       // the next sequence that is not empty, of 64 at a time (one by one, 2000 empty ones took 150 us)
       for (++b; b < args.B; b += 64) {
-        const uint32_t x = b + at.lane < args.B ? length_of(args, b + at.lane) : 0u;
+        const uint32_t x = b + at.lane < args.B ? walk_of<KIND>(args, b + at.lane) : 0u;
         const uint64_t some = __ballot(x > 0);
         if (some == 0) continue;
         b += __builtin_ctzll(some);
@@ -747,12 +934,12 @@ __global__ __launch_bounds__((64 * Attend<T, A, NQ>::kWaves), (Attend<T, A, NQ>:
 // memory).  Segments of 128 parts and more: 32 columns, so that 256 parts are in flight (one key head of 256, 16 queries, 32768
 // slots, 23.6 us as a whole with all columns, 18.6 with 32; one of 128, 32 queries, 131072 slots, 32.1 and 28.2; but eight of 128
 // with 8192 slots, 32 parts each, 13.8 and 14.5).
-template <typename T, int A, int NQ, int CB>
+template <typename T, int A, int NQ, int CB, int KIND>
 __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs args) {
   constexpr int cols = CB / 4, teams = 256 / cols;
   __shared__ f32x4 sums[teams * cols];
   __shared__ float2 ends[teams];
-  const int most = args.group < 16 * NQ ? args.group : 16 * NQ, team = threadIdx.x / cols;
+  const int most = args.rows < 16 * NQ ? args.rows : 16 * NQ, team = threadIdx.x / cols;
   const int col = (int)blockIdx.z * CB + (threadIdx.x - team * cols) * 4;
   const size_t place = (size_t)most * (A + 4);
   const float *base = args.part + (size_t)blockIdx.y * (A + 4);
@@ -772,7 +959,7 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs args) {
   if (j.x < 0) return;
   const uint32_t head = (uint32_t)j.y, h = args.by_tiles(head), tile = head - h * args.by_tiles.d;
   const int in = (int)tile * 16 * NQ + blockIdx.y, w = j.z >> 1, parts = j.w - w + 1;
-  if (in >= args.group) return;
+  if (in >= (KIND & kChunk ? tokens_of(args, j.x) * args.group : args.group)) return;
   float top = -INFINITY, sum = 0.f;
   f32x4 o = {0.f, 0.f, 0.f, 0.f};
   if (team < teams) {
@@ -816,7 +1003,8 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs args) {
     sum += f * ends[k].y;
     o += f * sums[k * cols + threadIdx.x];
   }
-  Attend<T, A, NQ>::store_row(args, j.x, (int)h * args.group + in, col, o, top, sum);
+  const int token = KIND & kChunk ? (int)args.by_group((uint32_t)in) : 0;
+  Attend<T, A, NQ, KIND>::store_row(args, j.x, (int)h * args.group + in - token * args.group, token, col, o, top, sum);
 }
 
 // ------------------------------------------------------------------ join ----
@@ -917,12 +1105,13 @@ struct AttendPlan {
 // Shares: up to three a CU for heads of 64, two, or with heads of 256 one, as registers leave room.  More than 4096 sequences (a lane
 // counts 64) or 2^31 units go by whole segments whatever their length: one sequence of 131072 slots among 4095 of 64 takes 122 us, among
 // 4096 of them 1730.
-AttendPlan attend_plan(const CacheDims &d) {
+// all: rows of a key head
+AttendPlan attend_plan(const CacheDims &d, int all) {
   AttendPlan p;
-  const int group = d.Z / d.Zkv, unit = 64;  // (of at least that many slots)
-  p.nq = group > 16 && d.A <= 128 ? 2 : 1;   // (two tiles of longer heads do not fit the registers)
-  p.tiles = (group + 16 * p.nq - 1) / (16 * p.nq);
-  p.rows = group < 16 * p.nq ? group : 16 * p.nq;
+  const int unit = 64;                     // (of at least that many slots)
+  p.nq = all > 16 && d.A <= 128 ? 2 : 1;   // (two tiles of longer heads do not fit the registers)
+  p.tiles = (all + 16 * p.nq - 1) / (16 * p.nq);
+  p.rows = all < 16 * p.nq ? all : 16 * p.nq;
   const int64_t slots = (int64_t)d.width * d.page, heads = (int64_t)d.Zkv * p.tiles, units = d.B * (slots / unit + 1) * heads;
   const bool whole = slots * d.A * (d.dtype == RSA_BF16 ? 2 : 4) <= 96 * 1024 || d.B > 4096 || units >= (1LL << 31);
   p.groups = whole ? 0 : (d.A == 64 ? 3 : d.A == 256 ? 1 : 2) * kCUs;
@@ -933,59 +1122,87 @@ AttendPlan attend_plan(const CacheDims &d) {
   p.many_parts = most >= 128 * segments;
   return p;
 }
+// ... of a chunk of T tokens: as many whole segments as shares, and there is nothing to divide
+AttendPlan chunk_plan(const CacheDims &d, int T) {
+  AttendPlan p = attend_plan(d, T * (d.Z / d.Zkv));
+  if ((int64_t)d.B * d.Zkv * p.tiles >= 4 * kCUs) p.groups = 0;
+  return p;
+}
 size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
-
-template <typename T, int A, int NQ>
-void launch_attend(const AttendArgs &a, const AttendPlan &p, hipStream_t st) {
-  if (p.groups == 0) {
-    attend_whole_kernel<T, A, NQ><<<a.B * a.Zkv * p.tiles, 64 * Attend<T, A, NQ>::kWaves, 0, st>>>(a);
-    return;
-  }
-  attend_shares_kernel<T, A, NQ><<<p.groups, 64 * Attend<T, A, NQ>::kWaves, 0, st>>>(a);
-  const uint32_t notes = a.by_segment ? a.B * a.Zkv * p.tiles : p.groups;
-  if (p.many_parts) attend_join_kernel<T, A, NQ, 32><<<dim3(notes, p.rows, A / 32), 256, 0, st>>>(a);
-  else attend_join_kernel<T, A, NQ, A><<<dim3(notes, p.rows), 256, 0, st>>>(a);
-}
-template <typename T, int A>
-void launch_attend(const AttendArgs &a, const AttendPlan &p, hipStream_t st) {
-  if constexpr (A <= 128) {
-    if (p.nq == 2) return launch_attend<T, A, 2>(a, p, st);
-  }
-  launch_attend<T, A, 1>(a, p, st);
-}
-template <typename T>
-void launch_attend(const AttendArgs &a, const AttendPlan &p, int A, hipStream_t st) {
-  switch (A) {
-    case 64: return launch_attend<T, 64>(a, p, st);
-    case 128: return launch_attend<T, 128>(a, p, st);
-    case 192: return launch_attend<T, 192>(a, p, st);
-    default: return launch_attend<T, 256>(a, p, st);
-  }
-}
-
-}  // namespace
-
 // The join's notes, 16 bytes a share, then two parts of a segment a share: rows of A sums, the maximum, the sum, two unused.
-size_t cache_workspace_bytes(const CacheDims &d) {
-  const AttendPlan p = attend_plan(d);
+size_t plan_bytes(const CacheDims &d, const AttendPlan &p) {
   return p.groups == 0 ? 0 : align256(p.groups * sizeof(int4)) + align256((size_t)2 * p.groups * p.rows * (d.A + 4) * 4);
 }
 
-hipError_t cache_attend(const CacheDims &d, const void *Q, const void *Kc, const void *Vc, const int32_t *table,
-                        const int32_t *lengths, void *O, float *LSE, void *ws, hipStream_t st) {
-  const AttendPlan p = attend_plan(d);
+template <typename T, int A, int NQ, int KIND>
+void launch_attend(const AttendArgs &a, const AttendPlan &p, hipStream_t st) {
+  constexpr int threads = 64 * Attend<T, A, NQ, KIND>::kWaves;
+  if (p.groups == 0) {
+    attend_whole_kernel<T, A, NQ, KIND><<<a.B * a.Zkv * p.tiles, threads, 0, st>>>(a);
+    return;
+  }
+  attend_shares_kernel<T, A, NQ, KIND><<<p.groups, threads, 0, st>>>(a);
+  const uint32_t notes = a.by_segment ? a.B * a.Zkv * p.tiles : p.groups;
+  if (p.many_parts) attend_join_kernel<T, A, NQ, 32, KIND><<<dim3(notes, p.rows, A / 32), 256, 0, st>>>(a);
+  else attend_join_kernel<T, A, NQ, A, KIND><<<dim3(notes, p.rows), 256, 0, st>>>(a);
+}
+template <typename T, int A, int KIND>
+void launch_attend(const AttendArgs &a, const AttendPlan &p, hipStream_t st) {
+  if constexpr (A <= 128) {
+    if (p.nq == 2) return launch_attend<T, A, 2, KIND>(a, p, st);
+  }
+  launch_attend<T, A, 1, KIND>(a, p, st);
+}
+template <typename T, int KIND>
+void launch_attend(const AttendArgs &a, const AttendPlan &p, int A, hipStream_t st) {
+  switch (A) {
+    case 64: return launch_attend<T, 64, KIND>(a, p, st);
+    case 128: return launch_attend<T, 128, KIND>(a, p, st);
+    case 192: return launch_attend<T, 192, KIND>(a, p, st);
+    default: return launch_attend<T, 256, KIND>(a, p, st);
+  }
+}
+
+AttendArgs attend_args(const CacheDims &d, const AttendPlan &p, const CachePools &c, const void *Q, const int32_t *table,
+                       const int32_t *lengths, void *O, float *LSE, void *ws) {
   AttendArgs a{};
-  a.Q = Q; a.Kc = Kc; a.Vc = Vc; a.table = table; a.lengths = lengths; a.O = O; a.LSE = LSE;
+  a.Q = Q; a.Kc = c.Kc; a.Vc = c.Vc; a.Ks = c.Ks; a.Vs = c.Vs; a.table = table; a.lengths = lengths; a.O = O; a.LSE = LSE;
   for (int k = 0; k < 3; ++k) { a.qs[k] = d.qs[k]; a.os[k] = d.os[k]; }
   a.by_page = make_fast_div(d.page); a.by_tiles = make_fast_div(p.tiles);
   a.B = d.B; a.Z = d.Z; a.Zkv = d.Zkv; a.group = d.Z / d.Zkv; a.pages = d.pages; a.width = d.width;
+  a.T = 1; a.rows = a.group; a.by_group = make_fast_div(a.group);
   a.per = (d.B + 63) / 64;
   a.c = d.scale * kLog2e;
   a.joins = static_cast<int4 *>(ws);
   a.by_segment = p.by_segment;
   a.part = reinterpret_cast<float *>(static_cast<char *>(ws) + align256(p.groups * sizeof(int4)));
-  if (d.dtype == RSA_BF16) launch_attend<bf16_t>(a, p, d.A, st);
-  else launch_attend<float>(a, p, d.A, st);
+  return a;
+}
+
+}  // namespace
+
+size_t cache_workspace_bytes(const CacheDims &d) { return plan_bytes(d, attend_plan(d, d.Z / d.Zkv)); }
+
+hipError_t cache_attend(const CacheDims &d, const CachePools &c, const void *Q, const int32_t *table, const int32_t *lengths, void *O,
+                        float *LSE, void *ws, hipStream_t st) {
+  const AttendPlan p = attend_plan(d, d.Z / d.Zkv);
+  const AttendArgs a = attend_args(d, p, c, Q, table, lengths, O, LSE, ws);
+  if (c.Ks) launch_attend<bf16_t, kEight>(a, p, d.A, st);
+  else if (d.dtype == RSA_BF16) launch_attend<bf16_t, kPlain>(a, p, d.A, st);
+  else launch_attend<float, kPlain>(a, p, d.A, st);
+  return hipGetLastError();
+}
+
+size_t chunk_few_workspace_bytes(const CacheDims &d, int T) { return plan_bytes(d, chunk_plan(d, T)); }
+
+hipError_t chunk_few(const CacheDims &d, const CachePools &c, int T, int causal, const void *Q, const int32_t *table, const int32_t *lengths,
+                     const int32_t *counts, void *O, float *LSE, void *ws, hipStream_t st) {
+  const AttendPlan p = chunk_plan(d, T);
+  AttendArgs a = attend_args(d, p, c, Q, table, lengths, O, LSE, ws);
+  a.counts = counts; a.causal = causal; a.T = T; a.rows = T * a.group;
+  if (c.Ks) launch_attend<bf16_t, kEight | kChunk>(a, p, d.A, st);
+  else if (d.dtype == RSA_BF16) launch_attend<bf16_t, kChunk>(a, p, d.A, st);
+  else launch_attend<float, kChunk>(a, p, d.A, st);
   return hipGetLastError();
 }
 

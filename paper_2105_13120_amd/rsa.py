@@ -27,6 +27,7 @@ EXPORTS = (
     "rsa_linformer_workspace_bytes", "rsa_linformer_project", "rsa_linformer_forward",
     "rsa_linformer_backward", "rsa_linformer_project_bwd",
     "rsa_rotate", "rsa_rotate_bwd", "rsa_cache_append", "rsa_cache_workspace_bytes", "rsa_cache_attend", "rsa_cache_join",
+    "rsa_cache_append8", "rsa_cache_attend8", "rsa_cache_read", "rsa_cache_chunk_workspace_bytes", "rsa_cache_attend_chunk",
 )
 
 
@@ -114,6 +115,12 @@ def lib():
         L.rsa_cache_workspace_bytes.restype = sz
         L.rsa_cache_attend.argtypes = [cp] + [vp] * 8 + [sz, vp]
         L.rsa_cache_join.argtypes = [cp, i] + [vp] * 5
+        L.rsa_cache_append8.argtypes = [cp, i] + [vp] * 7 + [i, i] + [vp] * 7
+        L.rsa_cache_attend8.argtypes = [cp] + [vp] * 10 + [sz, vp]
+        L.rsa_cache_read.argtypes = [cp, i] + [vp] * 10
+        L.rsa_cache_chunk_workspace_bytes.argtypes = [cp, i]
+        L.rsa_cache_chunk_workspace_bytes.restype = sz
+        L.rsa_cache_attend_chunk.argtypes = [cp, i, i] + [vp] * 11 + [sz, vp]
         _lib = L
     return _lib
 
@@ -354,35 +361,57 @@ def _like_given(given, t):
     return given if t is None else _like(given, t)
 
 
-# ---- a paged cache of keys and values, attention of one new token per sequence ----
+# ---- a paged cache of keys and values, attention of new tokens to it ----
 def make_cache_desc(Kc, table, Z, scale=0.0, Q=None, K=None, O=None):
-    """Descriptor for pools of shape (pages, Zkv, page, A), a table (B, width) and Z query heads.  Q, K, O, when given and not
-    contiguous, supply the strides of Q/Qr, of the new K/V and of O."""
+    """Descriptor for pools of shape (pages, Zkv, page, A), a table (B, width) and Z query heads.  Pools in e4m3 (torch.float8_e4m3fn,
+    with exponents Ks, Vs of their rows in the calls) are for calls in bf16.  Q, K, O, when given and not
+    contiguous, supply the strides of Q/Qr, of the new K/V (or those read) and of O."""
     pages, Zkv, page, A = Kc.shape
     B, width = table.shape
-    d = CacheDesc(B, Z, Zkv, A, page, pages, width, _dtype_code(Kc), float(scale), 0)
+    code = RSA_BF16 if Kc.dtype == torch.float8_e4m3fn else _dtype_code(Kc)
+    d = CacheDesc(B, Z, Zkv, A, page, pages, width, code, float(scale), 0)
     for name, t in (("q_stride", Q), ("kv_stride", K), ("o_stride", O)):
         if t is not None and not t.is_contiguous():
             setattr(d, name, _strides(t))
     return d
 
 
-def cache_append(desc, K, V, Kc, Vc, table, lengths, counts=None, first=None, inv_freq=None, adjacent=False, Q=None, Qr=None):
+def cache_append(desc, K, V, Kc, Vc, table, lengths, counts=None, first=None, inv_freq=None, adjacent=False, Q=None, Qr=None,
+                 Ks=None, Vs=None):
     """rsa_cache_append: K, V (B, Zkv, T, A) into the pools' slots lengths - counts .. lengths of every sequence (counts
     None: T), K turned by its position (first + slot).  Returns Q (B, Z, T, A) turned alike (None without Q); Qr may be Q.
-    Rows of Qr behind a sequence's count are left as they are; in a new tensor they are zero."""
+    Rows of Qr behind a sequence's count are left as they are; in a new tensor they are zero.
+    Pools in e4m3 (rsa_cache_append8) come with Ks, Vs: (pages, Zkv, page) bytes, each row's power of two + 127."""
     if Q is not None and type(Q) not in _PLAIN:
         Qr = _like(Qr, Q, torch.empty_like if counts is None else torch.zeros_like)
-    return _done(_native().cache_append(desc, K, V, Kc, Vc, table, lengths, counts, first, inv_freq, adjacent, Q, Qr))
+    return _done(_native().cache_append(desc, K, V, Kc, Vc, table, lengths, counts, first, inv_freq, adjacent, Q, Qr, Ks, Vs))
+
+
+def cache_read(desc, T, Kc, Vc, table, lengths, counts=None, K=None, V=None, Ks=None, Vs=None):
+    """rsa_cache_read: the slots lengths - counts .. lengths of every sequence (counts None: T) as K, V (B, Zkv, T, A), zero where they
+    are not held.  Rows behind a sequence's count are left as they are; in a new tensor they are zero."""
+    return _done(_native().cache_read(desc, T, Kc, Vc, table, lengths, counts, K, V, Ks, Vs))
 
 
 def cache_workspace_bytes(desc):
     return int(lib().rsa_cache_workspace_bytes(ctypes.byref(desc)))
 
 
-def cache_attend(desc, Q, Kc, Vc, table, lengths, O=None, LSE=None, ws=None):
-    """rsa_cache_attend: Q (B, Z, 1, A) to the first lengths[b] slots of every sequence.  Returns (O, LSE)."""
-    return _done(_native().cache_attend(desc, Q, Kc, Vc, table, lengths, O, LSE, ws))
+def cache_attend(desc, Q, Kc, Vc, table, lengths, O=None, LSE=None, ws=None, Ks=None, Vs=None):
+    """rsa_cache_attend: Q (B, Z, 1, A) to the first lengths[b] slots of every sequence.  Returns (O, LSE).  Ks, Vs: of pools in e4m3
+    (rsa_cache_attend8)."""
+    return _done(_native().cache_attend(desc, Q, Kc, Vc, table, lengths, O, LSE, ws, Ks, Vs))
+
+
+def cache_chunk_workspace_bytes(desc, T):
+    return int(lib().rsa_cache_chunk_workspace_bytes(ctypes.byref(desc), T))
+
+
+def cache_attend_chunk(desc, Q, Kc, Vc, table, lengths, counts=None, causal=True, O=None, LSE=None, ws=None, Ks=None, Vs=None):
+    """rsa_cache_attend_chunk: Q (B, Z, T, A), the tokens of slots lengths - counts .. lengths (counts None: T), each to the slots up to
+    its own (not causal: to all).  Returns (O, LSE).  Rows behind a sequence's count are left as they are; in new tensors they
+    are 0 and -inf.  Ks, Vs: of pools in e4m3."""
+    return _done(_native().cache_attend_chunk(desc, Q, Kc, Vc, table, lengths, counts, causal, O, LSE, ws, Ks, Vs))
 
 
 def cache_join(desc, Op, LSEp, O=None, LSE=None):
