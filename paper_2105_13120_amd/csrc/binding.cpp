@@ -9,15 +9,12 @@
 
 #include <ATen/ops/empty.h>
 #include <ATen/ops/empty_like.h>
-#include <ATen/ops/full.h>
-#include <ATen/ops/zeros.h>
 #include <ATen/ops/zeros_like.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <array>
-#include <cmath>
 
 #include "rsa.h"
 
@@ -426,7 +423,7 @@ PyObject *cache_read(Call &c) {
       for (int k = 0; k < 3; ++k)
         if (d.kv_stride[k] != 0) refuse(7 + i, "a result with strides has to be given");
       const auto o = c.tensor(2).options().dtype(type_of(d.dtype));
-      out[i] = counts ? at::zeros(shape, o) : at::empty(shape, o);
+      out[i] = at::empty(shape, o);
     } else {
       out[i] = c.tensor(7 + i);
     }
@@ -434,7 +431,7 @@ PyObject *cache_read(Call &c) {
   }
   check_device(c, 11);
   return finish([&](void *st) {
-    return rsa_cache_read(&d, (int32_t)T, ptr(c.tensor(2)), ptr(c.tensor(3)), exponents(c, 9), exponents(c, 10), table, lengths, counts,
+    return rsa_cache_read(&d, (int32_t)T, !c.given(7) | !c.given(8) << 1, ptr(c.tensor(2)), ptr(c.tensor(3)), exponents(c, 9), exponents(c, 10), table, lengths, counts,
                           ptr(out[0]), ptr(out[1]), st); }, {out[0], out[1]});
 }
 
@@ -473,19 +470,15 @@ PyObject *cache_attend_chunk(Call &c) {
   const int32_t *table, *lengths;
   check_places(c, 4, table, lengths);
   const int32_t *counts = int32s(c, 6, {d.B}), causal = truth(c, 7);
-  // (rows of tokens that are not there stay as they are)
-  const at::Tensor O = c.tensor_or(8, [&] { return counts ? at::zeros(shape, Q.options()) : at::empty(shape, Q.options()); });
+  const at::Tensor O = c.tensor_or(8, [&] { return at::empty(shape, Q.options()); });
   check(8, O, type_of(d.dtype), shape, d.o_stride);
-  const at::Tensor LSE = c.tensor_or(9, [&] {
-    const auto o = Q.options().dtype(at::kFloat);
-    return counts ? at::full({d.B, d.Z, T}, -INFINITY, o) : at::empty({d.B, d.Z, T}, o);
-  });
+  const at::Tensor LSE = c.tensor_or(9, [&] { return at::empty({d.B, d.Z, T}, Q.options().dtype(at::kFloat)); });
   check(9, LSE, at::kFloat, {d.B, d.Z, T});
   check_device(c, 13);
   size_t n = 0;
   const at::Tensor ws = cache_workspace(c, 10, c.given(10) ? 0 : rsa_cache_chunk_workspace_bytes(&d, T), Q, n);
   return finish([&](void *st) {
-    return rsa_cache_attend_chunk(&d, T, causal, ptr(Q), ptr(Kc), ptr(Vc), exponents(c, 11), exponents(c, 12), table, lengths, counts, ptr(O),
+    return rsa_cache_attend_chunk(&d, T, causal, !c.given(8) | !c.given(9) << 1, ptr(Q), ptr(Kc), ptr(Vc), exponents(c, 11), exponents(c, 12), table, lengths, counts, ptr(O),
                                   static_cast<float *>(ptr(LSE)), ptr(ws), n, st); }, {O, LSE});
 }
 

@@ -608,7 +608,7 @@ int rsa_cache_append8(const rsa_cache_desc *d, int32_t T, const void *Q, const v
   return append_to(d, T, Q, K, V, table, lengths, counts, first, R, adjacent, inv_freq, Qr, Kc, Vc, Ks, Vs, true, stream);
 }
 
-int rsa_cache_read(const rsa_cache_desc *d, int32_t T, const void *Kc, const void *Vc, const uint8_t *Ks, const uint8_t *Vs,
+int rsa_cache_read(const rsa_cache_desc *d, int32_t T, int32_t pad, const void *Kc, const void *Vc, const uint8_t *Ks, const uint8_t *Vs,
                    const int32_t *table, const int32_t *lengths, const int32_t *counts, void *K, void *V, void *stream) {
   RSA_CACHE_PROLOGUE(T, Kc && Vc && table && lengths && K && V && !Ks == !Vs, Kc, Vc, K, V);
   if (!words({table, lengths, counts}) || (Ks && d->dtype != RSA_BF16)) return RSA_ERR_UNSUPPORTED;
@@ -619,7 +619,7 @@ int rsa_cache_read(const rsa_cache_desc *d, int32_t T, const void *Kc, const voi
     return RSA_ERR_UNSUPPORTED;
   // (the kernel writes nothing to the pools)
   const rsa::CachePools pools = {const_cast<void *>(Kc), const_cast<void *>(Vc), const_cast<uint8_t *>(Ks), const_cast<uint8_t *>(Vs)};
-  return hip_status(rsa::cache_read(dm, pools, T, table, lengths, counts, K, V, st));
+  return hip_status(rsa::cache_read(dm, pools, T, counts ? pad & 3 : 0, table, lengths, counts, K, V, st));
 }
 
 size_t rsa_cache_workspace_bytes(const rsa_cache_desc *d) {
@@ -633,7 +633,7 @@ bool chunk_fits(const rsa::CacheDims &d, int64_t T) {
   return T * d.Z < (1LL << 31) && (int64_t)d.B * d.Z <= (1LL << 34) / d.A / T;
 }
 // T tokens per sequence (chunk), or the one of rsa_cache_attend
-int attend_to(const rsa_cache_desc *d, bool chunk, int32_t T, int32_t causal, const void *Q, const void *Kc, const void *Vc, const uint8_t *Ks,
+int attend_to(const rsa_cache_desc *d, bool chunk, int32_t T, int32_t causal, int32_t pad, const void *Q, const void *Kc, const void *Vc, const uint8_t *Ks,
               const uint8_t *Vs, const int32_t *table, const int32_t *lengths, const int32_t *counts, void *O, float *LSE, void *ws,
               size_t ws_bytes, void *stream) {
   RSA_CACHE_PROLOGUE(T, Q && Kc && Vc && table && lengths && O && LSE && !Ks == !Vs, Q, Kc, Vc, O, ws);
@@ -649,14 +649,14 @@ int attend_to(const rsa_cache_desc *d, bool chunk, int32_t T, int32_t causal, co
     return RSA_ERR_UNSUPPORTED;
   // (the kernels write nothing to the pools)
   const rsa::CachePools pools = {const_cast<void *>(Kc), const_cast<void *>(Vc), const_cast<uint8_t *>(Ks), const_cast<uint8_t *>(Vs)};
-  return hip_status(chunk ? rsa::cache_attend_chunk(dm, pools, T, causal != 0, Q, table, lengths, counts, O, LSE, ws, st)
+  return hip_status(chunk ? rsa::cache_attend_chunk(dm, pools, T, causal != 0, counts ? pad & 3 : 0, Q, table, lengths, counts, O, LSE, ws, st)
                           : rsa::cache_attend(dm, pools, Q, table, lengths, O, LSE, ws, st));
 }
 }  // namespace
 
 int rsa_cache_attend(const rsa_cache_desc *d, const void *Q, const void *Kc, const void *Vc, const int32_t *table,
                      const int32_t *lengths, void *O, float *LSE, void *ws, size_t ws_bytes, void *stream) {
-  return attend_to(d, false, 1, 1, Q, Kc, Vc, nullptr, nullptr, table, lengths, nullptr, O, LSE, ws, ws_bytes, stream);
+  return attend_to(d, false, 1, 1, 0, Q, Kc, Vc, nullptr, nullptr, table, lengths, nullptr, O, LSE, ws, ws_bytes, stream);
 }
 
 int rsa_cache_attend8(const rsa_cache_desc *d, const void *Q, const void *Kc, const void *Vc, const uint8_t *Ks, const uint8_t *Vs,
@@ -665,7 +665,7 @@ int rsa_cache_attend8(const rsa_cache_desc *d, const void *Q, const void *Kc, co
   const int rc = cache_validate(d, 1, &dm);
   if (rc != RSA_OK) return rc;
   if (!Ks || !Vs) return RSA_ERR_NULL;
-  return attend_to(d, false, 1, 1, Q, Kc, Vc, Ks, Vs, table, lengths, nullptr, O, LSE, ws, ws_bytes, stream);
+  return attend_to(d, false, 1, 1, 0, Q, Kc, Vc, Ks, Vs, table, lengths, nullptr, O, LSE, ws, ws_bytes, stream);
 }
 
 size_t rsa_cache_chunk_workspace_bytes(const rsa_cache_desc *d, int32_t T) {
@@ -673,10 +673,10 @@ size_t rsa_cache_chunk_workspace_bytes(const rsa_cache_desc *d, int32_t T) {
   return cache_validate(d, T, &dm) == RSA_OK && chunk_fits(dm, T) ? rsa::chunk_workspace_bytes(dm, T) : 0;
 }
 
-int rsa_cache_attend_chunk(const rsa_cache_desc *d, int32_t T, int32_t causal, const void *Q, const void *Kc, const void *Vc,
+int rsa_cache_attend_chunk(const rsa_cache_desc *d, int32_t T, int32_t causal, int32_t pad, const void *Q, const void *Kc, const void *Vc,
                            const uint8_t *Ks, const uint8_t *Vs, const int32_t *table, const int32_t *lengths, const int32_t *counts,
                            void *O, float *LSE, void *ws, size_t ws_bytes, void *stream) {
-  return attend_to(d, true, T, causal, Q, Kc, Vc, Ks, Vs, table, lengths, counts, O, LSE, ws, ws_bytes, stream);
+  return attend_to(d, true, T, causal, pad, Q, Kc, Vc, Ks, Vs, table, lengths, counts, O, LSE, ws, ws_bytes, stream);
 }
 
 int rsa_cache_join(const rsa_cache_desc *d, int32_t N, const void *Op, const float *LSEp, void *O, float *LSE, void *stream) {

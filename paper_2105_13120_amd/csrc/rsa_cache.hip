@@ -273,7 +273,7 @@ struct AttendArgs {
   int64_t qs[3], os[3];
   FastDiv by_page, by_tiles, by_group;  // by_tiles: query tiles of a key head
   int B, Z, Zkv, group, pages, width, per;  // per: sequences a lane counts
-  int T, rows, causal;  // tokens of a sequence (at most), rows of a key head: T group
+  int T, rows, causal, pad;  // tokens of a sequence (at most), rows of a key head: T group; which rows of tokens that are not there are written
   float c;           // scale log2(e)
   float *part;       // partial results of divided segments (whole segments have none)
   int4 *joins;
@@ -767,7 +767,7 @@ struct Attend : ChunkRows<KIND, NQ> {
   __device__ __forceinline__ void finish(int b, int h, int tile, float *part) {
 #pragma unroll
     for (int x = 0; x < NQ; ++x) {
-      const int rows = rows_here() - (tile * NQ + x) * 16;  // of this tile
+      const int rows = args.rows - (tile * NQ + x) * 16;  // of this tile, those of tokens that are not there among them
       __syncthreads();                                     // (LDS is read to the end)
       if (rows <= 0) break;
       if (n16 < rows) {
@@ -798,6 +798,11 @@ struct Attend : ChunkRows<KIND, NQ> {
           sum += f * lds.l[w][row];
           o += f * *reinterpret_cast<const f32x4 *>(&lds.o[w][row][col]);
         }
+        const bool there = !kRows || (tile * NQ + x) * 16 + row < rows_here();
+        if (!there) {
+          sum = 0.f;
+          o = f32x4{0.f, 0.f, 0.f, 0.f};
+        }
         if (part) {
           float *p = part + (size_t)(x * 16 + row) * (A + 4);
           *reinterpret_cast<f32x4 *>(p + col) = o;
@@ -805,23 +810,27 @@ struct Attend : ChunkRows<KIND, NQ> {
         } else {
           int token, z;
           place(h, (tile * NQ + x) * 16 + row, token, z);
-          store_row(args, b, z, token, col, o, top, sum);
+          store_row(args, b, z, token, col, o, top, sum, there);
         }
       }
     }
   }
 
   // Four columns of a row's result from sums relative to 2^top, and its LSE.
-  static __device__ __forceinline__ void store_row(const AttendArgs &args, int b, int z, int token, int col, f32x4 o, float top, float sum) {
+  // there: of a token that is
+  static __device__ __forceinline__ void store_row(const AttendArgs &args, int b, int z, int token, int col, f32x4 o, float top, float sum,
+                                                   bool there = true) {
+    const int write = !kRows || there ? 3 : args.pad;
     const float inv = sum != 0.f ? 1.f / sum : 0.f;
     T *y = static_cast<T *>(args.O) + (int64_t)b * args.os[0] + (int64_t)z * args.os[1] + col;
     if constexpr (kRows) y += (int64_t)token * args.os[2];
-    if constexpr (kHalf) {
+    if (!(write & 1)) {
+    } else if constexpr (kHalf) {
       *reinterpret_cast<u32x2 *>(y) = u32x2{pack_bf16(o[0] * inv, o[1] * inv), pack_bf16(o[2] * inv, o[3] * inv)};
     } else {
       *reinterpret_cast<f32x4 *>(y) = o * inv;
     }
-    if (col == 0) {
+    if (col == 0 && (write & 2)) {
       const int64_t row = kRows ? ((int64_t)b * args.Z + z) * args.T + token : (int64_t)b * args.Z + z;
       args.LSE[row] = sum != 0.f ? (top + __builtin_amdgcn_logf(sum)) * kLn2 : -INFINITY;
     }
@@ -831,9 +840,10 @@ struct Attend : ChunkRows<KIND, NQ> {
 // A sequence with no key.
 template <typename T, int A, int NQ, int KIND> __device__ __forceinline__ void store_empty(const AttendArgs &args, int b) {
   const int tokens = KIND & kChunk ? tokens_of(args, b) : 1;
-  for (int t = 0; t < tokens; ++t)
+  for (int t = 0; t < (args.pad ? args.T : tokens); ++t)
     for (int e = threadIdx.x; e < args.Z * (A / 4); e += 64 * Attend<T, A, NQ, KIND>::kWaves)
-      Attend<T, A, NQ, KIND>::store_row(args, b, e / (A / 4), t, e % (A / 4) * 4, f32x4{0.f, 0.f, 0.f, 0.f}, -INFINITY, 0.f);
+      Attend<T, A, NQ, KIND>::store_row(args, b, e / (A / 4), t, e % (A / 4) * 4, f32x4{0.f, 0.f, 0.f, 0.f}, -INFINITY, 0.f,
+                                            t < tokens);
 }
 // The slots of sequence b that its rows walk
 template <int KIND> __device__ __forceinline__ uint32_t walk_of(const AttendArgs &args, int b) {
@@ -959,7 +969,7 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs args) {
   if (j.x < 0) return;
   const uint32_t head = (uint32_t)j.y, h = args.by_tiles(head), tile = head - h * args.by_tiles.d;
   const int in = (int)tile * 16 * NQ + blockIdx.y, w = j.z >> 1, parts = j.w - w + 1;
-  if (in >= (KIND & kChunk ? tokens_of(args, j.x) * args.group : args.group)) return;
+  if (in >= args.rows) return;
   float top = -INFINITY, sum = 0.f;
   f32x4 o = {0.f, 0.f, 0.f, 0.f};
   if (team < teams) {
@@ -1004,7 +1014,8 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs args) {
     o += f * sums[k * cols + threadIdx.x];
   }
   const int token = KIND & kChunk ? (int)args.by_group((uint32_t)in) : 0;
-  Attend<T, A, NQ, KIND>::store_row(args, j.x, (int)h * args.group + in - token * args.group, token, col, o, top, sum);
+  Attend<T, A, NQ, KIND>::store_row(args, j.x, (int)h * args.group + in - token * args.group, token, col, o, top, sum,
+                                    !(KIND & kChunk) || token < tokens_of(args, j.x));
 }
 
 // ------------------------------------------------------------------ join ----
@@ -1195,11 +1206,11 @@ hipError_t cache_attend(const CacheDims &d, const CachePools &c, const void *Q, 
 
 size_t chunk_few_workspace_bytes(const CacheDims &d, int T) { return plan_bytes(d, chunk_plan(d, T)); }
 
-hipError_t chunk_few(const CacheDims &d, const CachePools &c, int T, int causal, const void *Q, const int32_t *table, const int32_t *lengths,
+hipError_t chunk_few(const CacheDims &d, const CachePools &c, int T, int causal, int pad, const void *Q, const int32_t *table, const int32_t *lengths,
                      const int32_t *counts, void *O, float *LSE, void *ws, hipStream_t st) {
   const AttendPlan p = chunk_plan(d, T);
   AttendArgs a = attend_args(d, p, c, Q, table, lengths, O, LSE, ws);
-  a.counts = counts; a.causal = causal; a.T = T; a.rows = T * a.group;
+  a.counts = counts; a.causal = causal; a.pad = pad; a.T = T; a.rows = T * a.group;
   if (c.Ks) launch_attend<bf16_t, kEight | kChunk>(a, p, d.A, st);
   else if (d.dtype == RSA_BF16) launch_attend<bf16_t, kChunk>(a, p, d.A, st);
   else launch_attend<float, kChunk>(a, p, d.A, st);

@@ -57,12 +57,12 @@ struct TokenArgs {
     return c < T ? c : T;
   }
 };
-// Token t of sequence b: whether it is there, its slot, and the row of a pool's first head that it lies in (-1: on no page that is
+// Token t of sequence b: whether there is such a row, whether the token is there, its slot, and the row of a pool's first head that it lies in (-1: on no page that is
 // held, page * Zkv * tokens of a page + place otherwise).
 struct TokenPlace {
   uint32_t b, t;
   int64_t slot;
-  bool there;
+  bool any, there;
   __device__ __forceinline__ int64_t row(const TokenArgs &a, int Zkv) const {
     const uint32_t page = a.by_page.d;
     if (!there || slot < 0 || slot >= (int64_t)a.width * page) return -1;
@@ -94,9 +94,10 @@ struct TokenTiles {
     }
   }
   __device__ __forceinline__ TokenPlace place(uint32_t r) const {
-    TokenPlace p{b0, t0 + r, 0, false};
+    TokenPlace p{b0, t0 + r, 0, false, false};
     if (a.per ? p.t >= a.by_T.d : p.t >= a.tokens) return p;
     if (!a.per) { p.b = a.by_T(p.t); p.t -= p.b * a.by_T.d; }
+    p.any = true;
     const int c = a.count_of(p.b);
     p.there = (int)p.t < c;
     p.slot = (int64_t)a.lengths[p.b] - c + p.t;

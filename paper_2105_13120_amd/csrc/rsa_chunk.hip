@@ -16,6 +16,8 @@
 #include "rsa_fused_tile.h"
 #include "rsa_kernels.h"
 
+#include <algorithm>
+
 namespace rsa {
 namespace {
 
@@ -28,9 +30,12 @@ struct ChunkArgs {
   float *LSE;
   int64_t qs[3], os[3];
   FastDiv by_page, by_group, by_heads, by_Zkv, by_row;  // by_heads: B Zkv; by_row: 16-byte pieces of a row in e4m3
-  int Z, Zkv, T, pages, width, causal, tiles;           // tiles: row tiles of a key head
+  int B, Z, Zkv, T, pages, width, causal, pad, tiles;   // tiles: row tiles of a key head
   float cl2;                                            // scale log2(e)
-  // divided walks (gridDim.y > 1): per part, key head and row the unnormalised O and the pair (maximum cl2, sum) that it is relative to
+  // Divided walks, where there may be parts > 1 of them: how many parts each sequence's are in, and per part, key head and row tile the
+  // unnormalised O, as the accumulators hold it (16 bytes a lane), and per row the pair (maximum cl2, sum) that it is relative to
+  int parts;
+  uint32_t *divided;
   float *part_o, *part_ml;
 };
 
@@ -43,6 +48,115 @@ __device__ __forceinline__ uint32_t length_of(const ChunkArgs &a, int b) {
   return (uint32_t)(n < 0 ? 0 : n < most ? n : most);
 }
 
+// What a call's work-groups take: a row tile of a key head of a sequence and, where its walk is divided, one of its parts.
+struct Item {
+  uint32_t b, h;
+  int tile, part, parts;
+};
+
+// Sequences of different lengths with different numbers of new tokens leave tiles without rows and walks of all lengths.  Up to
+// kSorted sequences are laid out by what they have: all items by the length of their walks, the longest first, without gaps (by
+// tiles of the longest call instead, empty ones among them: prompts of 128 to 2048 tokens 154 us, see below).  A walk that is long beside a
+// place's share of all the work is divided.
+//
+// A tile's walk is w = ceil(n / P) long, n the tiles of 64 slots that its last row sees and P the parts of its sequence's walks.  The
+// last row's limit grows with the tile, so that the tiles of a sequence with walks of w and more are those from a first one on, and
+// F(w), how many items there are of w and more, is a sum over the sequences.  The item `id` in descending order is in level w with
+// F(w + 1) <= id < F(w), found by halves; a lane has a sequence.
+constexpr int kSorted = 64;
+
+// Sums of a lane and those before it
+__device__ __forceinline__ uint32_t scan_lanes(uint32_t x) {
+  x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x111, 0xf, 0xf, true);  // row_shr 1, 2, 4, 8: within 16 lanes
+  x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x112, 0xf, 0xf, true);
+  x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x114, 0xf, 0xf, true);
+  x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x118, 0xf, 0xf, true);
+  x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x142, 0xa, 0xf, false);  // lane 15 of a row to the next, lane 31 to the upper half
+  x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x143, 0xc, 0xf, false);
+  return x;
+}
+__device__ __forceinline__ uint32_t sum_lanes(uint32_t x) { return (uint32_t)__builtin_amdgcn_readlane((int)scan_lanes(x), 63); }
+template <int BM>
+struct Layout {
+  const ChunkArgs &a;
+  int lane, tiles, most, slot0, parts;  // of the lane's sequence: row tiles that have any, tiles of its longest walk, its first token's slot
+  __device__ __forceinline__ static uint32_t walk_of(const ChunkArgs &a, int64_t slot0, uint32_t len, int token) {
+    const int64_t n = slot0 + token + 1;
+    const uint32_t see = !a.causal ? len : n < 0 ? 0u : n < (int64_t)len ? (uint32_t)n : len;
+    return (see + kTileKeys - 1) / kTileKeys;
+  }
+  __device__ __forceinline__ static int of(int x, int b) { return __builtin_amdgcn_readlane(x, b); }
+  // Tiles of a sequence whose walks are longer than n.  (n < most: 64 n lies in front of the last token's slot, and nothing passes 32 bits.)
+  __device__ __forceinline__ static int longer(const ChunkArgs &a, int n, int tiles, int most, int slot0) {
+    const int x = n * kTileKeys - slot0;  // their last rows are of this token at least
+    const int first = a.causal && x > 0 ? (int)((uint32_t)x * a.by_group.d / BM) : 0;
+    return n < most ? tiles - first : 0;
+  }
+  __device__ __forceinline__ explicit Layout(const ChunkArgs &args) : a(args), lane(threadIdx.x & 63) {
+    const bool in = lane < a.B;
+    const int tokens = in ? tokens_of(a, lane) : 0;
+    const uint32_t len = in ? length_of(a, lane) : 0u;
+    slot0 = len > 0 ? a.lengths[lane] - tokens : 0;  // (of a sequence with slots)
+    const int rows = tokens * (int)a.by_group.d;
+    tiles = (rows + BM - 1) / BM;
+    most = tokens > 0 ? (int)walk_of(a, slot0, len, tokens - 1) : 0;
+    parts = 1;
+    if (a.parts > 1) divide(len, rows);
+  }
+  // How many parts: lane q - 1 estimates what the call takes, in tiles of a place, with parts of at most a q-th of the longest walk.  Walks
+  // of about one length go by the rounds that they need, others are dealt to the places as these become free; a walk needs three
+  // tiles' time besides, as a part another three for its result, their join five.
+  __device__ __forceinline__ void divide(uint32_t len, int rows) {
+    int longest = 0;
+    for (int b = 0; b < a.B; ++b) longest = longest > of(most, b) ? longest : of(most, b);
+    const int q = lane + 1, per = (longest + q - 1) / q;
+    const float share = 1.f / (float)(per > 0 ? per : 1);
+    const int mean2 = most + (rows > 0 ? (int)walk_of(a, slot0, len, ((BM < rows ? BM : rows) - 1) / (int)a.by_group.d) : 0);
+    float all = 0.f, items = 0.f;
+    for (int b = 0; b < a.B; ++b) {
+      const float t = (float)(of(tiles, b) * a.Zkv);
+      all += t * 0.5f * (float)of(mean2, b);
+      items += t * __builtin_ceilf((float)of(most, b) * share);
+    }
+    constexpr float places = 2 * kCUs;
+    const float rounds = __builtin_ceilf(items / places), longest_one = items <= 0.5f * places ? 0.6f * (float)per : (float)per;
+    const float walks = all > 0.85f * items * (float)per ? rounds * longest_one : fmaxf(longest_one, all / places + 0.2f * (float)per);
+    float cost = walks + items / places * (q > 1 ? 6.f : 3.f) + (q > 1 ? 5.f : 0.f);
+    if (q > a.parts) cost = INFINITY;
+    float best = cost;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) best = fminf(best, __shfl_xor(best, o));
+    const int chosen = __builtin_ctzll(__ballot(cost == best)) + 1, most_of_part = (longest + chosen - 1) / chosen;
+    parts = most > most_of_part ? (most + most_of_part - 1) / most_of_part : 1;
+  }
+  // Items of levels w and more
+  __device__ __forceinline__ uint32_t upto(int w) const {
+    const int have = longer(a, w > 0 ? (w - 1) * parts : 0, tiles, most, slot0);
+    return sum_lanes(lane >= a.B ? 0u : (uint32_t)(w > 0 ? have * parts : have * (parts - 1) + a.tiles)) * (uint32_t)a.Zkv;
+  }
+  __device__ __forceinline__ bool find(uint32_t id, Item &it) const {
+    if (id >= upto(0)) return false;
+    int lo = 0, hi = (int)(((uint32_t)a.width * a.by_page.d + kTileKeys - 1) / kTileKeys) + 1;  // F(lo) > id >= F(hi)
+    while (hi - lo > 1) {
+      const int w = (lo + hi) >> 1;
+      if (upto(w) > id) lo = w;
+      else hi = w;
+    }
+    const int above = longer(a, lo * parts, tiles, most, slot0), mine = longer(a, lo > 0 ? (lo - 1) * parts : 0, tiles, most, slot0);
+    const uint32_t n = (lane < a.B ? (uint32_t)(lo > 0 ? (mine - above) * parts : a.tiles - mine) : 0u) * (uint32_t)a.Zkv, s = scan_lanes(n);
+    const uint32_t r = id - upto(lo + 1);
+    const int b = __builtin_ctzll(__ballot(r < s));
+    const uint32_t j = r - (uint32_t)of((int)(s - n), b), k = a.by_Zkv(j);
+    it.b = (uint32_t)b; it.h = j - k * (uint32_t)a.Zkv;
+    it.parts = lo > 0 ? of(parts, b) : 1;
+    const uint32_t t = it.parts > 1 ? k / (uint32_t)it.parts : k;
+    it.part = (int)(k - t * (uint32_t)it.parts);
+    const int first = of(tiles - mine, b);  // the first tile of this level; level 0: those in front of the others, those without rows
+    it.tile = lo > 0 ? first + (int)t : (int)t < first ? (int)t : of(tiles, b) + (int)t - first;
+    return true;
+  }
+};
+
 template <int AH, int QB, int RW, bool EIGHT>
 __global__ void __launch_bounds__(64 * RW, AH <= 2 ? 2 : 1) chunk_kernel(ChunkArgs a) {
   constexpr int A = 64 * AH, R = 32 * QB, BM = R * RW, THREADS = 64 * RW;
@@ -51,12 +165,20 @@ __global__ void __launch_bounds__(64 * RW, AH <= 2 ? 2 : 1) chunk_kernel(ChunkAr
 
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int col = lane & 31, half = lane >> 5;
-  uint32_t head_, rank;
-  longest_first(blockIdx.x, a.by_heads, head_, rank);
-  const uint32_t head = settled(head_), b = settled(a.by_Zkv(head)), h = head - b * (uint32_t)a.Zkv;
-  const int group = (int)a.by_group.d, tokens = tokens_of(a, (int)b), rows = tokens * group;
-  const int row0 = (a.tiles - 1 - (int)rank) * BM;
-  if (row0 >= rows) return;
+  Item it{};
+  if (a.B <= kSorted) {
+    const Layout<BM> layout(a);
+    if (!layout.find(blockIdx.x, it)) return;
+    if (a.parts > 1 && blockIdx.x == 0 && tid < a.B) a.divided[tid] = (uint32_t)layout.parts;
+  } else {
+    uint32_t head, rank;
+    longest_first(blockIdx.x, a.by_heads, head, rank);
+    it.b = a.by_Zkv(head); it.h = head - it.b * (uint32_t)a.Zkv; it.tile = a.tiles - 1 - (int)rank; it.parts = 1;
+  }
+  const uint32_t b = settled(it.b), h = settled(it.h), head = b * (uint32_t)a.Zkv + h;
+  const int parts = (int)settled((uint32_t)it.parts), part = (int)settled((uint32_t)it.part);
+  const int group = (int)a.by_group.d, tokens = tokens_of(a, (int)b), rows = tokens * group, rows_all = a.T * group;
+  const int row0 = (int)settled((uint32_t)it.tile) * BM;
   const uint32_t len = length_of(a, (int)b);
   const int64_t slot0 = (int64_t)a.lengths[b] - tokens;
   // the first slot that a row does not see
@@ -65,10 +187,12 @@ __global__ void __launch_bounds__(64 * RW, AH <= 2 ? 2 : 1) chunk_kernel(ChunkAr
     return !a.causal ? len : n < 0 ? 0u : n < (int64_t)len ? (uint32_t)n : len;
   };
   const int last = (row0 + BM < rows ? row0 + BM : rows) - 1;
-  const uint32_t least = limit_of(row0), most = limit_of(last);
+  const bool some = row0 < rows;
+  if (!some && !a.pad) return;
+  const uint32_t least = some ? limit_of(row0) : 0u, most = some ? limit_of(last) : 0u;
   // this work-group's tiles of the walk
-  const uint32_t all = (most + kTileKeys - 1) / kTileKeys, per = (all + gridDim.y - 1) / gridDim.y;
-  uint32_t t = blockIdx.y * per;
+  const uint32_t all = (most + kTileKeys - 1) / kTileKeys, per = (all + (uint32_t)parts - 1) / (uint32_t)parts;
+  uint32_t t = (uint32_t)part * per;
   const uint32_t end = t + per < all ? t + per : all;
 
   // Q^T operand: lane (col, half) holds elements dk 16 + half 8 .. + 8 of its row
@@ -77,8 +201,8 @@ __global__ void __launch_bounds__(64 * RW, AH <= 2 ? 2 : 1) chunk_kernel(ChunkAr
 #pragma unroll
   for (int qb = 0; qb < QB; ++qb) {
     int row = row0 + wave * R + qb * 32 + col;
-    row = row < rows ? row : rows - 1;
-    lim[qb] = limit_of(row);
+    row = row < rows_all ? row : rows_all - 1;
+    lim[qb] = row < rows ? limit_of(row) : 0u;
     const int token = (int)a.by_group((uint32_t)row), z = (int)h * group + row - token * group;
     const uint16_t *q = a.Q + (int64_t)b * a.qs[0] + (int64_t)z * a.qs[1] + (int64_t)token * a.qs[2] + half * 8;
 #pragma unroll
@@ -351,21 +475,19 @@ __global__ void __launch_bounds__(64 * RW, AH <= 2 ? 2 : 1) chunk_kernel(ChunkAr
     stage(K1, V1, K0, V0);
   }
 
-  if (gridDim.y > 1) {  // this part's result
+  if (parts > 1) {  // this part's result
+    const int64_t place = ((int64_t)part * a.by_heads.d + head) * a.tiles + it.tile;
+    f32x4 *po = reinterpret_cast<f32x4 *>(a.part_o + (place * BM + wave * R) * A) + lane;
+    float2 *ml = reinterpret_cast<float2 *>(a.part_ml) + place * BM + wave * R + col;
 #pragma unroll
     for (int qb = 0; qb < QB; ++qb) {
       const float lt = xhalf_sum(l[qb]);
-      const int row = row0 + wave * R + qb * 32 + col;
-      if (row >= rows) continue;
-      const int64_t pr = ((int64_t)blockIdx.y * a.by_heads.d + head) * ((int64_t)a.T * group) + row;
-      float *po = a.part_o + pr * A + half * 4;
 #pragma unroll
       for (int db = 0; db < 2 * AH; ++db)
 #pragma unroll
         for (int g = 0; g < 4; ++g)
-          *reinterpret_cast<f32x4 *>(po + db * 32 + g * 8) =
-              f32x4{o[db][qb][g * 4 + 0], o[db][qb][g * 4 + 1], o[db][qb][g * 4 + 2], o[db][qb][g * 4 + 3]};
-      if (half == 0) *reinterpret_cast<float2 *>(a.part_ml + pr * 2) = make_float2(lt != 0.f ? mc[qb] : -INFINITY, lt);
+          po[((qb * 2 * AH + db) * 4 + g) * 64] = f32x4{o[db][qb][g * 4 + 0], o[db][qb][g * 4 + 1], o[db][qb][g * 4 + 2], o[db][qb][g * 4 + 3]};
+      if (half == 0) ml[qb * 32] = make_float2(lt != 0.f ? mc[qb] : -INFINITY, lt);
     }
     return;
   }
@@ -378,9 +500,9 @@ __global__ void __launch_bounds__(64 * RW, AH <= 2 ? 2 : 1) chunk_kernel(ChunkAr
     const float lt = xhalf_sum(l[qb]);
     inv[qb] = lt != 0.f ? 1.0f / lt : 0.f;
     const int row = row0 + wave * R + qb * 32 + col;
-    if (row < rows && half == 0) {
+    if (half == 0 && (row < rows || ((a.pad & 2) && row < rows_all))) {
       const int token = (int)a.by_group((uint32_t)row), z = (int)h * group + row - token * group;
-      a.LSE[((int64_t)b * a.Z + z) * a.T + token] = lt != 0.f ? (mc[qb] + __builtin_amdgcn_logf(lt)) * kLn2 : -INFINITY;
+      a.LSE[((int64_t)b * a.Z + z) * a.T + token] = lt != 0.f && row < rows ? (mc[qb] + __builtin_amdgcn_logf(lt)) * kLn2 : -INFINITY;
     }
   }
   unsigned char *ot = wave == 0 ? K0[0] : wave == 1 ? K1[0] : wave == 2 ? V0[0] : V1[0];
@@ -391,64 +513,82 @@ __global__ void __launch_bounds__(64 * RW, AH <= 2 ? 2 : 1) chunk_kernel(ChunkAr
 #pragma unroll
     for (int it = 0; it < R / 8; ++it) {
       const int r = it * 8 + (lane >> 3), cc = lane & 7, row = row0 + wave * R + r;
-      if (row < rows) {
+      if (row < rows || ((a.pad & 1) && row < rows_all)) {
         const int token = (int)a.by_group((uint32_t)row), z = (int)h * group + row - token * group;
         *reinterpret_cast<u32x4 *>(a.O + (int64_t)b * a.os[0] + (int64_t)z * a.os[1] + (int64_t)token * a.os[2] + ah * 64 + cc * 8) =
-            *reinterpret_cast<const u32x4 *>(ot + tile_off(r, cc));
+            row < rows ? *reinterpret_cast<const u32x4 *>(ot + tile_off(r, cc)) : u32x4{0, 0, 0, 0};
       }
     }
   }
 }
 
 // The parts of divided walks: with M the largest of a row's maxima, O = sum_s 2^(m_s - M) o_s / sum_s 2^(m_s - M) l_s.  A part that
-// saw no key of the row has m = -inf and is left out.  A / 4 lanes a row, 4 columns each; eight parts in flight.
-__global__ void __launch_bounds__(256) chunk_join_kernel(ChunkArgs a, FastDiv by_units, FastDiv by_rows, int A, int parts, uint32_t units) {
-  const uint32_t i = blockIdx.x * 256 + threadIdx.x;
-  if (i >= units) return;
-  const uint32_t flat = by_units(i), col = (i - flat * by_units.d) * 4, head = by_rows(flat), row = flat - head * by_rows.d;
+// saw no key of the row has m = -inf and is left out.  A work-group has 32 rows, a thread 16 bytes of every 32 columns as a lane of the
+// accumulators had them; the rows leave through LDS.
+template <int AH>
+__global__ void __launch_bounds__(256) chunk_join_kernel(ChunkArgs a, int BM) {
+  constexpr int A = 64 * AH;
+  __shared__ __attribute__((aligned(16))) uint16_t out[32][A + 8];
+  const uint32_t blocks = (uint32_t)(a.tiles * (BM / 32)), head = blockIdx.x / blocks, block = blockIdx.x - head * blocks;
   const uint32_t b = a.by_Zkv(head), h = head - b * (uint32_t)a.Zkv;
-  const int group = (int)a.by_group.d;
-  if ((int)row >= tokens_of(a, (int)b) * group) return;
-  const int64_t rows = (int64_t)a.by_heads.d * by_rows.d;
+  const int parts = (int)a.divided[b], group = (int)a.by_group.d, tokens = tokens_of(a, (int)b), have = tokens * group;
+  const int row0 = (int)block * 32, first = row0 / BM * BM;
+  if (parts <= 1 || first >= have) return;
+  // (a tile that sees nothing is not divided)
+  const int last = (first + BM < have ? first + BM : have) - 1;
+  if (a.causal && (int64_t)a.lengths[b] - tokens + (int)a.by_group((uint32_t)last) < 0) return;
+  const int lane = threadIdx.x & 63, g = threadIdx.x >> 6, col = lane & 31, half = lane >> 5, row = row0 + col;
+  const int64_t step = (int64_t)a.by_heads.d * a.tiles * BM, rows = (int64_t)head * a.tiles * BM + row0;
+  const f32x4 *po = reinterpret_cast<const f32x4 *>(a.part_o + rows * A) + g * 64 + lane;
+  const float2 *ml = reinterpret_cast<const float2 *>(a.part_ml) + rows + col;
   float M = -INFINITY, sum = 0.f;
-  f32x4 o = {0.f, 0.f, 0.f, 0.f};
-  for (int s0 = 0; s0 < parts; s0 += 8) {
-    float2 ml[8];
-    f32x4 x[8];
+  f32x4 o[2 * AH];
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      const int64_t pr = (int64_t)(s0 + k < parts ? s0 + k : s0) * rows + flat;
-      ml[k] = *reinterpret_cast<const float2 *>(a.part_ml + pr * 2);
-      x[k] = *reinterpret_cast<const f32x4 *>(a.part_o + pr * A + col);
-      if (s0 + k >= parts) ml[k].x = -INFINITY;
-    }
-    float top = M;
+  for (int db = 0; db < 2 * AH; ++db) o[db] = f32x4{0.f, 0.f, 0.f, 0.f};
+  for (int s = 0; s < parts; ++s) M = fmaxf(M, ml[s * step].x);
+#pragma unroll 2
+  for (int s = 0; s < parts; ++s) {
+    const float2 x = ml[s * step];
+    f32x4 y[2 * AH];
 #pragma unroll
-    for (int k = 0; k < 8; ++k) top = fmaxf(top, ml[k].x);
-    const float ref = top == -INFINITY ? 0.f : top, keep = __builtin_amdgcn_exp2f(M - ref);
-    M = top;
-    sum *= keep;
-    o *= keep;
+    for (int db = 0; db < 2 * AH; ++db) y[db] = po[s * step * (A / 4) + db * 256];
+    const float w = x.x > -INFINITY ? __builtin_amdgcn_exp2f(x.x - M) : 0.f;
+    sum = x.x > -INFINITY ? fmaf(w, x.y, sum) : sum;
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      if (ml[k].x == -INFINITY) continue;
-      const float w = __builtin_amdgcn_exp2f(ml[k].x - ref);
-      sum = fmaf(w, ml[k].y, sum);
-      o += x[k] * w;
+    for (int db = 0; db < 2 * AH; ++db)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[db][e] = x.x > -INFINITY ? fmaf(w, y[db][e], o[db][e]) : o[db][e];
+  }
+  const bool there = row < have;
+  const float inv = sum != 0.f ? 1.0f / sum : 0.f;
+#pragma unroll
+  for (int db = 0; db < 2 * AH; ++db)
+    *reinterpret_cast<u32x2 *>(&out[col][db * 32 + g * 8 + half * 4]) =
+        there ? u32x2{pack_bf16(o[db][0] * inv, o[db][1] * inv), pack_bf16(o[db][2] * inv, o[db][3] * inv)} : u32x2{0, 0};
+  const auto place = [&](int r, int &token, int &z) { token = (int)a.by_group((uint32_t)r); z = (int)h * group + r - token * group; };
+  const int all = a.T * group;
+  if (g == 0 && half == 0 && (there || ((a.pad & 2) && row < all))) {
+    int token, z;
+    place(row, token, z);
+    a.LSE[((int64_t)b * a.Z + z) * a.T + token] = there && sum != 0.f ? (M + __builtin_amdgcn_logf(sum)) * kLn2 : -INFINITY;
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < 32 * (A / 8); i += 256) {
+    const int r = i / (A / 8), c = i - r * (A / 8), y = row0 + r;
+    if (y < have || ((a.pad & 1) && y < all)) {
+      int token, z;
+      place(y, token, z);
+      *reinterpret_cast<u32x4 *>(a.O + (int64_t)b * a.os[0] + (int64_t)z * a.os[1] + (int64_t)token * a.os[2] + c * 8) =
+          *reinterpret_cast<const u32x4 *>(&out[r][c * 8]);
     }
   }
-  const int token = (int)a.by_group(row), z = (int)h * group + (int)row - token * group;
-  const float inv = sum != 0.f ? 1.0f / sum : 0.f;
-  *reinterpret_cast<u32x2 *>(a.O + (int64_t)b * a.os[0] + (int64_t)z * a.os[1] + (int64_t)token * a.os[2] + col) =
-      u32x2{pack_bf16(o[0] * inv, o[1] * inv), pack_bf16(o[2] * inv, o[3] * inv)};
-  if (col == 0) a.LSE[((int64_t)b * a.Z + z) * a.T + token] = sum != 0.f ? (M + __builtin_amdgcn_logf(sum)) * kLn2 : -INFINITY;
 }
 
 // How a call is laid over the chip, from what the host knows: the tokens and the table's width, not counts and lengths.
 struct ChunkPlan {
   bool few;         // by 16 or 32 rows at a time, from memory to the operands (rsa_cache.hip)
   int qb, rw;       // 32-row blocks of a wave, waves
-  int tiles, parts;
+  int tiles, parts; // row tiles of a key head; parts of a walk at most
 };
 ChunkPlan plan_of(const CacheDims &d, int T) {
   ChunkPlan p{};
@@ -458,16 +598,19 @@ ChunkPlan plan_of(const CacheDims &d, int T) {
   p.qb = 1; p.rw = rows <= 64 ? 2 : 4;
   if (d.A == 64 && heads * ((rows + 255) / 256) >= 512) p.qb = 2;
   p.tiles = (int)((rows + 32 * p.qb * p.rw - 1) / (32 * p.qb * p.rw));
-  // too few work-groups for two on every CU: their walks are divided, sixteen tiles and more a part
-  const int64_t wgs = heads * p.tiles, walk = ((int64_t)d.width * d.page + kTileKeys - 1) / kTileKeys;
-  const int64_t want = (2 * kCUs + wgs - 1) / wgs, most = walk / 16 < 32 ? walk / 16 : 32;
-  p.parts = (int)(want < most ? want : most > 1 ? most : 1);
+  // Parts.  None where the walks are short for a full chip, where one sequence alone fills two rounds of places (two work-groups on a
+  // CU), where the only one fills its rounds; else up to eight rounds of them, eight tiles and more a part, results within 512 MB.
+  const int64_t wgs = heads * p.tiles, walk = ((int64_t)d.width * d.page + kTileKeys - 1) / kTileKeys, places = 2 * kCUs;
+  const int64_t room = (512LL << 20) / (wgs * 32 * p.qb * p.rw * (d.A + 2) * 4), want = (8 * places + wgs - 1) / wgs;
+  const int64_t most = std::min<int64_t>(std::min<int64_t>(walk / 8, room), 32), rounds = (wgs + places - 1) / places;
+  const bool whole = d.B > kSorted || (wgs >= places && walk < 64) || wgs / d.B >= 2 * places || (d.B == 1 && wgs * 20 >= rounds * places * 17);
+  p.parts = whole ? 1 : (int)(want < most ? want : most > 1 ? most : 1);
   return p;
 }
 
 template <int AH, int QB, int RW>
 void launch_chunk(const ChunkArgs &a, const ChunkPlan &p, hipStream_t st) {
-  const dim3 grid((unsigned)(a.by_heads.d * p.tiles), (unsigned)p.parts);
+  const unsigned grid = (unsigned)(a.by_heads.d * p.tiles * p.parts);
   if (a.Ks) chunk_kernel<AH, QB, RW, true><<<grid, 64 * RW, 0, st>>>(a);
   else chunk_kernel<AH, QB, RW, false><<<grid, 64 * RW, 0, st>>>(a);
 }
@@ -479,39 +622,48 @@ void launch_chunk(const ChunkArgs &a, const ChunkPlan &p, hipStream_t st) {
   if (p.rw == 2) launch_chunk<AH, 1, 2>(a, p, st);
   else launch_chunk<AH, 1, 4>(a, p, st);
 }
+template <int AH>
+void launch_all(const ChunkArgs &a, const ChunkPlan &p, hipStream_t st) {
+  launch_chunk<AH>(a, p, st);
+  const int BM = 32 * p.qb * p.rw;
+  if (p.parts > 1) chunk_join_kernel<AH><<<(unsigned)(a.by_heads.d * a.tiles * (BM / 32)), 256, 0, st>>>(a, BM);
+}
 
+}  // namespace
+
+namespace {
+size_t part_rows(const CacheDims &d, const ChunkPlan &p) { return (size_t)p.parts * d.B * d.Zkv * p.tiles * 32 * p.qb * p.rw; }
 }  // namespace
 
 size_t chunk_workspace_bytes(const CacheDims &d, int T) {
   const ChunkPlan p = plan_of(d, T);
   if (p.few) return chunk_few_workspace_bytes(d, T);
-  return p.parts == 1 ? 0 : ((size_t)p.parts * d.B * d.Z * T * (d.A + 2) * 4 + 255) & ~(size_t)255;
+  return p.parts == 1 ? 0 : kSorted * sizeof(uint32_t) + part_rows(d, p) * (d.A + 2) * 4;
 }
 
-hipError_t cache_attend_chunk(const CacheDims &d, const CachePools &c, int T, int causal, const void *Q, const int32_t *table,
+hipError_t cache_attend_chunk(const CacheDims &d, const CachePools &c, int T, int causal, int pad, const void *Q, const int32_t *table,
                               const int32_t *lengths, const int32_t *counts, void *O, float *LSE, void *ws, hipStream_t st) {
   const ChunkPlan p = plan_of(d, T);
-  if (p.few) return chunk_few(d, c, T, causal, Q, table, lengths, counts, O, LSE, ws, st);
+  if (p.few) return chunk_few(d, c, T, causal, pad, Q, table, lengths, counts, O, LSE, ws, st);
   ChunkArgs a{};
   a.Q = static_cast<const uint16_t *>(Q); a.Kc = c.Kc; a.Vc = c.Vc; a.Ks = c.Ks; a.Vs = c.Vs;
   a.table = table; a.lengths = lengths; a.counts = counts; a.O = static_cast<uint16_t *>(O); a.LSE = LSE;
   for (int k = 0; k < 3; ++k) { a.qs[k] = d.qs[k]; a.os[k] = d.os[k]; }
   a.by_page = make_fast_div(d.page); a.by_group = make_fast_div(d.Z / d.Zkv);
   a.by_heads = make_fast_div((int64_t)d.B * d.Zkv); a.by_Zkv = make_fast_div(d.Zkv); a.by_row = make_fast_div(d.A / 16);
-  a.Z = d.Z; a.Zkv = d.Zkv; a.T = T; a.pages = d.pages; a.width = d.width; a.causal = causal; a.tiles = p.tiles;
+  a.B = d.B; a.Z = d.Z; a.Zkv = d.Zkv; a.T = T; a.pages = d.pages; a.width = d.width; a.causal = causal; a.pad = pad; a.tiles = p.tiles;
   a.cl2 = d.scale * kLog2e;
-  const int64_t rows = (int64_t)d.B * d.Z * T;
-  a.part_o = static_cast<float *>(ws);
-  a.part_ml = a.part_o + (p.parts > 1 ? p.parts * rows * d.A : 0);
-  switch (d.A) {
-    case 64: launch_chunk<1>(a, p, st); break;
-    case 128: launch_chunk<2>(a, p, st); break;
-    case 192: launch_chunk<3>(a, p, st); break;
-    default: launch_chunk<4>(a, p, st);
-  }
+  a.parts = p.parts;
   if (p.parts > 1) {
-    const uint32_t units = (uint32_t)(rows * (d.A / 4));
-    chunk_join_kernel<<<(units + 255) / 256, 256, 0, st>>>(a, make_fast_div(d.A / 4), make_fast_div((int64_t)T * (d.Z / d.Zkv)), d.A, p.parts, units);
+    a.divided = static_cast<uint32_t *>(ws);
+    a.part_o = static_cast<float *>(ws) + kSorted;
+    a.part_ml = a.part_o + part_rows(d, p) * d.A;
+  }
+  switch (d.A) {
+    case 64: launch_all<1>(a, p, st); break;
+    case 128: launch_all<2>(a, p, st); break;
+    case 192: launch_all<3>(a, p, st); break;
+    default: launch_all<4>(a, p, st);
   }
   return hipGetLastError();
 }

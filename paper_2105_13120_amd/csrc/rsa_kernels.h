@@ -150,17 +150,18 @@ struct CachePools {
 hipError_t cache_append8(const CacheDims &d, const CachePools &c, int T, int R, int adjacent, const float *inv_freq, const void *Q,
                          const void *K, const void *V, const int32_t *table, const int32_t *lengths, const int32_t *counts,
                          const int32_t *first, void *Qr, hipStream_t st);
-hipError_t cache_read(const CacheDims &d, const CachePools &c, int T, const int32_t *table, const int32_t *lengths, const int32_t *counts,
+hipError_t cache_read(const CacheDims &d, const CachePools &c, int T, int pad, const int32_t *table, const int32_t *lengths, const int32_t *counts,
                       void *K, void *V, hipStream_t st);
 size_t cache_workspace_bytes(const CacheDims &d);
 hipError_t cache_attend(const CacheDims &d, const CachePools &c, const void *Q, const int32_t *table, const int32_t *lengths, void *O,
                         float *LSE, void *ws, hipStream_t st);
 // Several new tokens per sequence: any number of rows, and by 16 or 32 rows of a key head at a time (fp32, and few rows)
 size_t chunk_workspace_bytes(const CacheDims &d, int T);
-hipError_t cache_attend_chunk(const CacheDims &d, const CachePools &c, int T, int causal, const void *Q, const int32_t *table,
+// (pad: bits, whether rows of tokens that are not there are written, of O (1) and LSE (2); of K and V likewise)
+hipError_t cache_attend_chunk(const CacheDims &d, const CachePools &c, int T, int causal, int pad, const void *Q, const int32_t *table,
                               const int32_t *lengths, const int32_t *counts, void *O, float *LSE, void *ws, hipStream_t st);
 size_t chunk_few_workspace_bytes(const CacheDims &d, int T);
-hipError_t chunk_few(const CacheDims &d, const CachePools &c, int T, int causal, const void *Q, const int32_t *table, const int32_t *lengths,
+hipError_t chunk_few(const CacheDims &d, const CachePools &c, int T, int causal, int pad, const void *Q, const int32_t *table, const int32_t *lengths,
                      const int32_t *counts, void *O, float *LSE, void *ws, hipStream_t st);
 hipError_t cache_join(const CacheDims &d, int N, const void *Op, const float *LSEp, void *O, float *LSE, hipStream_t st);
 

@@ -117,10 +117,10 @@ def lib():
         L.rsa_cache_join.argtypes = [cp, i] + [vp] * 5
         L.rsa_cache_append8.argtypes = [cp, i] + [vp] * 7 + [i, i] + [vp] * 7
         L.rsa_cache_attend8.argtypes = [cp] + [vp] * 10 + [sz, vp]
-        L.rsa_cache_read.argtypes = [cp, i] + [vp] * 10
+        L.rsa_cache_read.argtypes = [cp, i, i] + [vp] * 10
         L.rsa_cache_chunk_workspace_bytes.argtypes = [cp, i]
         L.rsa_cache_chunk_workspace_bytes.restype = sz
-        L.rsa_cache_attend_chunk.argtypes = [cp, i, i] + [vp] * 11 + [sz, vp]
+        L.rsa_cache_attend_chunk.argtypes = [cp, i, i, i] + [vp] * 11 + [sz, vp]
         _lib = L
     return _lib
 

@@ -173,6 +173,8 @@ def test_read(case, eight):
     assert got[0].data_ptr() == K.data_ptr()
     for x, pool in ((K, c.Kc), (V, c.Vc)):
         assert np.array_equal(f64(x), oracle.read(f64(pool), c.table, lengths, T, counts, np.full(K.shape, 5.0)))
+    half = rsa.cache_read(d, T, Kc, Vc, table, n, dev, V=torch.full_like(V, 5.0), **s)
+    assert np.array_equal(f64(half[0]), oracle.read(f64(c.Kc), c.table, lengths, T, counts)) and torch.equal(half[1], V)
     for x, pool in zip(rsa.cache_read(d, T, Kc, Vc, table, n, dev, **s), (c.Kc, c.Vc)):
         assert np.array_equal(f64(x), oracle.read(f64(pool), c.table, lengths, T, counts))
     # heads side by side

@@ -178,6 +178,7 @@ def test_long_and_many(dtype, Z, Zkv, A, page, T, lengths, counts, causal, eight
 
 @pytest.mark.parametrize("dtype,T", [("bf16", 6), ("bf16", 70), ("f32", 30)])
 def test_rows_of_no_token_are_left_as_they_are(dtype, T):
+    """... in results that are given, and those of rows that see nothing in new ones."""
     rng = np.random.default_rng(38)
     lengths, counts = [100, 30, 5], [T, 2, 0]
     c = Cache(rng, lengths, 2, 64, 16, 8, dtype)
@@ -185,10 +186,13 @@ def test_rows_of_no_token_are_left_as_they_are(dtype, T):
     O, LSE = torch.full(Q.shape, 3.0, dtype=Q.dtype, device="cuda"), torch.full((3, 4, T), 5.0, device="cuda")
     got = chunk(c, Q, counts, O=O, LSE=LSE)
     assert got[0].data_ptr() == O.data_ptr() and got[1].data_ptr() == LSE.data_ptr()
+    Q[1, :, 2:], Q[2] = float("nan"), float("inf")              # what lies in rows of no token does not count
     new = chunk(c, Q, counts)
+    half = chunk(c, Q, counts, O=torch.full_like(O, 3.0))
+    assert torch.equal(half[0], O) and torch.equal(half[1], new[1])
     for b, n in enumerate(counts):
         assert torch.equal(O[b, :, :n], new[0][b, :, :n]) and torch.equal(LSE[b, :, :n], new[1][b, :, :n])
-        assert (O[b, :, n:] == 3).all() and (LSE[b, :, n:] == 5).all()
+        assert (O[b, :, n:] == 3).all() and (LSE[b, :, n:] == 5).all() and torch.isfinite(LSE[b, :, :n]).all()
         assert (new[0][b, :, n:] == 0).all() and torch.isneginf(new[1][b, :, n:]).all()
 
 
@@ -335,3 +339,40 @@ def test_a_prompt_in_chunks_and_then_token_by_token(eight):
             compare_chunk(Dense, q.cpu(), (O, LSE), "bf16", counts)
         else:
             compare_chunk(Dense, q.cpu(), (O, LSE), "bf16", [1] * B)
+
+
+@pytest.mark.parametrize("seed", range(16))
+def test_uneven_sequences(seed):
+    """Random lengths and counts, empty sequences and tokens in front of slot 0 among them: the order in which work-groups take them, walks
+    that are divided and such that are not; more sequences than are put in order."""
+    r = np.random.default_rng(100 + seed)
+    B = [1, 2, 3, 5, 8, 13, 31, 32, 33, 40, 4, 6, 7, 1, 2, 64][seed]
+    Zkv, group, A = int(r.integers(1, 4)), int(r.choice([1, 2, 3, 8])), int(r.choice([64, 64, 128]))
+    T, most, page = int(r.integers(33, 400)), int(r.choice([200, 1500, 6000])), int(r.choice([5, 16, 64]))
+    causal, eight = bool(r.random() < 0.75), bool(r.random() < 0.5)
+    Z = Zkv * group
+    lengths = [int(most ** x) if r.random() > 0.15 else int(r.integers(-5, 5)) for x in r.random(B)]
+    lengths[0] = most
+    counts = [int(r.integers(-2, T + 3)) if r.random() < 0.6 else T for _ in range(B)]
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    W = -(-most // page)
+    K, V = (torch.randn(B * W, Zkv, page, A, generator=g, device="cuda").bfloat16() for _ in range(2))
+    pools, kw = (K, V), {}
+    if eight:
+        pools = [x.to(torch.float8_e4m3fn) for x in pools]
+        K, V = (x.float() for x in pools)
+        kw = {k: torch.full((B * W, Zkv, page), 127, dtype=torch.uint8, device="cuda") for k in ("Ks", "Vs")}
+    table = torch.randperm(B * W, generator=g, device="cuda").reshape(B, W).int()
+    Q = torch.randn(B, Z, T, A, generator=g, device="cuda").bfloat16()
+    d = rsa.make_cache_desc(pools[0], table, Z)
+    ws = torch.full((max(16, rsa.cache_chunk_workspace_bytes(d, T)),), 0xFF, dtype=torch.uint8, device="cuda")
+    O, LSE = rsa.cache_attend_chunk(d, Q, *pools, table, i32(lengths), i32(counts), causal, ws=ws, **kw)
+    mine = rsa.cache_attend_chunk(d, Q, *pools, table, i32(lengths), i32(counts), causal, torch.full_like(Q, 9.0), torch.full_like(LSE, 9.0), **kw)
+    there = torch.arange(T, device="cuda")[None] < i32(counts)[:, None]
+    assert torch.equal(mine[0], torch.where(there[:, None, :, None], O, 9.0)) and torch.equal(mine[1], torch.where(there[:, None], LSE, 9.0))
+    have = [max(0, min(c, T)) for c in counts]
+    rO, rLSE, PV = vectorised_chunk(Q, K, V, table, lengths, have, causal)
+    rel = 2 * (A + 4) * F32 * A ** 0.5 * 6 + 2.0 ** -21 + 2 * most * F32
+    within(O, f64(rO), f64((rel + 2.0 ** -8) * PV + STEP["bf16"] * rO.abs()), "O")
+    ref = f64(rLSE)
+    within(LSE, ref, rel + 4 * F32 * np.abs(np.where(np.isfinite(ref), ref, 0.0)), "LSE")
