@@ -338,8 +338,8 @@ struct Attend : ChunkRows<KIND, NQ> {
   typedef __attribute__((__vector_size__(kDw * sizeof(uint32_t)))) uint32_t VReg;
 
   // registers: tile, operands and accumulators, and about 60 more; of 512 a SIMD has room for these waves
-  static constexpr int kRegs = 4 * (KT * KP + NQ * KF + NQ * NB * VW) + VR * NB * kDw + 60 + (k8 ? 8 * NQ : 0) + (kRows ? 8 * NQ : 0);
-  static constexpr int kSimd = kRegs <= 128 ? 4 : kRegs <= 256 ? 2 : 1;
+  static constexpr int kRegs = 4 * (KT * KP + NQ * KF + NQ * NB * VW) + VR * NB * kDw + 60 + (k8 ? 8 * NQ : 0);
+  static constexpr int kSimd = kRows && A == 64 && NQ == 1 ? 3 : kRows && A == 256 ? 1 : kRegs <= (kRows ? 0 : 128) ? 4 : kRegs <= 256 ? 2 : 1;
   static constexpr int kWaves = 4, kTiles = kWaves, kUnit = kKeys * kTiles;
 
   struct Lds {
@@ -438,7 +438,7 @@ struct Attend : ChunkRows<KIND, NQ> {
                                                        (kRows ? (int64_t)token * args.qs[2] : 0));
       // (a 16-byte piece of e4m3 has the elements of two of a query's, side by side)
 #pragma unroll
-      for (int i = 0; i < KF; ++i) q[x][i] = in < rows_here() ? p[k8 ? 8 * (i >> 1) + 2 * g + (i & 1) : 4 * i + g] : u32x4{0, 0, 0, 0};
+      for (int i = 0; i < KF; ++i) q[x][i] = in < args.rows ? p[k8 ? 8 * (i >> 1) + 2 * g + (i & 1) : 4 * i + g] : u32x4{0, 0, 0, 0};
     }
   }
   // (of a slot that is not seen: 1, not what lies there)
@@ -714,19 +714,7 @@ struct Attend : ChunkRows<KIND, NQ> {
   __device__ __forceinline__ void walk(int b, int h, int tile, uint32_t len, uint32_t t, uint32_t end) {
     const int32_t *table = args.table + (int64_t)b * args.width;
     t += wave;
-    begin(b);
     load_q(b, h, tile);
-    if constexpr (kRows) {
-      const int first = tile * NQ * 16, last = (first + NQ * 16 < this->rows ? first + NQ * 16 : this->rows) - 1;
-      this->least = limit_of(first, len);
-      const uint32_t most = (limit_of(last < first ? first : last, len) + kKeys - 1) / kKeys;
-      end = first >= this->rows ? 0u : end < most ? end : most;
-#pragma unroll
-      for (int x = 0; x < NQ; ++x) {
-        const int in = first + x * 16 + n16;
-        this->lim[x] = in < this->rows ? limit_of(in, len) : 0u;
-      }
-    }
 #pragma unroll
     for (int x = 0; x < NQ; ++x) {
       m[x] = -INFINITY;
@@ -734,7 +722,10 @@ struct Attend : ChunkRows<KIND, NQ> {
 #pragma unroll
       for (int k = 0; k < NB * VW; ++k) acc[x][k] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
-    if (t >= end) return;
+    if (t >= end) {
+      if constexpr (kRows) begin(b);
+      return;
+    }
     Rows now = rows_of(page_of(table, len, t), len, h, t);
     load_k(now);
     __builtin_amdgcn_sched_barrier(0);  // (issued in the loop's order, which its waits count by)
@@ -742,6 +733,18 @@ struct Attend : ChunkRows<KIND, NQ> {
     __builtin_amdgcn_sched_barrier(0);
     load_v(now);
     __builtin_amdgcn_sched_barrier(0);
+    if constexpr (kRows) {  // (counts and lengths come while the first tile does; one that no row sees adds nothing)
+      begin(b);
+      const int first = tile * NQ * 16, last = (first + NQ * 16 < this->rows ? first + NQ * 16 : this->rows) - 1;
+      this->least = limit_of(first, len);
+      const uint32_t most = (limit_of(last < first ? first : last, len) + kKeys - 1) / kKeys;
+      end = end < most ? end : most;
+#pragma unroll
+      for (int x = 0; x < NQ; ++x) {
+        const int in = first + x * 16 + n16;
+        this->lim[x] = in < this->rows ? limit_of(in, len) : 0u;
+      }
+    }
     f32x4 s[NQ][KT];
     for (; t + kWaves < end; t += kWaves) {  // (the last tile behind the loop: in it, no wait counts loads that may be missing)
       scores(s, now.seen);

@@ -45,25 +45,40 @@ __device__ __forceinline__ CosSin turned_by(const CosSin *turn, double x) {
 __device__ __forceinline__ float element(const u32x4 &w, int k) {
   return __builtin_bit_cast(float, k & 1 ? w[k >> 1] & 0xffff0000u : w[k >> 1] << 16);
 }
-// The exponent that a row needs for its largest finite element `top`: 448 = 1.75 2^8
-__device__ __forceinline__ int exponent_for(double top) {
-  const uint64_t u = __builtin_bit_cast(uint64_t, top);
-  const int k = (int)(u >> 52) - 1023;  // (top >= 0)
-  return k - 8 + ((u & 0xfffffffffffffULL) > 0xc000000000000ULL ? 1 : 0);
-}
-// x as the fp32 number that rounds to e4m3 as x does: one that is not exact becomes the odd one of its two neighbours.
-__device__ __forceinline__ float to_odd(double x) {
-  const float f = (float)x;
-  const double back = (double)f;
-  uint32_t u = __builtin_bit_cast(uint32_t, f);
-  if (back != x) u = (u - (__builtin_fabs(back) > __builtin_fabs(x) ? 1u : 0u)) | 1u;
-  return __builtin_bit_cast(float, u);
-}
+// Numbers by their bits, which full-rate integer instructions take apart: conversions and comparisons of fp64 run at a fraction of that.
+struct Bits {
+  uint32_t lo, hi;
+  __device__ __forceinline__ explicit Bits(double x) {
+    const uint64_t u = __builtin_bit_cast(uint64_t, x);
+    lo = (uint32_t)u; hi = (uint32_t)(u >> 32);
+  }
+  __device__ __forceinline__ uint32_t size() const { return hi & 0x7fffffffu; }
+  __device__ __forceinline__ bool finite() const { return size() < 0x7ff00000u; }
+  // In the order of the numbers' sizes, 21 bits of each, any bit behind them counted upwards; 0 for what is infinite or NaN
+  __device__ __forceinline__ uint32_t rank() const { return finite() ? size() + (lo != 0) : 0u; }
+  // x 2^-e as the fp32 number that rounds to e4m3 as x 2^-e does: cut off, and odd where anything was
+  __device__ __forceinline__ float to_odd(int e) const {
+    const int t = (int)size() - ((896 + e) << 20);  // (below fp32's normal numbers: no e4m3 number but 0)
+    const uint32_t u = t < 0 ? 0u : ((uint32_t)t << 3 | lo >> 29) | ((lo & 0x1fffffffu) != 0);
+    return __builtin_bit_cast(float, finite() ? u | (hi & 0x80000000u) : 0x7fc00000u);
+  }
+};
+// The exponent that a row needs for its largest element's rank: 448 = 1.75 2^8
+__device__ __forceinline__ int exponent_for(uint32_t rank) { return (int)(rank >> 20) - 1023 - 8 + ((rank & 0xfffffu) > 0xc0000u ? 1 : 0); }
 __device__ __forceinline__ uint32_t four_e4m3(float a, float b, float c, float d) {
   const int lo = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
   return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, lo, true);
 }
-__device__ __forceinline__ double power_of_two(int e) { return __builtin_bit_cast(double, (uint64_t)(e + 1023) << 52); }
+// The exponent of a row of which the lane knows the largest rank of its part, and one after the other's
+template <int LANES> __device__ __forceinline__ int exponent_of_row(uint32_t rank) {
+#pragma unroll
+  for (int o = 1; o < LANES; o <<= 1) {
+    const uint32_t y = (uint32_t)__shfl_xor((int)rank, o);
+    rank = rank > y ? rank : y;
+  }
+  const int e = exponent_for(rank);
+  return e < -64 ? -64 : e > 120 ? 120 : e;
+}
 
 // How a row's pairs lie over the lanes' pieces of eight elements: no turn; neighbours; whole pieces that change places; anything else.
 enum Pairs { kNone, kNeighbours, kPieces, kAny };
@@ -79,11 +94,18 @@ __global__ __launch_bounds__(256, 4) void append8_kernel(Append8Args a) {
   if constexpr (PAIRS != kNone) sincospi((double)threadIdx.x * (2.0 / kTurn), &turn[threadIdx.x].s, &turn[threadIdx.x].c);
   if (threadIdx.x == 0) angles[kTokens * A / 2] = {1.0, -0.0};  // (-0 stays -0)
   const bool adjacent = PAIRS == kNeighbours || (PAIRS == kAny && a.ro.adjacent);
+  // Where a token's pairs are kept: such that the lanes of a row, each with its k-th, read one place after the other (in their own order, 16
+  // lanes met in eight banks)
+  const auto kept = [&](int p) __attribute__((always_inline)) {
+    if constexpr (PAIRS == kPieces) return (p & 7) * (half / 8) + (p >> 3);
+    if constexpr (PAIRS == kNeighbours) return (p & 3) * (half / 4) + (p >> 2);
+    return p;
+  };
   int pair[8];  // of element k
 #pragma unroll
   for (int k = 0; k < 8; ++k) {
     const int e = at + k;
-    pair[k] = e >= R ? kTokens * A / 2 : r * half + (adjacent ? e >> 1 : e < half ? e : e - half);
+    pair[k] = e >= R ? kTokens * A / 2 : r * half + kept(adjacent ? e >> 1 : e < half ? e : e - half);
   }
   const int from = (int)(threadIdx.x & 63) + (at >= R ? 0 : at < half ? half / 8 : -(half / 8));
   const uint32_t sign = adjacent ? 0x8000u : at < half ? 0x80008000u : 0u;  // of the partner of a pair's first element
@@ -107,88 +129,113 @@ __global__ __launch_bounds__(256, 4) void append8_kernel(Append8Args a) {
     }
     return w;
   };
-  // (the next head's row is on its way while one is turned)
-  const auto row_at = [&](const uint16_t *x, int z, int heads) __attribute__((always_inline)) {
-    return in && z < heads ? *reinterpret_cast<const u32x4 *>(x + at) : u32x4{0, 0, 0, 0};
+  // (the next heads' rows are on their way while some are turned, the first ones while the angles are worked out)
+  const auto row_at = [&](const uint16_t *x, bool any) __attribute__((always_inline)) {
+    return any ? *reinterpret_cast<const u32x4 *>(x) : u32x4{0, 0, 0, 0};
   };
   for (uint32_t item = blockIdx.x; item < tiles.items; item += gridDim.x) {
     const uint32_t tile = a.tok.by_split(item);
     tiles.begin(tile);
     const TokenPlace p = tiles.place(r);
     if (!__syncthreads_or(p.there)) continue;  // (the angles of the tile before are read)
-    for (int i = threadIdx.x; PAIRS != kNone && i < kTokens * half; i += 256) {
-      const uint32_t w = a.by_half(i);
-      const TokenPlace q = tiles.place(w);
-      if (q.there) angles[i] = turned_by(turn, half_turns_of(q.slot + (a.first ? a.first[q.b] : 0), a.ro.inv_freq[i - w * half]));
-    }
-    const int64_t row = p.row(a.tok, a.Zkv);
-    __syncthreads();
-    if (!p.there) continue;
     const int step = kHeads * (int)a.tok.by_split.d;
     // heads of Q, then of K, then of V, are dealt to the work-groups and rows in turn: this one's first of those from `base` on
     const int z0 = (int)(item - tile * a.tok.by_split.d) * kHeads + head0;
     const auto first_from = [&](int base) { return z0 >= base ? z0 - base : (base - z0 + step - 1) / step * step + z0 - base; };
-    const int64_t q = (int64_t)p.b * a.qs[0] + (int64_t)p.t * a.qs[2], kv = (int64_t)p.b * a.ks[0] + (int64_t)p.t * a.ks[2];
-
+    // (heads from here on, one after the other: additions instead of products of 64 bits)
+    const int64_t q = (int64_t)p.b * a.qs[0] + (int64_t)p.t * a.qs[2] + z0 * a.qs[1] + at, q_step = step * a.qs[1];
+    const int64_t kv = (int64_t)p.b * a.ks[0] + (int64_t)p.t * a.ks[2] + at, kv_step = step * a.ks[1];
+    constexpr int kAhead = 2;
+    const bool mine = p.there && in;
+    u32x4 x[kAhead], first_kv[2];
+#pragma unroll
+    for (int n = 0; n < kAhead; ++n) x[n] = row_at(a.Q + q + n * q_step, mine && z0 + n * step < a.Zq);
+#pragma unroll
+    for (int side = 0; side < 2; ++side) {
+      const int z = first_from(a.Zq + side * a.Zkv);
+      first_kv[side] = row_at((side ? a.V : a.K) + kv + z * a.ks[1], mine && z < a.Zkv);
+    }
+    for (int i = threadIdx.x; PAIRS != kNone && i < kTokens * half; i += 256) {
+      const uint32_t w = a.by_half(i);
+      const TokenPlace q = tiles.place(w);
+      if (q.there) angles[w * half + kept(i - w * half)] = turned_by(turn, half_turns_of(q.slot + (a.first ? a.first[q.b] : 0), a.ro.inv_freq[i - w * half]));
+    }
+    const int64_t row = p.row(a.tok, a.Zkv);
+    __syncthreads();
+    if (!p.there) continue;
     if (z0 < a.Zq) {
       float c[8], sn[8];
 #pragma unroll
       for (int k = 0; k < 8; ++k) { c[k] = (float)angles[pair[k]].c; sn[k] = (float)angles[pair[k]].s; }
-      u32x4 x = row_at(a.Q + q + z0 * a.qs[1], z0, a.Zq);
-      for (int z = z0; z < a.Zq; z += step) {
-        const int64_t off = q + z * a.qs[1];
-        const u32x4 next = row_at(a.Q + off + step * a.qs[1], z + step, a.Zq);
-        if constexpr (PAIRS != kNone) {
-          const u32x4 w = partners(x, a.Q + off);
-          u32x4 y;
+      const uint16_t *from_q = a.Q + q;
+      uint16_t *to_q = a.Qr + q;
+      for (int z = z0; z < a.Zq; z += kAhead * step) {
+        u32x4 next[kAhead];
+        const uint16_t *behind = from_q + kAhead * q_step;
 #pragma unroll
-          for (int k = 0; k < 4; ++k)
-            y[k] = pack_bf16(element(x, 2 * k) * c[2 * k] + element(w, 2 * k) * sn[2 * k],
-                             element(x, 2 * k + 1) * c[2 * k + 1] + element(w, 2 * k + 1) * sn[2 * k + 1]);
-          x = at < R ? y : x;
+        for (int n = 0; n < kAhead; ++n) next[n] = row_at(behind + n * q_step, in && z + (kAhead + n) * step < a.Zq);
+#pragma unroll
+        for (int n = 0; n < kAhead; ++n) {
+          if (z + n * step < a.Zq) {
+            if constexpr (PAIRS != kNone) {
+              const u32x4 w = partners(x[n], from_q - at);
+              u32x4 y;
+#pragma unroll
+              for (int k = 0; k < 4; ++k)
+                y[k] = pack_bf16(element(x[n], 2 * k) * c[2 * k] + element(w, 2 * k) * sn[2 * k],
+                                 element(x[n], 2 * k + 1) * c[2 * k + 1] + element(w, 2 * k + 1) * sn[2 * k + 1]);
+              x[n] = at < R ? y : x[n];
+            }
+            if (in) *reinterpret_cast<u32x4 *>(to_q) = x[n];
+          }
+          from_q += q_step;
+          to_q += q_step;
+          x[n] = next[n];
         }
-        if (in) *reinterpret_cast<u32x4 *>(a.Qr + off + at) = x;
-        x = next;
       }
     }
     if (row < 0) continue;
 #pragma unroll
     for (int side = 0; side < 2; ++side) {  // keys, values
-      const uint16_t *src = (side ? a.V : a.K) + kv;
       uint8_t *pool = side ? a.Vc : a.Kc, *scales = side ? a.Vs : a.Ks;
       int z = first_from(a.Zq + side * a.Zkv);
-      u32x4 x = row_at(src + z * a.ks[1], z, a.Zkv);
-      for (; z < a.Zkv; z += step) {
-        const u32x4 next = row_at(src + (z + step) * a.ks[1], z + step, a.Zkv);
-        double v[8], top = 0.0;
-        u32x4 w{};
-        if (side == 0 && PAIRS != kNone) w = partners(x, src + z * a.ks[1]);
+      const uint16_t *src = (side ? a.V : a.K) + kv + z * a.ks[1];
+      int64_t to = row + (int64_t)z * a.tok.by_page.d;
+      const int64_t to_step = (int64_t)step * a.tok.by_page.d;
+      u32x4 x = first_kv[side];
+      for (; z < a.Zkv; z += step, src += kv_step, to += to_step) {
+        const u32x4 next = row_at(src + kv_step, in && z + step < a.Zkv);
+        float f[8];
+        uint32_t top = 0;
+        int e;
+        if (side == 0 && PAIRS != kNone) {
+          double v[8];
+          const u32x4 w = partners(x, src - at);
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          v[k] = (double)element(x, k);
-          if (side == 0 && PAIRS != kNone) {
+          for (int k = 0; k < 8; ++k) {
             const CosSin t = angles[pair[k]];
+            v[k] = (double)element(x, k);
             v[k] = at + k < R ? v[k] * t.c + (double)element(w, k) * t.s : v[k];
+            const uint32_t n = Bits(v[k]).rank();
+            top = top > n ? top : n;
             if (k & 1) __builtin_amdgcn_sched_barrier(0);  // (all eight at once take 40 registers more)
           }
-          const double size = __builtin_fabs(v[k]);
-          top = size < __builtin_inf() ? __builtin_fmax(top, size) : top;
-        }
-        int e = exponent_for(top);
+          e = exponent_of_row<LANES>(top);
 #pragma unroll
-        for (int o = 1; o < LANES; o <<= 1) {
-          const int y = __shfl_xor(e, o);
-          e = e > y ? e : y;
-        }
-        e = e < -64 ? -64 : e > 120 ? 120 : e;
-        const double power = power_of_two(-e);
-        float f[8];
+          for (int k = 0; k < 8; ++k) f[k] = Bits(v[k]).to_odd(e);
+        } else {  // (bf16 numbers as they are: fp32 holds them times any power of two here)
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          f[k] = __builtin_fabs(v[k]) < __builtin_inf() ? to_odd(v[k] * power) : __builtin_nanf("");
-          __builtin_amdgcn_sched_barrier(0);
+          for (int k = 0; k < 8; ++k) {
+            const uint32_t u = __builtin_bit_cast(uint32_t, element(x, k)) & 0x7fffffffu;
+            top = u < 0x7f800000u && u > top ? u : top;
+          }
+          e = exponent_of_row<LANES>((top >> 3) + (896u << 20));
+#pragma unroll
+          for (int k = 0; k < 8; ++k) {
+            const float y = element(x, k);
+            f[k] = __builtin_fabsf(y) < INFINITY ? y * __builtin_bit_cast(float, (uint32_t)(127 - e) << 23) : __builtin_nanf("");
+          }
         }
-        const int64_t to = row + (int64_t)z * a.tok.by_page.d;
         if (in) *reinterpret_cast<u32x2 *>(pool + to * A + at) = u32x2{four_e4m3(f[0], f[1], f[2], f[3]), four_e4m3(f[4], f[5], f[6], f[7])};
         if (lane == 0) scales[to] = (uint8_t)(e + 127);
         x = next;

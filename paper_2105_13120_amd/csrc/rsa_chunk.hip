@@ -43,15 +43,16 @@ __device__ __forceinline__ int tokens_of(const ChunkArgs &a, int b) {
   const int n = a.counts ? a.counts[b] : a.T;
   return n < 0 ? 0 : n < a.T ? n : a.T;
 }
-__device__ __forceinline__ uint32_t length_of(const ChunkArgs &a, int b) {
-  const int n = a.lengths[b], most = a.width * (int)a.by_page.d;
-  return (uint32_t)(n < 0 ? 0 : n < most ? n : most);
+__device__ __forceinline__ uint32_t slots_of(const ChunkArgs &a, int length) {
+  const int most = a.width * (int)a.by_page.d;
+  return (uint32_t)(length < 0 ? 0 : length < most ? length : most);
 }
 
 // What a call's work-groups take: a row tile of a key head of a sequence and, where its walk is divided, one of its parts.
 struct Item {
   uint32_t b, h;
   int tile, part, parts;
+  int tokens, length;  // of the sequence: new tokens that are there, its entry of `lengths`
 };
 
 // Sequences of different lengths with different numbers of new tokens leave tiles without rows and walks of all lengths.  Up to
@@ -79,7 +80,7 @@ __device__ __forceinline__ uint32_t sum_lanes(uint32_t x) { return (uint32_t)__b
 template <int BM>
 struct Layout {
   const ChunkArgs &a;
-  int lane, tiles, most, slot0, parts;  // of the lane's sequence: row tiles that have any, tiles of its longest walk, its first token's slot
+  int lane, tokens, length, tiles, most, slot0, parts;  // of the lane's sequence, row tiles that have any, tiles of its longest walk, its first token's slot
   __device__ __forceinline__ static uint32_t walk_of(const ChunkArgs &a, int64_t slot0, uint32_t len, int token) {
     const int64_t n = slot0 + token + 1;
     const uint32_t see = !a.causal ? len : n < 0 ? 0u : n < (int64_t)len ? (uint32_t)n : len;
@@ -94,9 +95,10 @@ struct Layout {
   }
   __device__ __forceinline__ explicit Layout(const ChunkArgs &args) : a(args), lane(threadIdx.x & 63) {
     const bool in = lane < a.B;
-    const int tokens = in ? tokens_of(a, lane) : 0;
-    const uint32_t len = in ? length_of(a, lane) : 0u;
-    slot0 = len > 0 ? a.lengths[lane] - tokens : 0;  // (of a sequence with slots)
+    tokens = in ? tokens_of(a, lane) : 0;
+    length = in ? a.lengths[lane] : 0;
+    const uint32_t len = slots_of(a, length);
+    slot0 = len > 0 ? length - tokens : 0;  // (of a sequence with slots)
     const int rows = tokens * (int)a.by_group.d;
     tiles = (rows + BM - 1) / BM;
     most = tokens > 0 ? (int)walk_of(a, slot0, len, tokens - 1) : 0;
@@ -148,6 +150,7 @@ struct Layout {
     const int b = __builtin_ctzll(__ballot(r < s));
     const uint32_t j = r - (uint32_t)of((int)(s - n), b), k = a.by_Zkv(j);
     it.b = (uint32_t)b; it.h = j - k * (uint32_t)a.Zkv;
+    it.tokens = of(tokens, b); it.length = of(length, b);
     it.parts = lo > 0 ? of(parts, b) : 1;
     const uint32_t t = it.parts > 1 ? k / (uint32_t)it.parts : k;
     it.part = (int)(k - t * (uint32_t)it.parts);
@@ -158,7 +161,7 @@ struct Layout {
 };
 
 template <int AH, int QB, int RW, bool EIGHT>
-__global__ void __launch_bounds__(64 * RW, AH <= 2 ? 2 : 1) chunk_kernel(ChunkArgs a) {
+__global__ void __launch_bounds__(64 * RW, AH <= 2 || RW == 8 ? 2 : 1) chunk_kernel(ChunkArgs a) {
   constexpr int A = 64 * AH, R = 32 * QB, BM = R * RW, THREADS = 64 * RW;
   // (two buffers, each an object of its own, so that the compiler sees that loads into one miss the reads of the other)
   __shared__ __attribute__((aligned(16))) unsigned char K0[AH][kTileBytes], K1[AH][kTileBytes], V0[AH][kTileBytes], V1[AH][kTileBytes];
@@ -174,13 +177,15 @@ __global__ void __launch_bounds__(64 * RW, AH <= 2 ? 2 : 1) chunk_kernel(ChunkAr
     uint32_t head, rank;
     longest_first(blockIdx.x, a.by_heads, head, rank);
     it.b = a.by_Zkv(head); it.h = head - it.b * (uint32_t)a.Zkv; it.tile = a.tiles - 1 - (int)rank; it.parts = 1;
+    it.tokens = tokens_of(a, (int)it.b); it.length = a.lengths[it.b];
   }
   const uint32_t b = settled(it.b), h = settled(it.h), head = b * (uint32_t)a.Zkv + h;
   const int parts = (int)settled((uint32_t)it.parts), part = (int)settled((uint32_t)it.part);
-  const int group = (int)a.by_group.d, tokens = tokens_of(a, (int)b), rows = tokens * group, rows_all = a.T * group;
+  const int group = (int)a.by_group.d, tokens = (int)settled((uint32_t)it.tokens), rows = tokens * group, rows_all = a.T * group;
+  const int length = (int)settled((uint32_t)it.length);
   const int row0 = (int)settled((uint32_t)it.tile) * BM;
-  const uint32_t len = length_of(a, (int)b);
-  const int64_t slot0 = (int64_t)a.lengths[b] - tokens;
+  const uint32_t len = slots_of(a, length);
+  const int64_t slot0 = (int64_t)length - tokens;
   // the first slot that a row does not see
   const auto limit_of = [&](int row) -> uint32_t {
     const int64_t n = slot0 + (int)a.by_group((uint32_t)row) + 1;
@@ -227,54 +232,53 @@ __global__ void __launch_bounds__(64 * RW, AH <= 2 ? 2 : 1) chunk_kernel(ChunkAr
 
   // ---- tiles into LDS.  bf16: wave w moves pieces (w PER + j) 64 + lane of 16 bytes (see TileDMAT).  e4m3: thread i has pieces
   // i, i + THREADS, ..., of 16 elements each.
-  constexpr int PER = 8 / RW, P8 = 64 * (A / 16) / THREADS;
-  u32x4 kraw[EIGHT ? P8 : 1], vraw[EIGHT ? P8 : 1];
-  uint32_t kexp[EIGHT ? P8 : 1], vexp[EIGHT ? P8 : 1];
+  constexpr int PER = 8 / RW, P8 = (64 * (A / 16) + THREADS - 1) / THREADS;
+  constexpr bool kUneven = 64 * (A / 16) % THREADS != 0;  // (the last of some threads' pieces is not there: its row is beyond the tile's)
+  u32x4 raw[2][EIGHT ? P8 : 1];  // keys, values
+  uint32_t exps[2][EIGHT ? P8 : 1];
   const auto place8 = [&](int i, int &row, int &pc) {
     const uint32_t p = i * THREADS + tid;
     row = (int)a.by_row(p);
     pc = (int)p - row * (A / 16);
   };
-  const auto load = [&](const Rows &r, auto &Kn, auto &Vn) __attribute__((always_inline)) {
-    if constexpr (EIGHT) {
+  const auto load8 = [&](const Rows &r) __attribute__((always_inline)) {
 #pragma unroll
-      for (int i = 0; i < P8; ++i) {
-        int row, pc;
-        place8(i, row, pc);
-        const uint64_t from = __shfl(r.row, row);
-        kraw[i] = *reinterpret_cast<const u32x4 *>(static_cast<const uint8_t *>(a.Kc) + from * A + pc * 16);
-        vraw[i] = *reinterpret_cast<const u32x4 *>(static_cast<const uint8_t *>(a.Vc) + from * A + pc * 16);
-        kexp[i] = a.Ks[from];
-        vexp[i] = a.Vs[from];
-        if (!((r.seen >> row) & 1)) kexp[i] = vexp[i] = 127;  // (not what lies there)
-      }
-    } else {
+    for (int i = 0; i < P8; ++i) {
+      int row, pc;
+      place8(i, row, pc);
+      const uint64_t from = __shfl(r.row, row);
+      raw[0][i] = *reinterpret_cast<const u32x4 *>(static_cast<const uint8_t *>(a.Kc) + from * A + pc * 16);
+      raw[1][i] = *reinterpret_cast<const u32x4 *>(static_cast<const uint8_t *>(a.Vc) + from * A + pc * 16);
+      exps[0][i] = a.Ks[from];
+      exps[1][i] = a.Vs[from];
+    }
+  };
+  const auto store8 = [&](const Rows &r, auto &Kn, auto &Vn) __attribute__((always_inline)) {
 #pragma unroll
-      for (int j = 0; j < PER; ++j) {
-        const int row = (wave * PER + j) * 8 + (lane >> 3), cc = (lane & 7) ^ swz_rot(row);
-        const uint64_t off = (uint64_t)__shfl(r.row, row) * A + cc * 8;
+    for (int i = 0; i < P8; ++i) {
+      int row, pc;
+      place8(i, row, pc);
+      if (kUneven && i == P8 - 1 && row >= kTileKeys) continue;
+      const bool seen = (r.seen >> row) & 1;
 #pragma unroll
-        for (int ah = 0; ah < AH; ++ah) {
-          lds_dma16(static_cast<const uint16_t *>(a.Kc) + off + ah * 64, Kn[ah] + (wave * PER + j) * 1024);
-          lds_dma16(static_cast<const uint16_t *>(a.Vc) + off + ah * 64, Vn[ah] + (wave * PER + j) * 1024);
-        }
+      for (int side = 0; side < 2; ++side) {
+        const float power = __builtin_bit_cast(float, (seen ? exps[side][i] : 127u) << 23);  // (not what lies there)
+        const u32x4 &x = raw[side][i];
+        unsigned char *y = side ? Vn[pc >> 2] : Kn[pc >> 2];
+        *reinterpret_cast<u32x4 *>(y + tile_off(row, 2 * (pc & 3))) = widened8(x[0], x[1], power);
+        *reinterpret_cast<u32x4 *>(y + tile_off(row, 2 * (pc & 3) + 1)) = widened8(x[2], x[3], power);
       }
     }
   };
-  // what has come through registers
-  const auto store = [&](auto &Kn, auto &Vn) __attribute__((always_inline)) {
-    if constexpr (EIGHT) {
+  const auto load = [&](const Rows &r, auto &Kn, auto &Vn) __attribute__((always_inline)) {
 #pragma unroll
-      for (int i = 0; i < P8; ++i) {
-        int row, pc;
-        place8(i, row, pc);
-        const int at0 = tile_off(row, 2 * (pc & 3)), at1 = tile_off(row, 2 * (pc & 3) + 1);
-        const float kp = __builtin_bit_cast(float, kexp[i] << 23), vp = __builtin_bit_cast(float, vexp[i] << 23);
-        unsigned char *k = Kn[pc >> 2], *v = Vn[pc >> 2];
-        *reinterpret_cast<u32x4 *>(k + at0) = widened8(kraw[i][0], kraw[i][1], kp);
-        *reinterpret_cast<u32x4 *>(k + at1) = widened8(kraw[i][2], kraw[i][3], kp);
-        *reinterpret_cast<u32x4 *>(v + at0) = widened8(vraw[i][0], vraw[i][1], vp);
-        *reinterpret_cast<u32x4 *>(v + at1) = widened8(vraw[i][2], vraw[i][3], vp);
+    for (int j = 0; j < PER; ++j) {
+      const int row = (wave * PER + j) * 8 + (lane >> 3), cc = (lane & 7) ^ swz_rot(row);
+      const uint64_t off = (uint64_t)__shfl(r.row, row) * A + cc * 8;
+#pragma unroll
+      for (int ah = 0; ah < AH; ++ah) {
+        lds_dma16(static_cast<const uint16_t *>(a.Kc) + off + ah * 64, Kn[ah] + (wave * PER + j) * 1024);
+        lds_dma16(static_cast<const uint16_t *>(a.Vc) + off + ah * 64, Vn[ah] + (wave * PER + j) * 1024);
       }
     }
   };
@@ -295,9 +299,14 @@ __global__ void __launch_bounds__(64 * RW, AH <= 2 ? 2 : 1) chunk_kernel(ChunkAr
   int id = 0;
   if (t < end) {
     next = rows_of(page_of(t), t);
-    load(next, K0, V0);
-    id = page_of(t + 1);
-    store(K0, V0);
+    if constexpr (EIGHT) {
+      load8(next);
+      id = page_of(t + 1);
+      store8(next, K0, V0);
+    } else {
+      load(next, K0, V0);
+      id = page_of(t + 1);
+    }
   }
   wait_vmem();
   __syncthreads();
@@ -308,7 +317,11 @@ __global__ void __launch_bounds__(64 * RW, AH <= 2 ? 2 : 1) chunk_kernel(ChunkAr
     const bool more = t + 1 < end;
     if (more) {
       next = rows_of(id, t + 1);
-      load(next, Kn, Vn);
+      if constexpr (EIGHT) {
+        load8(next);
+      } else {
+        load(next, Kn, Vn);
+      }
       id = page_of(t + 2);
     }
     const uint32_t k0 = t * kTileKeys;
@@ -464,7 +477,7 @@ __global__ void __launch_bounds__(64 * RW, AH <= 2 ? 2 : 1) chunk_kernel(ChunkAr
 #pragma unroll
         for (int qb = 0; qb < QB; ++qb) o[db][qb] = mfma_32x32x16(va, pf[qb][kk], o[db][qb]);
       }
-    if (more) store(Kn, Vn);
+    if (EIGHT && more) store8(next, Kn, Vn);
     wait_vmem();
     __syncthreads();
     ++t;
@@ -505,7 +518,7 @@ __global__ void __launch_bounds__(64 * RW, AH <= 2 ? 2 : 1) chunk_kernel(ChunkAr
       a.LSE[((int64_t)b * a.Z + z) * a.T + token] = lt != 0.f && row < rows ? (mc[qb] + __builtin_amdgcn_logf(lt)) * kLn2 : -INFINITY;
     }
   }
-  unsigned char *ot = wave == 0 ? K0[0] : wave == 1 ? K1[0] : wave == 2 ? V0[0] : V1[0];
+  unsigned char *ot = ((wave & 3) == 0 ? K0[0] : (wave & 3) == 1 ? K1[0] : (wave & 3) == 2 ? V0[0] : V1[0]) + (wave >> 2) * 32 * 128;
 #pragma unroll
   for (int ah = 0; ah < AH; ++ah) {
 #pragma unroll
@@ -595,7 +608,7 @@ ChunkPlan plan_of(const CacheDims &d, int T) {
   const int64_t rows = (int64_t)T * (d.Z / d.Zkv), heads = (int64_t)d.B * d.Zkv;
   p.few = d.dtype != RSA_BF16 || rows <= 32;
   if (p.few) return p;
-  p.qb = 1; p.rw = rows <= 64 ? 2 : 4;
+  p.qb = 1; p.rw = rows <= 64 && d.A <= 128 ? 2 : rows > 128 && d.A == 192 ? 8 : 4;
   if (d.A == 64 && heads * ((rows + 255) / 256) >= 512) p.qb = 2;
   p.tiles = (int)((rows + 32 * p.qb * p.rw - 1) / (32 * p.qb * p.rw));
   // Parts.  None where the walks are short for a full chip, where one sequence alone fills two rounds of places (two work-groups on a
@@ -619,8 +632,13 @@ void launch_chunk(const ChunkArgs &a, const ChunkPlan &p, hipStream_t st) {
   if constexpr (AH == 1) {
     if (p.qb == 2) return launch_chunk<AH, 2, 4>(a, p, st);
   }
-  if (p.rw == 2) launch_chunk<AH, 1, 2>(a, p, st);
-  else launch_chunk<AH, 1, 4>(a, p, st);
+  if constexpr (AH <= 2) {
+    if (p.rw == 2) return launch_chunk<AH, 1, 2>(a, p, st);
+  }
+  if constexpr (AH == 3) {
+    if (p.rw == 8) return launch_chunk<AH, 1, 8>(a, p, st);
+  }
+  launch_chunk<AH, 1, 4>(a, p, st);
 }
 template <int AH>
 void launch_all(const ChunkArgs &a, const ChunkPlan &p, hipStream_t st) {
