@@ -77,7 +77,7 @@ __device__ __forceinline__ uint32_t scan_lanes(uint32_t x) {
   return x;
 }
 __device__ __forceinline__ uint32_t sum_lanes(uint32_t x) { return (uint32_t)__builtin_amdgcn_readlane((int)scan_lanes(x), 63); }
-template <int BM>
+template <int BM, int PLACES>
 struct Layout {
   const ChunkArgs &a;
   int lane, tokens, length, tiles, most, slot0, parts;  // of the lane's sequence, row tiles that have any, tiles of its longest walk, its first token's slot
@@ -120,8 +120,8 @@ struct Layout {
       all += t * 0.5f * (float)of(mean2, b);
       items += t * __builtin_ceilf((float)of(most, b) * share);
     }
-    constexpr float places = 2 * kCUs;
-    const float rounds = __builtin_ceilf(items / places), longest_one = items <= 0.5f * places ? 0.6f * (float)per : (float)per;
+    constexpr float places = PLACES;
+    const float rounds = __builtin_ceilf(items / places), longest_one = PLACES > kCUs && items <= kCUs ? 0.6f * (float)per : (float)per;
     const float walks = all > 0.85f * items * (float)per ? rounds * longest_one : fmaxf(longest_one, all / places + 0.2f * (float)per);
     float cost = walks + items / places * (q > 1 ? 6.f : 3.f) + (q > 1 ? 5.f : 0.f);
     if (q > a.parts) cost = INFINITY;
@@ -170,7 +170,7 @@ __global__ void __launch_bounds__(64 * RW, AH <= 2 || RW == 8 ? 2 : 1) chunk_ker
   const int col = lane & 31, half = lane >> 5;
   Item it{};
   if (a.B <= kSorted) {
-    const Layout<BM> layout(a);
+    const Layout<BM, (RW == 8 || AH > 2 ? kCUs : 2 * kCUs)> layout(a);
     if (!layout.find(blockIdx.x, it)) return;
     if (a.parts > 1 && blockIdx.x == 0 && tid < a.B) a.divided[tid] = (uint32_t)layout.parts;
   } else {
@@ -598,6 +598,11 @@ __global__ void __launch_bounds__(256) chunk_join_kernel(ChunkArgs a, int BM) {
 }
 
 // How a call is laid over the chip, from what the host knows: the tokens and the table's width, not counts and lengths.
+// Work-groups.  256 rows by eight waves read a tile from memory for twice the rows, but leave a CU to one work-group: heads of 192, whose four waves
+// would be alone on it too (2048 tokens of 16384 slots, 8 key heads, us: 1073 -> 747), and of 128 where these work-groups fill the chip twice, or
+// once with walks of about one length (the same 512 -> 501, 64k slots 2145 -> 1973, 8 x 512 of 8192 572 -> 541, in e4m3 578 -> 527; but 2048 of
+// 2048 57 -> 65, 512 of 8192 84 -> 97, 4 x 1024 of 1024, 16 key heads, 36 -> 43).  Heads of 64 take 64 rows a wave where these fill the chip (eight
+// waves of 32: 307 -> 341).
 struct ChunkPlan {
   bool few;         // by 16 or 32 rows at a time, from memory to the operands (rsa_cache.hip)
   int qb, rw;       // 32-row blocks of a wave, waves
@@ -608,12 +613,15 @@ ChunkPlan plan_of(const CacheDims &d, int T) {
   const int64_t rows = (int64_t)T * (d.Z / d.Zkv), heads = (int64_t)d.B * d.Zkv;
   p.few = d.dtype != RSA_BF16 || rows <= 32;
   if (p.few) return p;
-  p.qb = 1; p.rw = rows <= 64 && d.A <= 128 ? 2 : rows > 128 && d.A == 192 ? 8 : 4;
-  if (d.A == 64 && heads * ((rows + 255) / 256) >= 512) p.qb = 2;
+  p.qb = 1; const int64_t large = heads * ((rows + 255) / 256), slots = (int64_t)d.width * d.page;
+  p.rw = rows <= 64 && d.A <= 128 ? 2 : 4;
+  if (d.A == 192 ? rows > 128 : d.A == 128 && (large >= 512 || (large >= 256 && slots >= 4 * (int64_t)T))) p.rw = 8;
+  if (d.A == 64 && large >= 512) p.qb = 2;
   p.tiles = (int)((rows + 32 * p.qb * p.rw - 1) / (32 * p.qb * p.rw));
-  // Parts.  None where the walks are short for a full chip, where one sequence alone fills two rounds of places (two work-groups on a
+  // Parts.  None where the walks are short for a full chip, where one sequence alone fills two rounds of places (one or two work-groups on a
   // CU), where the only one fills its rounds; else up to eight rounds of them, eight tiles and more a part, results within 512 MB.
-  const int64_t wgs = heads * p.tiles, walk = ((int64_t)d.width * d.page + kTileKeys - 1) / kTileKeys, places = 2 * kCUs;
+  const int64_t wgs = heads * p.tiles, walk = (slots + kTileKeys - 1) / kTileKeys;
+  const int64_t places = p.rw == 8 || d.A > 128 ? kCUs : 2 * kCUs;
   const int64_t room = (512LL << 20) / (wgs * 32 * p.qb * p.rw * (d.A + 2) * 4), want = (8 * places + wgs - 1) / wgs;
   const int64_t most = std::min<int64_t>(std::min<int64_t>(walk / 8, room), 32), rounds = (wgs + places - 1) / places;
   const bool whole = d.B > kSorted || (wgs >= places && walk < 64) || wgs / d.B >= 2 * places || (d.B == 1 && wgs * 20 >= rounds * places * 17);
@@ -635,7 +643,7 @@ void launch_chunk(const ChunkArgs &a, const ChunkPlan &p, hipStream_t st) {
   if constexpr (AH <= 2) {
     if (p.rw == 2) return launch_chunk<AH, 1, 2>(a, p, st);
   }
-  if constexpr (AH == 3) {
+  if constexpr (AH == 2 || AH == 3) {
     if (p.rw == 8) return launch_chunk<AH, 1, 8>(a, p, st);
   }
   launch_chunk<AH, 1, 4>(a, p, st);
