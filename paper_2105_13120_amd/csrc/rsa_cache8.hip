@@ -253,10 +253,9 @@ struct ReadArgs {
   const uint8_t *Ks, *Vs;
   void *K, *V;
   int64_t ks[3];
-  int Zkv, pad, past;
+  int Zkv, pad;
 };
 // P: type of the pools (uint8_t: e4m3), T of the results
-// past: results of 16 MB and more are stored past the caches
 template <typename P, typename T, int A>
 __global__ __launch_bounds__(256) void read_kernel(ReadArgs a) {
   constexpr int W = 16 / sizeof(T), kUnits = A / W, LANES = kUnits <= 8 ? 8 : kUnits <= 16 ? 16 : kUnits <= 32 ? 32 : 64;
@@ -301,9 +300,7 @@ __global__ __launch_bounds__(256) void read_kernel(ReadArgs a) {
         if (!(write & (h < a.Zkv ? 1 : 2))) continue;
         if constexpr (sizeof(P) == 1) x[n] = widened8(x[n][0], x[n][1], __builtin_bit_cast(float, e[n] << 23));
         T *y = h < a.Zkv ? static_cast<T *>(a.K) + h * a.ks[1] : static_cast<T *>(a.V) + (h - a.Zkv) * a.ks[1];
-        u32x4 *place = reinterpret_cast<u32x4 *>(y + to);
-        if (a.past) __builtin_nontemporal_store(x[n], place);
-        else *place = x[n];
+        *reinterpret_cast<u32x4 *>(y + to) = x[n];
       }
     }
   }
@@ -377,7 +374,6 @@ hipError_t cache_read(const CacheDims &d, const CachePools &c, int T, int pad, c
   a.Kc = c.Kc; a.Vc = c.Vc; a.Ks = c.Ks; a.Vs = c.Vs; a.K = K; a.V = V;
   for (int k = 0; k < 3; ++k) a.ks[k] = d.ks[k];
   a.Zkv = d.Zkv; a.pad = pad;
-  a.past = (int64_t)d.B * d.Zkv * T * d.A * (d.dtype == RSA_BF16 ? 2 : 4) >= 16 << 20;
   if (c.Ks) launch_read<uint8_t, bf16_t>(d, a, T, st);
   else if (d.dtype == RSA_BF16) launch_read<bf16_t, bf16_t>(d, a, T, st);
   else launch_read<float, float>(d, a, T, st);
