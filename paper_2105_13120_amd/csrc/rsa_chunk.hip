@@ -87,9 +87,10 @@ struct Layout {
     return (see + kTileKeys - 1) / kTileKeys;
   }
   __device__ __forceinline__ static int of(int x, int b) { return __builtin_amdgcn_readlane(x, b); }
-  // Tiles of a sequence whose walks are longer than n.  (n < most: 64 n lies in front of the last token's slot, and nothing passes 32 bits.)
+  // Tiles of a sequence whose walks are longer than n.  (n < most: 64 n lies in front of the last token's slot, and nothing passes 32 bits;
+  // for others the product may, and is not used.)
   __device__ __forceinline__ static int longer(const ChunkArgs &a, int n, int tiles, int most, int slot0) {
-    const int x = n * kTileKeys - slot0;  // their last rows are of this token at least
+    const int x = (int)((uint32_t)n * kTileKeys - (uint32_t)slot0);  // their last rows are of this token at least
     const int first = a.causal && x > 0 ? (int)((uint32_t)x * a.by_group.d / BM) : 0;
     return n < most ? tiles - first : 0;
   }

@@ -111,6 +111,43 @@ def test_infinite_and_nan_tokens_reach_the_rows_that_see_them_alone(dtype, T, ki
     assert torch.equal(O, ref[0]) and torch.equal(LSE, ref[1])
 
 
+@pytest.mark.parametrize("A,B,Z,T,n", [(128, 8, 32, 512, 2048), (128, 2, 32, 1024, 4200), (192, 2, 2, 300, 700), (192, 1, 2, 200, 3000), (256, 1, 2, 90, 2000), (64, 16, 32, 1000, 1000)])
+@pytest.mark.parametrize("eight", [False, True])
+def test_infinite_and_nan_tokens_of_large_work_groups(A, B, Z, T, n, eight):
+    """The same where work-groups have 256 rows or walks are divided: one value of one slot NaN, another head's infinite, one key NaN."""
+    g = torch.Generator(device="cuda").manual_seed(45)
+    page, Zkv = 16, max(2, Z // 4)
+    W = -(-n // page)
+    Kc, Vc = (torch.randn(B * W, Zkv, page, A, generator=g, device="cuda").to(torch.float8_e4m3fn if eight else torch.bfloat16) for _ in range(2))
+    s = {k: torch.full((B * W, Zkv, page), 127, dtype=torch.uint8, device="cuda") for k in ("Ks", "Vs")} if eight else {}
+    table = torch.randperm(B * W, generator=g, device="cuda").reshape(B, W).int()
+    Q = torch.randn(B, Z, T, A, generator=g, device="cuda").bfloat16()
+    d, lengths = rsa.make_cache_desc(Kc, table, Z), i32([n] * B)
+    ref = rsa.cache_attend_chunk(d, Q, Kc, Vc, table, lengths, **s)
+    nan = float("nan")
+    group, b = Z // Zkv, B - 1
+    first = n - T
+
+    def put(pool, h, slot, col, value):
+        at = (int(table[b, slot // page]), h, slot % page, col)
+        if eight:
+            pool.view(torch.uint8)[at] = 127
+        else:
+            pool[at] = value
+    put(Vc, 0, first + T // 3, A - 3, nan)
+    put(Vc, 1, first + T // 2, 7, float("inf"))
+    put(Kc, 1, first + T - 5, 1, nan)
+    O, LSE = (x.clone() for x in rsa.cache_attend_chunk(d, Q, Kc, Vc, table, lengths, **s))
+    one, two = slice(0, group), slice(group, 2 * group)
+    assert O[b, one, T // 3:, A - 3].isnan().all() and O[b, two, T - 5:].isnan().all() and LSE[b, two, T - 5:].isnan().all()
+    seen = O[b, two, T // 2:T - 5, 7]
+    assert (seen.isnan() if eight else torch.isposinf(seen)).all()
+    O[b, one, T // 3:, A - 3] = ref[0][b, one, T // 3:, A - 3]
+    O[b, two, T // 2:, 7] = ref[0][b, two, T // 2:, 7]
+    O[b, two, T - 5:], LSE[b, two, T - 5:] = ref[0][b, two, T - 5:], ref[1][b, two, T - 5:]
+    assert torch.equal(O, ref[0]) and torch.equal(LSE, ref[1])
+
+
 @pytest.mark.parametrize("T", [6, 70])
 @pytest.mark.parametrize("scale,spread", [(0.3, 1.0), (0.0, 8.0), (0.01, 1.0)])
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
@@ -145,6 +182,10 @@ def test_scores_that_grow_by_large_steps(Z, T):
     ("bf16", 6, 2, 256, 32, 200, [3000, 222], None, True, False), ("bf16", 6, 2, 256, 32, 200, [3000, 222], [200, 99], False, True),
     ("bf16", 5, 5, 192, 16, 130, [3001, 130], None, False, False), ("bf16", 5, 5, 192, 16, 130, [3001, 130], None, True, True),
     ("bf16", 3, 1, 192, 16, 20, [6001], None, True, True), ("bf16", 9, 9, 64, 16, 40, [7000], None, True, True),
+    ("bf16", 16, 4, 128, 16, 1024, [4096, 2100, 1024, 3000], [1024, 500, 1024, 7], True, False),  # heads of 128 by 256 rows
+    ("bf16", 32, 8, 128, 16, 520, [4500], None, True, True), ("bf16", 32, 8, 128, 16, 520, [4500, 600, 2000, 1], [520, 520, 0, 1], False, True),
+    ("bf16", 8, 8, 128, 16, 500, [2000 + 31 * b for b in range(17)], None, True, False),   # ... one tile and a part of one, divided
+    ("bf16", 4, 2, 192, 16, 300, [2000, 400], [300, 299], True, False),
     ("f32", 6, 3, 64, 24, 300, [2000, 300], None, True, False), ("f32", 20, 1, 128, 16, 5, [6000] * 3, None, True, False),
     ("f32", 4, 2, 256, 16, 100, [3000], [77], True, False), ("bf16", 2, 1, 64, 16, 8, [50 + 3 * b for b in range(700)], None, True, False)])
 def test_long_and_many(dtype, Z, Zkv, A, page, T, lengths, counts, causal, eight):
@@ -341,12 +382,12 @@ def test_a_prompt_in_chunks_and_then_token_by_token(eight):
             compare_chunk(Dense, q.cpu(), (O, LSE), "bf16", [1] * B)
 
 
-@pytest.mark.parametrize("seed", range(16))
+@pytest.mark.parametrize("seed", range(18))
 def test_uneven_sequences(seed):
     """Random lengths and counts, empty sequences and tokens in front of slot 0 among them: the order in which work-groups take them, walks
     that are divided and such that are not; more sequences than are put in order."""
     r = np.random.default_rng(100 + seed)
-    B = [1, 2, 3, 5, 8, 13, 31, 32, 33, 40, 4, 6, 7, 1, 2, 64][seed]
+    B = [1, 2, 3, 5, 8, 13, 31, 32, 33, 70, 4, 6, 7, 1, 2, 64, 65, 130][seed]
     Zkv, group, A = int(r.integers(1, 4)), int(r.choice([1, 2, 3, 8])), int(r.choice([64, 64, 128]))
     T, most, page = int(r.integers(33, 400)), int(r.choice([200, 1500, 6000])), int(r.choice([5, 16, 64]))
     causal, eight = bool(r.random() < 0.75), bool(r.random() < 0.5)
