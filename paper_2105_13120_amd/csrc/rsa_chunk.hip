@@ -163,12 +163,22 @@ struct Layout {
 
 template <int AH, int QB, int RW, bool EIGHT>
 __global__ void __launch_bounds__(64 * RW, AH <= 2 || RW == 8 ? 2 : 1) chunk_kernel(ChunkArgs a) {
-  constexpr int A = 64 * AH, R = 32 * QB, BM = R * RW, THREADS = 64 * RW;
+  constexpr int A = 64 * AH, R = 32 * QB, BM = R * RW, THREADS = 64 * RW, KB = RW == 8 && (AH == 4 || (AH == 3 && EIGHT)) ? 1 : 2;
+  // Long heads' pools in e4m3 wait in LDS (K1, V1) as they are, since registers have no room for them, and are widened into K0 and V0 when their turn
+  // comes (2048 tokens of 16384 slots, us: heads of 192 963 -> 764, of 256 1872 -> 1197)
+  constexpr bool RAW = EIGHT && RW == 8 && AH > 2;
   // (two buffers, each an object of its own, so that the compiler sees that loads into one miss the reads of the other)
   __shared__ __attribute__((aligned(16))) unsigned char K0[AH][kTileBytes], K1[AH][kTileBytes], V0[AH][kTileBytes], V1[AH][kTileBytes];
 
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int col = lane & 31, half = lane >> 5;
+  // The lane as a number of its own, from which a tile's addresses are worked out anew where registers are scarce (kept over the walk they
+  // would be spilled, and a reload waits for the next tile's loads: heads of 256, 2048 tokens of 16384 slots 1117 -> 1083 us, 1024 of 1024 99 -> 85)
+  const auto anew = [&]() __attribute__((always_inline)) {
+    int l = lane;
+    if constexpr (KB == 1) asm volatile("" : "+v"(l));
+    return l;
+  };
   Item it{};
   if (a.B <= kSorted) {
     const Layout<BM, (RW == 8 || AH > 2 ? kCUs : 2 * kCUs)> layout(a);
@@ -238,7 +248,7 @@ __global__ void __launch_bounds__(64 * RW, AH <= 2 || RW == 8 ? 2 : 1) chunk_ker
   u32x4 raw[2][EIGHT ? P8 : 1];  // keys, values
   uint32_t exps[2][EIGHT ? P8 : 1];
   const auto place8 = [&](int i, int &row, int &pc) {
-    const uint32_t p = i * THREADS + tid;
+    const uint32_t p = i * THREADS + wave * 64 + anew();
     row = (int)a.by_row(p);
     pc = (int)p - row * (A / 16);
   };
@@ -254,6 +264,20 @@ __global__ void __launch_bounds__(64 * RW, AH <= 2 || RW == 8 ? 2 : 1) chunk_ker
       exps[1][i] = a.Vs[from];
     }
   };
+  const auto piece8 = [&](int i, int side) { return (side ? &V1[0][0] : &K1[0][0]) + (i * THREADS + wave * 64) * 16; };  // of the wave's first lane
+  const auto load_raw = [&](const Rows &r) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < P8; ++i) {
+      int row, pc;
+      place8(i, row, pc);
+      const uint64_t from = __shfl(r.row, row);
+      if (kUneven && i * THREADS + wave * 64 >= 64 * (A / 16)) break;  // (whole waves)
+      lds_dma16(static_cast<const uint8_t *>(a.Kc) + from * A + pc * 16, piece8(i, 0));
+      lds_dma16(static_cast<const uint8_t *>(a.Vc) + from * A + pc * 16, piece8(i, 1));
+      exps[0][i] = a.Ks[from];
+      exps[1][i] = a.Vs[from];
+    }
+  };
   const auto store8 = [&](const Rows &r, auto &Kn, auto &Vn) __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < P8; ++i) {
@@ -264,7 +288,7 @@ __global__ void __launch_bounds__(64 * RW, AH <= 2 || RW == 8 ? 2 : 1) chunk_ker
 #pragma unroll
       for (int side = 0; side < 2; ++side) {
         const float power = __builtin_bit_cast(float, (seen ? exps[side][i] : 127u) << 23);  // (not what lies there)
-        const u32x4 &x = raw[side][i];
+        const u32x4 x = RAW ? reinterpret_cast<const u32x4 *>(piece8(i, side))[lane] : raw[side][i];
         unsigned char *y = side ? Vn[pc >> 2] : Kn[pc >> 2];
         *reinterpret_cast<u32x4 *>(y + tile_off(row, 2 * (pc & 3))) = widened8(x[0], x[1], power);
         *reinterpret_cast<u32x4 *>(y + tile_off(row, 2 * (pc & 3) + 1)) = widened8(x[2], x[3], power);
@@ -272,6 +296,7 @@ __global__ void __launch_bounds__(64 * RW, AH <= 2 || RW == 8 ? 2 : 1) chunk_ker
     }
   };
   const auto load = [&](const Rows &r, auto &Kn, auto &Vn) __attribute__((always_inline)) {
+    const int lane = anew();
 #pragma unroll
     for (int j = 0; j < PER; ++j) {
       const int row = (wave * PER + j) * 8 + (lane >> 3), cc = (lane & 7) ^ swz_rot(row);
@@ -294,13 +319,14 @@ __global__ void __launch_bounds__(64 * RW, AH <= 2 || RW == 8 ? 2 : 1) chunk_ker
 #pragma unroll
       for (int v = 0; v < 16; ++v) o[db][qb][v] = 0.f;
   }
-  const TileLanes tl(lane);
-
   Rows now{0, 0}, next{0, 0};
   int id = 0;
   if (t < end) {
     next = rows_of(page_of(t), t);
-    if constexpr (EIGHT) {
+    if constexpr (RAW) {
+      load_raw(next);
+      id = page_of(t + 1);
+    } else if constexpr (EIGHT) {
       load8(next);
       id = page_of(t + 1);
       store8(next, K0, V0);
@@ -314,11 +340,18 @@ __global__ void __launch_bounds__(64 * RW, AH <= 2 || RW == 8 ? 2 : 1) chunk_ker
 
   // one tile: start the loads of the next one into (Kn, Vn), compute on (Kt, Vt)
   const auto stage = [&](auto &Kt, auto &Vt, auto &Kn, auto &Vn) __attribute__((always_inline)) {
+    const TileLanes tl(anew());
     now = next;
     const bool more = t + 1 < end;
+    if constexpr (RAW) {  // (a lane reads what it has asked for itself)
+      store8(now, Kt, Vt);
+      __syncthreads();
+    }
     if (more) {
       next = rows_of(id, t + 1);
-      if constexpr (EIGHT) {
+      if constexpr (RAW) {
+        load_raw(next);
+      } else if constexpr (EIGHT) {
         load8(next);
       } else {
         load(next, Kn, Vn);
@@ -332,7 +365,7 @@ __global__ void __launch_bounds__(64 * RW, AH <= 2 || RW == 8 ? 2 : 1) chunk_ker
       bool special = false;
 #pragma unroll
       for (int i = 0; i < 8 * AH / RW; ++i) {
-        const int p = i * THREADS + tid, row = (p >> 3) & 63, ah = p >> 9;
+        const int p = i * THREADS + wave * 64 + anew(), row = (p >> 3) & 63, ah = p >> 9;
         u32x4 *x = reinterpret_cast<u32x4 *>(Vt[ah] + row * 128 + (p & 7) * 16);
         if ((now.seen >> row) & 1) {
           const u32x4 w = *x;
@@ -381,7 +414,7 @@ __global__ void __launch_bounds__(64 * RW, AH <= 2 || RW == 8 ? 2 : 1) chunk_ker
         // ... and they are 0 from here on
 #pragma unroll
         for (int i = 0; i < 8 * AH / RW; ++i) {
-          const int p = i * THREADS + tid, row = (p >> 3) & 63, ah = p >> 9;
+          const int p = i * THREADS + wave * 64 + anew(), row = (p >> 3) & 63, ah = p >> 9;
           u32x4 *x = reinterpret_cast<u32x4 *>(Vt[ah] + row * 128 + (p & 7) * 16);
           u32x4 w = *x;
 #pragma unroll
@@ -393,100 +426,104 @@ __global__ void __launch_bounds__(64 * RW, AH <= 2 || RW == 8 ? 2 : 1) chunk_ker
       }
     }
 
-    // ---- S^T = K Q^T
-    f32x16 s[2][QB];
-    float tm[QB];
+    // ---- by blocks of 32 keys: both at once or, where the accumulators leave no room for both's scores, one after the other
 #pragma unroll
-    for (int kb = 0; kb < 2; ++kb) {
-      bf16x8 ka[4 * AH];
+    for (int k1 = 0; k1 < 2; k1 += KB) {
+      // ---- S^T = K Q^T
+      f32x16 s[KB][QB];
+      float tm[QB];
 #pragma unroll
-      for (int dk = 0; dk < 4 * AH; ++dk) ka[dk] = tl.read_rows(Kt[dk >> 2], kb * 32, dk & 3);
+      for (int kb = 0; kb < KB; ++kb) {
+        bf16x8 ka[4 * AH];
 #pragma unroll
-      for (int qb = 0; qb < QB; ++qb) {
+        for (int dk = 0; dk < 4 * AH; ++dk) ka[dk] = tl.read_rows(Kt[dk >> 2], (k1 + kb) * 32, dk & 3);
 #pragma unroll
-        for (int v = 0; v < 16; ++v) s[kb][qb][v] = 0.f;
+        for (int qb = 0; qb < QB; ++qb) {
 #pragma unroll
-        for (int dk = 0; dk < 4 * AH; ++dk) s[kb][qb] = mfma_32x32x16(ka[dk], qreg[qb][dk], s[kb][qb]);
-      }
-    }
-    if (edge) {
+          for (int v = 0; v < 16; ++v) s[kb][qb][v] = 0.f;
 #pragma unroll
-      for (int qb = 0; qb < QB; ++qb) {
-        const int n = (int)lim[qb] - (int)k0;  // (slots are below 2^31)
-#pragma unroll
-        for (int kb = 0; kb < 2; ++kb) {
-          const uint32_t seen = ((uint32_t)(now.seen >> (kb * 32)) & low_bits(n - kb * 32)) >> (half * 4);
-#pragma unroll
-          for (int v = 0; v < 16; ++v) s[kb][qb][v] = keep_bit(s[kb][qb][v], seen, (v >> 2) * 8 + (v & 3));
+          for (int dk = 0; dk < 4 * AH; ++dk) s[kb][qb] = mfma_32x32x16(ka[dk], qreg[qb][dk], s[kb][qb]);
         }
       }
-    }
+      if (edge) {
 #pragma unroll
-    for (int qb = 0; qb < QB; ++qb) {
-      float x = s[0][qb][0];
+        for (int qb = 0; qb < QB; ++qb) {
+          const int n = (int)lim[qb] - (int)k0;  // (slots are below 2^31)
 #pragma unroll
-      for (int v = 1; v < 16; ++v) x = fmaxf(x, s[0][qb][v]);
+          for (int kb = 0; kb < KB; ++kb) {
+            const uint32_t seen = ((uint32_t)(now.seen >> ((k1 + kb) * 32)) & low_bits(n - (k1 + kb) * 32)) >> (half * 4);
 #pragma unroll
-      for (int v = 0; v < 16; ++v) x = fmaxf(x, s[1][qb][v]);
-      tm[qb] = xhalf_max(x);
-    }
-    // ---- the accumulators are rescaled only when some row's maximum grew by more than 2^8 (exact: l and O share the stale one)
-    bool need = false;
-#pragma unroll
-    for (int qb = 0; qb < QB; ++qb) need |= (tm[qb] - m[qb]) * a.cl2 > 8.0f;
-    if (__builtin_amdgcn_ballot_w64(need) != 0) {
+            for (int v = 0; v < 16; ++v) s[kb][qb][v] = keep_bit(s[kb][qb][v], seen, (v >> 2) * 8 + (v & 3));
+          }
+        }
+      }
 #pragma unroll
       for (int qb = 0; qb < QB; ++qb) {
-        // (a row that has seen no key yet keeps mc = 0)
-        const float mn = fmaxf(m[qb], tm[qb]);
-        const bool any = mn > -INFINITY;
-        const float alpha = any ? __builtin_amdgcn_exp2f((m[qb] - mn) * a.cl2) : 1.0f;
-        m[qb] = mn;
-        mc[qb] = any ? mn * a.cl2 : 0.f;
-        l[qb] *= alpha;
+        float x = s[0][qb][0];
 #pragma unroll
-        for (int db = 0; db < 2 * AH; ++db)
-#pragma unroll
-          for (int v = 0; v < 16; ++v) o[db][qb][v] *= alpha;
+        for (int i = 1; i < 16 * KB; ++i) x = fmaxf(x, s[i >> 4][qb][i & 15]);
+        tm[qb] = xhalf_max(x);
       }
+      // ---- the accumulators are rescaled only when some row's maximum grew by more than 2^8 (exact: l and O share the stale one)
+      bool need = false;
+#pragma unroll
+      for (int qb = 0; qb < QB; ++qb) need |= (tm[qb] - m[qb]) * a.cl2 > 8.0f;
+      if (__builtin_amdgcn_ballot_w64(need) != 0) {
+#pragma unroll
+        for (int qb = 0; qb < QB; ++qb) {
+          // (a row that has seen no key yet keeps mc = 0)
+          const float mn = fmaxf(m[qb], tm[qb]);
+          const bool any = mn > -INFINITY;
+          const float alpha = any ? __builtin_amdgcn_exp2f((m[qb] - mn) * a.cl2) : 1.0f;
+          m[qb] = mn;
+          mc[qb] = any ? mn * a.cl2 : 0.f;
+          l[qb] *= alpha;
+#pragma unroll
+          for (int db = 0; db < 2 * AH; ++db)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) o[db][qb][v] *= alpha;
+        }
+      }
+      // ---- P^T = exp2(S^T cl2 - m cl2), packed to bf16 as the B operand
+      bf16x8 pf[QB][2 * KB];
+#pragma unroll
+      for (int qb = 0; qb < QB; ++qb)
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb) {
+          float p[16];
+#pragma unroll
+          for (int v = 0; v < 16; ++v) {
+            p[v] = __builtin_amdgcn_exp2f(fmaf(s[kb][qb][v], a.cl2, -mc[qb]));
+            l[qb] += p[v];
+          }
+#pragma unroll
+          for (int u = 0; u < 2; ++u) {
+            const u32x4 w = {pack_bf16(p[u * 8 + 0], p[u * 8 + 1]), pack_bf16(p[u * 8 + 2], p[u * 8 + 3]),
+                             pack_bf16(p[u * 8 + 4], p[u * 8 + 5]), pack_bf16(p[u * 8 + 6], p[u * 8 + 7])};
+            pf[qb][kb * 2 + u] = __builtin_bit_cast(bf16x8, w);
+          }
+        }
+      // ---- O^T += V^T P^T
+#pragma unroll
+      for (int db = 0; db < 2 * AH; ++db)
+#pragma unroll
+        for (int kk = 0; kk < 2 * KB; ++kk) {
+          const bf16x8 va = tl.read_cols(Vt[db >> 1], (k1 * 2 + kk) * 16, db & 1);
+#pragma unroll
+          for (int qb = 0; qb < QB; ++qb) o[db][qb] = mfma_32x32x16(va, pf[qb][kk], o[db][qb]);
+        }
     }
-    // ---- P^T = exp2(S^T cl2 - m cl2), packed to bf16 as the B operand
-    bf16x8 pf[QB][4];
-#pragma unroll
-    for (int qb = 0; qb < QB; ++qb)
-#pragma unroll
-      for (int kb = 0; kb < 2; ++kb) {
-        float p[16];
-#pragma unroll
-        for (int v = 0; v < 16; ++v) {
-          p[v] = __builtin_amdgcn_exp2f(fmaf(s[kb][qb][v], a.cl2, -mc[qb]));
-          l[qb] += p[v];
-        }
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-          const u32x4 w = {pack_bf16(p[u * 8 + 0], p[u * 8 + 1]), pack_bf16(p[u * 8 + 2], p[u * 8 + 3]),
-                           pack_bf16(p[u * 8 + 4], p[u * 8 + 5]), pack_bf16(p[u * 8 + 6], p[u * 8 + 7])};
-          pf[qb][kb * 2 + u] = __builtin_bit_cast(bf16x8, w);
-        }
-      }
-    // ---- O^T += V^T P^T
-#pragma unroll
-    for (int db = 0; db < 2 * AH; ++db)
-#pragma unroll
-      for (int kk = 0; kk < 4; ++kk) {
-        const bf16x8 va = tl.read_cols(Vt[db >> 1], kk * 16, db & 1);
-#pragma unroll
-        for (int qb = 0; qb < QB; ++qb) o[db][qb] = mfma_32x32x16(va, pf[qb][kk], o[db][qb]);
-      }
-    if (EIGHT && more) store8(next, Kn, Vn);
+    if (EIGHT && !RAW && more) store8(next, Kn, Vn);
     wait_vmem();
     __syncthreads();
     ++t;
   };
   while (t < end) {
     stage(K0, V0, K1, V1);
-    if (t >= end) break;
-    stage(K1, V1, K0, V0);
+    if constexpr (!RAW) {
+      if (t >= end) break;
+      stage(K1, V1, K0, V0);
+    }
   }
 
   if (parts > 1) {  // this part's result
@@ -599,8 +636,9 @@ __global__ void __launch_bounds__(256) chunk_join_kernel(ChunkArgs a, int BM) {
 }
 
 // How a call is laid over the chip, from what the host knows: the tokens and the table's width, not counts and lengths.
-// Work-groups.  256 rows by eight waves read a tile from memory for twice the rows, but leave a CU to one work-group: heads of 192, whose four waves
-// would be alone on it too (2048 tokens of 16384 slots, 8 key heads, us: 1073 -> 747), and of 128 where these work-groups fill the chip twice, or
+// Work-groups.  256 rows by eight waves read a tile from memory for twice the rows, but leave a CU to one work-group: heads of 192 and 256, whose four
+// waves would be alone on it too (2048 tokens of 16384 slots, 8 key heads, us: 1073 -> 747, 1504 -> 1083, in e4m3 1657 -> 764, 1872 -> 1197; 1024 of 1024,
+// 4 x 16 key heads of 256, 82 -> 85 and 112 -> 97), and of 128 where these work-groups fill the chip twice, or
 // once with walks of about one length (the same 512 -> 501, 64k slots 2145 -> 1973, 8 x 512 of 8192 572 -> 541, in e4m3 578 -> 527; but 2048 of
 // 2048 57 -> 65, 512 of 8192 84 -> 97, 4 x 1024 of 1024, 16 key heads, 36 -> 43).  Heads of 64 take 64 rows a wave where these fill the chip (eight
 // waves of 32: 307 -> 341).
@@ -616,7 +654,7 @@ ChunkPlan plan_of(const CacheDims &d, int T) {
   if (p.few) return p;
   p.qb = 1; const int64_t large = heads * ((rows + 255) / 256), slots = (int64_t)d.width * d.page;
   p.rw = rows <= 64 && d.A <= 128 ? 2 : 4;
-  if (d.A == 192 ? rows > 128 : d.A == 128 && (large >= 512 || (large >= 256 && slots >= 4 * (int64_t)T))) p.rw = 8;
+  if (d.A >= 192 ? rows > 128 : d.A == 128 && (large >= 512 || (large >= 256 && slots >= 4 * (int64_t)T))) p.rw = 8;
   if (d.A == 64 && large >= 512) p.qb = 2;
   p.tiles = (int)((rows + 32 * p.qb * p.rw - 1) / (32 * p.qb * p.rw));
   // Parts.  None where the walks are short for a full chip, where one sequence alone fills two rounds of places (one or two work-groups on a
@@ -644,7 +682,7 @@ void launch_chunk(const ChunkArgs &a, const ChunkPlan &p, hipStream_t st) {
   if constexpr (AH <= 2) {
     if (p.rw == 2) return launch_chunk<AH, 1, 2>(a, p, st);
   }
-  if constexpr (AH == 2 || AH == 3) {
+  if constexpr (AH >= 2) {
     if (p.rw == 8) return launch_chunk<AH, 1, 8>(a, p, st);
   }
   launch_chunk<AH, 1, 4>(a, p, st);

@@ -49,7 +49,7 @@ def test_few_rows_and_many(rec, kw, T, few, eight):
     (64, 1, 2, 1, 64, 1024, 1, 2, True), (64, 8, 8, 4, 512, 512, 2, 4, False),
     (64, 1, 8, 4, 480, 480, 1, 4, False), (128, 1, 8, 4, 2048, 2048, 1, 4, False), (128, 1, 8, 4, 2048, 8192, 1, 8, False),
     (128, 8, 8, 4, 512, 512, 1, 8, False), (128, 1, 8, 4, 500, 65536, 1, 4, True), (192, 1, 2, 1, 128, 128, 1, 4, False),
-    (192, 1, 2, 1, 129, 129, 1, 8, False), (192, 1, 2, 1, 129, 4096, 1, 8, True), (256, 1, 2, 1, 500, 500, 1, 4, False),
+    (192, 1, 2, 1, 129, 129, 1, 8, False), (192, 1, 2, 1, 129, 4096, 1, 8, True), (256, 1, 2, 1, 500, 500, 1, 8, False), (256, 1, 2, 1, 128, 500, 1, 4, False),
     (256, 1, 2, 1, 33, 8192, 1, 4, True), (128, 65, 2, 1, 65, 8192, 1, 4, False), (128, 64, 2, 1, 65, 8192, 1, 4, True)])
 @pytest.mark.parametrize("eight", [False, True])
 def test_work_groups_and_parts(rec, A, B, Zkv, group, T, slots, qb, rw, divided, eight):

@@ -111,7 +111,7 @@ def test_infinite_and_nan_tokens_reach_the_rows_that_see_them_alone(dtype, T, ki
     assert torch.equal(O, ref[0]) and torch.equal(LSE, ref[1])
 
 
-@pytest.mark.parametrize("A,B,Z,T,n", [(128, 8, 32, 512, 2048), (128, 2, 32, 1024, 4200), (192, 2, 2, 300, 700), (192, 1, 2, 200, 3000), (256, 1, 2, 90, 2000), (64, 16, 32, 1000, 1000)])
+@pytest.mark.parametrize("A,B,Z,T,n", [(128, 8, 32, 512, 2048), (128, 2, 32, 1024, 4200), (192, 2, 2, 300, 700), (192, 1, 2, 200, 3000), (256, 1, 2, 90, 2000), (256, 2, 2, 300, 700), (256, 1, 8, 100, 3000), (64, 16, 32, 1000, 1000)])
 @pytest.mark.parametrize("eight", [False, True])
 def test_infinite_and_nan_tokens_of_large_work_groups(A, B, Z, T, n, eight):
     """The same where work-groups have 256 rows or walks are divided: one value of one slot NaN, another head's infinite, one key NaN."""
@@ -185,7 +185,8 @@ def test_scores_that_grow_by_large_steps(Z, T):
     ("bf16", 16, 4, 128, 16, 1024, [4096, 2100, 1024, 3000], [1024, 500, 1024, 7], True, False),  # heads of 128 by 256 rows
     ("bf16", 32, 8, 128, 16, 520, [4500], None, True, True), ("bf16", 32, 8, 128, 16, 520, [4500, 600, 2000, 1], [520, 520, 0, 1], False, True),
     ("bf16", 8, 8, 128, 16, 500, [2000 + 31 * b for b in range(17)], None, True, False),   # ... one tile and a part of one, divided
-    ("bf16", 4, 2, 192, 16, 300, [2000, 400], [300, 299], True, False),
+    ("bf16", 4, 2, 192, 16, 300, [2000, 400], [300, 299], True, False), ("bf16", 4, 2, 192, 16, 300, [2000, 400], [300, 299], True, True),
+    ("bf16", 4, 2, 256, 16, 300, [2000, 400], [300, 299], False, False), ("bf16", 3, 1, 256, 24, 331, [4000, 331, 1], None, True, True),
     ("f32", 6, 3, 64, 24, 300, [2000, 300], None, True, False), ("f32", 20, 1, 128, 16, 5, [6000] * 3, None, True, False),
     ("f32", 4, 2, 256, 16, 100, [3000], [77], True, False), ("bf16", 2, 1, 64, 16, 8, [50 + 3 * b for b in range(700)], None, True, False)])
 def test_long_and_many(dtype, Z, Zkv, A, page, T, lengths, counts, causal, eight):
