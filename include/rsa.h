@@ -388,7 +388,8 @@ int rsa_cache_attend8(const rsa_cache_desc *d, const void *Q, const void *Kc, co
 
 /* The tokens of a cache as dense tensors: K, V (B, Zkv, T, A), strides kv_stride.  Of sequence b the last counts[b] slots (NULL, or
  * above T: T; below 0: 0) are read, token t from slot lengths[b] - counts[b] + t; zeros where that is not held.  Rows of
- * tokens that are not there are left as they are or, by the bits of pad, become zeros: 1 those of K, 2 of V.  Ks, Vs: of pools in e4m3, of which the results have the exact values, else both NULL. */
+ * tokens that are not there are left as they are or, by the bits of pad, become zeros: 1 those of K, 2 of V.  Ks, Vs: of pools in
+ * e4m3, of which the results have the exact values, else both NULL. */
 int rsa_cache_read(const rsa_cache_desc *d, int32_t T, int32_t pad, const void *Kc, const void *Vc, const uint8_t *Ks,
                    const uint8_t *Vs, const int32_t *table, const int32_t *lengths, const int32_t *counts,
                    void *K, void *V, void *stream);
@@ -397,8 +398,8 @@ int rsa_cache_read(const rsa_cache_desc *d, int32_t T, int32_t pad, const void *
  * Q and O are (B, Z, T, A), LSE (B, Z, T) fp32.  Of sequence b the first counts[b] tokens (as in rsa_cache_append) are there; token t
  * is that of slot lengths[b] - counts[b] + t and sees the slots that are held up to its own or, without `causal`, all that are held (a rank
  * whose share of the cache lies in front of the tokens).  A row that sees no key gets O = 0 and LSE = -inf; rows of tokens that are not there
- * are left as they are or, by the bits of pad, get these as well: 1 in O, 2 in LSE.  Pool memory outside the slots that a row sees does not reach its result, whatever it holds: not one of an infinite or
- * NaN key or value either.  Ks, Vs as in rsa_cache_read.  fp32, and bf16 up to 32 rows of a key head (T Z/Zkv), as rsa_cache_attend; beyond that P is
+ * are left as they are or, by the bits of pad, get these as well: 1 in O, 2 in LSE.  Pool memory outside the slots that a row
+ * sees does not reach its result, whatever it holds: not one of an infinite or NaN key or value either.  Ks, Vs as in rsa_cache_read.  fp32, and bf16 up to 32 rows of a key head (T Z/Zkv), as rsa_cache_attend; beyond that P is
  * rounded to bf16 once, as in rsa_forward.  T * Z must be below 2^31, B * Z * T * A at most 2^34.  ws:
  * rsa_cache_chunk_workspace_bytes(d, T) bytes, as for rsa_cache_attend.
  * Results of shares are joined by rsa_cache_join with Z * T for Z: rows are rows. */

@@ -431,8 +431,8 @@ PyObject *cache_read(Call &c) {
   }
   check_device(c, 11);
   return finish([&](void *st) {
-    return rsa_cache_read(&d, (int32_t)T, !c.given(7) | !c.given(8) << 1, ptr(c.tensor(2)), ptr(c.tensor(3)), exponents(c, 9), exponents(c, 10), table, lengths, counts,
-                          ptr(out[0]), ptr(out[1]), st); }, {out[0], out[1]});
+    return rsa_cache_read(&d, (int32_t)T, !c.given(7) | !c.given(8) << 1, ptr(c.tensor(2)), ptr(c.tensor(3)), exponents(c, 9), exponents(c, 10),
+                          table, lengths, counts, ptr(out[0]), ptr(out[1]), st); }, {out[0], out[1]});
 }
 
 // desc, Q, Kc, Vc, table, lengths, O, LSE, ws, Ks, Vs
@@ -478,8 +478,8 @@ PyObject *cache_attend_chunk(Call &c) {
   size_t n = 0;
   const at::Tensor ws = cache_workspace(c, 10, c.given(10) ? 0 : rsa_cache_chunk_workspace_bytes(&d, T), Q, n);
   return finish([&](void *st) {
-    return rsa_cache_attend_chunk(&d, T, causal, !c.given(8) | !c.given(9) << 1, ptr(Q), ptr(Kc), ptr(Vc), exponents(c, 11), exponents(c, 12), table, lengths, counts, ptr(O),
-                                  static_cast<float *>(ptr(LSE)), ptr(ws), n, st); }, {O, LSE});
+    return rsa_cache_attend_chunk(&d, T, causal, !c.given(8) | !c.given(9) << 1, ptr(Q), ptr(Kc), ptr(Vc), exponents(c, 11), exponents(c, 12),
+                                  table, lengths, counts, ptr(O), static_cast<float *>(ptr(LSE)), ptr(ws), n, st); }, {O, LSE});
 }
 
 // desc, Op, LSEp, O, LSE

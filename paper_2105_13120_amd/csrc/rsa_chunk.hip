@@ -10,6 +10,11 @@
 // have them, would triple half of the matrix work, which is what bounds this kernel).
 // Tiles come into LDS by direct loads from wherever their slots' pages are, a slot per lane looked up one tile further ahead; pools in
 // e4m3 come through registers, where what they stand for is formed exactly in bf16, once for all rows of the work-group.
+// Bound by the matrix cores: 2048 tokens of 65536 slots, 32 query, 8 key heads of 128, run at 1.07 to 1.13 PFLOP/s from one GPU to another, where
+// a product of two 8192 x 8192 matrices by the library does 1.23; prompts of up to 2048 tokens at 0.58, of which a work-group's start and end, when
+// the matrix cores wait, take a third.
+// Tried: work-groups that stay and ask for the next item's first tile ahead (1954 -> 2172 us, prompts 126 -> 142); loads a tile and a half ahead with two
+// barriers (3 to 9 % slower but for short walks).
 // Slots that are not seen: a score is -inf, and a value is cleared in LDS, since 0 times what lies there could be NaN.  Where rows of a
 // work-group see different slots of a tile, infinite and NaN values are taken out likewise and given to the rows that see them.
 #include "rsa_cache_tokens.h"
@@ -56,9 +61,9 @@ struct Item {
 };
 
 // Sequences of different lengths with different numbers of new tokens leave tiles without rows and walks of all lengths.  Up to
-// kSorted sequences are laid out by what they have: all items by the length of their walks, the longest first, without gaps (by
-// tiles of the longest call instead, empty ones among them: prompts of 128 to 2048 tokens 154 us, see below).  A walk that is long beside a
-// place's share of all the work is divided.
+// kSorted sequences are laid out by what they have: all items by the length of their walks, the longest first, without gaps (8 prompts of 128 to
+// 2048 tokens by the tiles of the longest, empty ones among them: 154 us; in this order 126).  A walk that is long beside a place's share of all the
+// work is divided.
 //
 // A tile's walk is w = ceil(n / P) long, n the tiles of 64 slots that its last row sees and P the parts of its sequence's walks.  The
 // last row's limit grows with the tile, so that the tiles of a sequence with walks of w and more are those from a first one on, and
@@ -574,7 +579,8 @@ __global__ void __launch_bounds__(64 * RW, AH <= 2 || RW == 8 ? 2 : 1) chunk_ker
 }
 
 // The parts of divided walks: with M the largest of a row's maxima, O = sum_s 2^(m_s - M) o_s / sum_s 2^(m_s - M) l_s.  A part that
-// saw no key of the row has m = -inf and is left out.  A work-group has 32 rows, a thread 16 bytes of every 32 columns as a lane of the
+// saw no key of the row has m = -inf and is left out.  Memory bounds it (8 x 512 tokens of up to 16384 slots: 15 us of 505).
+// A work-group has 32 rows, a thread 16 bytes of every 32 columns as a lane of the
 // accumulators had them; the rows leave through LDS.
 template <int AH>
 __global__ void __launch_bounds__(256) chunk_join_kernel(ChunkArgs a, int BM) {
