@@ -166,22 +166,26 @@ struct Layout {
   }
 };
 
-template <int AH, int QB, int RW, bool EIGHT>
+// KS: the waves that share a row block's rows, each with its part of a tile's keys
+template <int AH, int QB, int RW, int KS, bool EIGHT>
 __global__ void __launch_bounds__(64 * RW, AH <= 2 || RW == 8 ? 2 : 1) chunk_kernel(ChunkArgs a) {
-  constexpr int A = 64 * AH, R = 32 * QB, BM = R * RW, THREADS = 64 * RW, KB = RW == 8 && (AH == 4 || (AH == 3 && EIGHT)) ? 1 : 2;
+  constexpr int A = 64 * AH, R = 32 * QB, ROWS = RW / KS, BM = R * ROWS, THREADS = 64 * RW;
+  constexpr int KB = KS == 2 || (RW == 8 && (AH == 4 || (AH == 3 && EIGHT))) ? 1 : 2;
   // Long heads' pools in e4m3 wait in LDS (K1, V1) as they are, since registers have no room for them, and are widened into K0 and V0 when their turn
   // comes (2048 tokens of 16384 slots, us: heads of 192 963 -> 764, of 256 1872 -> 1197)
   constexpr bool RAW = EIGHT && RW == 8 && AH > 2;
   // (two buffers, each an object of its own, so that the compiler sees that loads into one miss the reads of the other)
   __shared__ __attribute__((aligned(16))) unsigned char K0[AH][kTileBytes], K1[AH][kTileBytes], V0[AH][kTileBytes], V1[AH][kTileBytes];
 
+  __shared__ float2 shared_ends[KS == 2 ? BM : 1];
+
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int col = lane & 31, half = lane >> 5;
+  const int col = lane & 31, half = lane >> 5, block = wave & (ROWS - 1), share = wave / ROWS;
   // The lane as a number of its own, from which a tile's addresses are worked out anew where registers are scarce (kept over the walk they
   // would be spilled, and a reload waits for the next tile's loads: heads of 256, 2048 tokens of 16384 slots 1117 -> 1083 us, 1024 of 1024 99 -> 85)
   const auto anew = [&]() __attribute__((always_inline)) {
     int l = lane;
-    if constexpr (KB == 1) asm volatile("" : "+v"(l));
+    if constexpr (RW == 8 && KB == 1) asm volatile("" : "+v"(l));
     return l;
   };
   Item it{};
@@ -221,7 +225,7 @@ __global__ void __launch_bounds__(64 * RW, AH <= 2 || RW == 8 ? 2 : 1) chunk_ker
   uint32_t lim[QB];
 #pragma unroll
   for (int qb = 0; qb < QB; ++qb) {
-    int row = row0 + wave * R + qb * 32 + col;
+    int row = row0 + block * R + qb * 32 + col;
     row = row < rows_all ? row : rows_all - 1;
     lim[qb] = row < rows ? limit_of(row) : 0u;
     const int token = (int)a.by_group((uint32_t)row), z = (int)h * group + row - token * group;
@@ -433,7 +437,8 @@ __global__ void __launch_bounds__(64 * RW, AH <= 2 || RW == 8 ? 2 : 1) chunk_ker
 
     // ---- by blocks of 32 keys: both at once or, where the accumulators leave no room for both's scores, one after the other
 #pragma unroll
-    for (int k1 = 0; k1 < 2; k1 += KB) {
+    for (int k0th = 0; k0th < 2 / KS; k0th += KB) {
+      const int k1 = KS == 2 ? share : k0th;
       // ---- S^T = K Q^T
       f32x16 s[KB][QB];
       float tm[QB];
@@ -531,10 +536,42 @@ __global__ void __launch_bounds__(64 * RW, AH <= 2 || RW == 8 ? 2 : 1) chunk_ker
     }
   }
 
+  if constexpr (KS == 2) {  // the shares of a block's rows together, as parts are
+    float *other = reinterpret_cast<float *>(block == 0 ? K0[0] : block == 1 ? K1[0] : block == 2 ? V0[0] : V1[0]);
+    float2 *ends = shared_ends + block * R + col;
+    float lt = xhalf_sum(l[0]), top = lt != 0.f ? mc[0] : -INFINITY;
+    if (share == 1) {
+#pragma unroll
+      for (int db = 0; db < 2 * AH; ++db)
+#pragma unroll
+        for (int g = 0; g < 4; ++g)
+          reinterpret_cast<f32x4 *>(other)[(db * 4 + g) * 64 + lane] = f32x4{o[db][0][g * 4 + 0], o[db][0][g * 4 + 1], o[db][0][g * 4 + 2], o[db][0][g * 4 + 3]};
+      if (half == 0) *ends = make_float2(top, lt);
+    }
+    __syncthreads();
+    if (share == 1) return;
+    const float2 x = *ends;
+    const float M = fmaxf(top, x.x), w0 = top > -INFINITY ? __builtin_amdgcn_exp2f(top - M) : 0.f, w1 = x.x > -INFINITY ? __builtin_amdgcn_exp2f(x.x - M) : 0.f;
+    const bool one = top > -INFINITY, two = x.x > -INFINITY;
+#pragma unroll
+    for (int db = 0; db < 2 * AH; ++db)
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const f32x4 y = reinterpret_cast<const f32x4 *>(other)[(db * 4 + g) * 64 + lane];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float z = one ? o[db][0][g * 4 + e] * w0 : 0.f;
+          o[db][0][g * 4 + e] = two ? fmaf(w1, y[e], z) : z;
+        }
+      }
+    l[0] = half == 0 ? (one ? lt * w0 : 0.f) + (two ? x.y * w1 : 0.f) : 0.f;
+    mc[0] = one || two ? M : 0.f;
+  }
+
   if (parts > 1) {  // this part's result
     const int64_t place = ((int64_t)part * a.by_heads.d + head) * a.tiles + it.tile;
-    f32x4 *po = reinterpret_cast<f32x4 *>(a.part_o + (place * BM + wave * R) * A) + lane;
-    float2 *ml = reinterpret_cast<float2 *>(a.part_ml) + place * BM + wave * R + col;
+    f32x4 *po = reinterpret_cast<f32x4 *>(a.part_o + (place * BM + block * R) * A) + lane;
+    float2 *ml = reinterpret_cast<float2 *>(a.part_ml) + place * BM + block * R + col;
 #pragma unroll
     for (int qb = 0; qb < QB; ++qb) {
       const float lt = xhalf_sum(l[qb]);
@@ -555,20 +592,20 @@ __global__ void __launch_bounds__(64 * RW, AH <= 2 || RW == 8 ? 2 : 1) chunk_ker
   for (int qb = 0; qb < QB; ++qb) {
     const float lt = xhalf_sum(l[qb]);
     inv[qb] = lt != 0.f ? 1.0f / lt : 0.f;
-    const int row = row0 + wave * R + qb * 32 + col;
+    const int row = row0 + block * R + qb * 32 + col;
     if (half == 0 && (row < rows || ((a.pad & 2) && row < rows_all))) {
       const int token = (int)a.by_group((uint32_t)row), z = (int)h * group + row - token * group;
       a.LSE[((int64_t)b * a.Z + z) * a.T + token] = lt != 0.f && row < rows ? (mc[qb] + __builtin_amdgcn_logf(lt)) * kLn2 : -INFINITY;
     }
   }
-  unsigned char *ot = ((wave & 3) == 0 ? K0[0] : (wave & 3) == 1 ? K1[0] : (wave & 3) == 2 ? V0[0] : V1[0]) + (wave >> 2) * 32 * 128;
+  unsigned char *ot = ((block & 3) == 0 ? K0[0] : (block & 3) == 1 ? K1[0] : (block & 3) == 2 ? V0[0] : V1[0]) + (block >> 2) * 32 * 128;
 #pragma unroll
   for (int ah = 0; ah < AH; ++ah) {
 #pragma unroll
     for (int qb = 0; qb < QB; ++qb) stage_block_T(ot, qb * 32, o[2 * ah][qb], o[2 * ah + 1][qb], inv[qb], lane);
 #pragma unroll
     for (int it = 0; it < R / 8; ++it) {
-      const int r = it * 8 + (lane >> 3), cc = lane & 7, row = row0 + wave * R + r;
+      const int r = it * 8 + (lane >> 3), cc = lane & 7, row = row0 + block * R + r;
       if (row < rows || ((a.pad & 1) && row < rows_all)) {
         const int token = (int)a.by_group((uint32_t)row), z = (int)h * group + row - token * group;
         *reinterpret_cast<u32x4 *>(a.O + (int64_t)b * a.os[0] + (int64_t)z * a.os[1] + (int64_t)token * a.os[2] + ah * 64 + cc * 8) =
@@ -648,9 +685,13 @@ __global__ void __launch_bounds__(256) chunk_join_kernel(ChunkArgs a, int BM) {
 // once with walks of about one length (the same 512 -> 501, 64k slots 2145 -> 1973, 8 x 512 of 8192 572 -> 541, in e4m3 578 -> 527; but 2048 of
 // 2048 57 -> 65, 512 of 8192 84 -> 97, 4 x 1024 of 1024, 16 key heads, 36 -> 43).  Heads of 64 take 64 rows a wave where these fill the chip (eight
 // waves of 32: 307 -> 341).
+// Fewer rows leave waves without any, or CUs with few waves.  Two waves then share 32 rows, each with half of a tile's keys, and are joined at the end: up to
+// 64 rows on four waves (16 tokens of each of 16 sequences of 4096, 4 query heads a key head, us, before and with it, bf16 and e4m3: heads of 64
+// 37 -> 34, 39 -> 32, of 128 68 -> 65, 58 -> 46, of 192 114 -> 101, 115 -> 86, of 256 146 -> 127, 198 -> 127), up to 128 of long heads on eight (32 tokens:
+// heads of 192 118 -> 107, 115 -> 98, of 256 in e4m3 195 -> 165; in bf16 these spill, 148 -> 181, and take four waves, one a row block).
 struct ChunkPlan {
   bool few;         // by 16 or 32 rows at a time, from memory to the operands (rsa_cache.hip)
-  int qb, rw;       // 32-row blocks of a wave, waves
+  int qb, rw;       // 32-row blocks of a wave, waves of different rows
   int tiles, parts; // row tiles of a key head; parts of a walk at most
 };
 ChunkPlan plan_of(const CacheDims &d, int T) {
@@ -659,7 +700,7 @@ ChunkPlan plan_of(const CacheDims &d, int T) {
   p.few = d.dtype != RSA_BF16 || rows <= 32;
   if (p.few) return p;
   p.qb = 1; const int64_t large = heads * ((rows + 255) / 256), slots = (int64_t)d.width * d.page;
-  p.rw = rows <= 64 && d.A <= 128 ? 2 : 4;
+  p.rw = rows <= 64 ? 2 : 4;
   if (d.A >= 192 ? rows > 128 : d.A == 128 && (large >= 512 || (large >= 256 && slots >= 4 * (int64_t)T))) p.rw = 8;
   if (d.A == 64 && large >= 512) p.qb = 2;
   p.tiles = (int)((rows + 32 * p.qb * p.rw - 1) / (32 * p.qb * p.rw));
@@ -674,24 +715,28 @@ ChunkPlan plan_of(const CacheDims &d, int T) {
   return p;
 }
 
-template <int AH, int QB, int RW>
+template <int AH, int QB, int RW, int KS>
 void launch_chunk(const ChunkArgs &a, const ChunkPlan &p, hipStream_t st) {
+  // (128 rows of heads of 256 in bf16: see plan_of)
+  constexpr bool apart = AH == 4 && RW == 8 && KS == 2;
   const unsigned grid = (unsigned)(a.by_heads.d * p.tiles * p.parts);
-  if (a.Ks) chunk_kernel<AH, QB, RW, true><<<grid, 64 * RW, 0, st>>>(a);
-  else chunk_kernel<AH, QB, RW, false><<<grid, 64 * RW, 0, st>>>(a);
+  if (a.Ks) chunk_kernel<AH, QB, RW, KS, true><<<grid, 64 * RW, 0, st>>>(a);
+  else if constexpr (apart) chunk_kernel<AH, QB, 4, 1, false><<<grid, 256, 0, st>>>(a);
+  else chunk_kernel<AH, QB, RW, KS, false><<<grid, 64 * RW, 0, st>>>(a);
 }
 template <int AH>
 void launch_chunk(const ChunkArgs &a, const ChunkPlan &p, hipStream_t st) {
+  if constexpr (AH > 2) {
+    if (p.rw == 4) return launch_chunk<AH, 1, 8, 2>(a, p, st);
+  }
   if constexpr (AH == 1) {
-    if (p.qb == 2) return launch_chunk<AH, 2, 4>(a, p, st);
+    if (p.qb == 2) return launch_chunk<AH, 2, 4, 1>(a, p, st);
   }
-  if constexpr (AH <= 2) {
-    if (p.rw == 2) return launch_chunk<AH, 1, 2>(a, p, st);
-  }
+  if (p.rw == 2) return launch_chunk<AH, 1, 4, 2>(a, p, st);
   if constexpr (AH >= 2) {
-    if (p.rw == 8) return launch_chunk<AH, 1, 8>(a, p, st);
+    if (p.rw == 8) return launch_chunk<AH, 1, 8, 1>(a, p, st);
   }
-  launch_chunk<AH, 1, 4>(a, p, st);
+  if constexpr (AH <= 2) launch_chunk<AH, 1, 4, 1>(a, p, st);
 }
 template <int AH>
 void launch_all(const ChunkArgs &a, const ChunkPlan &p, hipStream_t st) {

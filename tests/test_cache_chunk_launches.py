@@ -43,19 +43,20 @@ def test_few_rows_and_many(rec, kw, T, few, eight):
         assert form[0] == d.A // 64 and form[-1] == eight
 
 
-# (A, heads, rows of a key head) and the table's slots: 32-row blocks of a wave, waves, divided or not
+# (A, heads, rows of a key head) and the table's slots: 32-row blocks of a wave, waves of different rows, divided or not
 @pytest.mark.parametrize("A,B,Zkv,group,T,slots,qb,rw,divided", [
     (64, 1, 2, 1, 33, 64, 1, 2, False), (128, 1, 2, 1, 64, 64, 1, 2, False), (128, 1, 2, 1, 65, 65, 1, 4, False),
     (64, 1, 2, 1, 64, 1024, 1, 2, True), (64, 8, 8, 4, 512, 512, 2, 4, False),
     (64, 1, 8, 4, 480, 480, 1, 4, False), (128, 1, 8, 4, 2048, 2048, 1, 4, False), (128, 1, 8, 4, 2048, 8192, 1, 8, False),
     (128, 8, 8, 4, 512, 512, 1, 8, False), (128, 1, 8, 4, 500, 65536, 1, 4, True), (192, 1, 2, 1, 128, 128, 1, 4, False),
     (192, 1, 2, 1, 129, 129, 1, 8, False), (192, 1, 2, 1, 129, 4096, 1, 8, True), (256, 1, 2, 1, 500, 500, 1, 8, False), (256, 1, 2, 1, 128, 500, 1, 4, False),
-    (256, 1, 2, 1, 33, 8192, 1, 4, True), (128, 65, 2, 1, 65, 8192, 1, 4, False), (128, 64, 2, 1, 65, 8192, 1, 4, True)])
+    (256, 1, 2, 1, 33, 8192, 1, 2, True), (256, 1, 2, 1, 65, 8192, 1, 4, True), (192, 1, 2, 1, 64, 100, 1, 2, False), (128, 65, 2, 1, 65, 8192, 1, 4, False), (128, 64, 2, 1, 65, 8192, 1, 4, True)])
 @pytest.mark.parametrize("eight", [False, True])
 def test_work_groups_and_parts(rec, A, B, Zkv, group, T, slots, qb, rw, divided, eight):
     d = cache(A=A, B=B, Z=Zkv * group, Zkv=Zkv, page=1, width=slots, pages=B * slots)
     k = chunk(rec, d, T, eight)
-    assert numbers(k[0].name) == [A // 64, qb, rw, eight] and k[0].threads == 64 * rw
+    shares = 2 if rw == 2 or (rw == 4 and (A == 192 or (A == 256 and eight))) else 1                            # waves of the same rows
+    assert numbers(k[0].name) == [A // 64, qb, rw * shares, shares, eight] and k[0].threads == 64 * rw * shares
     tiles = -(-T * group // (32 * qb * rw))
     heads = B * Zkv
     need = rsa.cache_chunk_workspace_bytes(d, T)

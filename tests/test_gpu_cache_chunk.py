@@ -111,10 +111,11 @@ def test_infinite_and_nan_tokens_reach_the_rows_that_see_them_alone(dtype, T, ki
     assert torch.equal(O, ref[0]) and torch.equal(LSE, ref[1])
 
 
-@pytest.mark.parametrize("A,B,Z,T,n", [(128, 8, 32, 512, 2048), (128, 2, 32, 1024, 4200), (192, 2, 2, 300, 700), (192, 1, 2, 200, 3000), (256, 1, 2, 90, 2000), (256, 2, 2, 300, 700), (256, 1, 8, 100, 3000), (64, 16, 32, 1000, 1000)])
+@pytest.mark.parametrize("A,B,Z,T,n", [(128, 8, 32, 512, 2048), (128, 2, 32, 1024, 4200), (192, 2, 2, 300, 700), (192, 1, 2, 200, 3000), (256, 1, 2, 90, 2000), (256, 2, 2, 300, 700), (256, 1, 8, 100, 3000), (64, 16, 32, 1000, 1000),
+                                        (64, 2, 2, 33, 200), (128, 1, 2, 50, 700), (128, 1, 2, 64, 5000), (192, 2, 2, 50, 200), (192, 1, 2, 100, 3000), (256, 1, 2, 50, 600)])
 @pytest.mark.parametrize("eight", [False, True])
 def test_infinite_and_nan_tokens_of_large_work_groups(A, B, Z, T, n, eight):
-    """The same where work-groups have 256 rows or walks are divided: one value of one slot NaN, another head's infinite, one key NaN."""
+    """The same where work-groups have 256 rows, waves share rows or walks are divided: one value of one slot NaN, another head's infinite, one key NaN."""
     g = torch.Generator(device="cuda").manual_seed(45)
     page, Zkv = 16, max(2, Z // 4)
     W = -(-n // page)
@@ -158,10 +159,11 @@ def test_scales(T, scale, spread, dtype):
     compare_chunk(c, Q, chunk(c, Q, scale=scale), dtype, scale=scale or None)
 
 
-@pytest.mark.parametrize("Z,T", [(2, 5), (2, 60)])
-def test_scores_that_grow_by_large_steps(Z, T):
+@pytest.mark.parametrize("Z,T", [(2, 5), (2, 60), (1, 100), (1, 300)])
+@pytest.mark.parametrize("A", [64, 192, 256])
+def test_scores_that_grow_by_large_steps(Z, T, A):
     """Keys in ascending and in descending order of their scores, by hundreds."""
-    n, A = 300, 64
+    n = 300
     for order in (np.arange(n), np.arange(n)[::-1]):
         rng = np.random.default_rng(36)
         c = Cache(rng, [n], 1, A, 16, 19, "bf16")
