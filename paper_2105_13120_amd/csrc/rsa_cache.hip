@@ -1168,7 +1168,8 @@ void launch_attend(const AttendArgs &a, const AttendPlan &p, hipStream_t st) {
 }
 template <typename T, int A, int KIND>
 void launch_attend(const AttendArgs &a, const AttendPlan &p, hipStream_t st) {
-  if constexpr (A <= 128) {
+  // (chunks of more than 16 rows of heads of 64 in bf16 have a kernel of their own)
+  if constexpr (A <= 128 && !(A == 64 && sizeof(T) == 2 && (KIND & kChunk) != 0)) {
     if (p.nq == 2) return launch_attend<T, A, 2, KIND>(a, p, st);
   }
   launch_attend<T, A, 1, KIND>(a, p, st);

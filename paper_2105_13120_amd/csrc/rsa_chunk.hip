@@ -689,15 +689,18 @@ __global__ void __launch_bounds__(256) chunk_join_kernel(ChunkArgs a, int BM) {
 // 64 rows on four waves (16 tokens of each of 16 sequences of 4096, 4 query heads a key head, us, before and with it, bf16 and e4m3: heads of 64
 // 37 -> 34, 39 -> 32, of 128 68 -> 65, 58 -> 46, of 192 114 -> 101, 115 -> 86, of 256 146 -> 127, 198 -> 127), up to 128 of long heads on eight (32 tokens:
 // heads of 192 118 -> 107, 115 -> 98, of 256 in e4m3 195 -> 165; in bf16 these spill, 148 -> 181, and take four waves, one a row block).
+// Up to 16 rows go straight from memory to the operands; up to 32 in heads of 128 and, in e4m3, of 256, where the others' ways of 32 rows are slower (8 tokens
+// of each of 16 sequences of 4096, 4 query heads a key head, us, so and by tiles in LDS, bf16 and e4m3: heads of 64 47 and 34, 42 and 32, of 128 66 and
+// 64, 47 and 45, but of 64 sequences of 1024 67 and 84, 47 and 77; of 192 140 and 98, 86 and 85, of 256 173 and 124, 96 and 127).
 struct ChunkPlan {
   bool few;         // by 16 or 32 rows at a time, from memory to the operands (rsa_cache.hip)
   int qb, rw;       // 32-row blocks of a wave, waves of different rows
   int tiles, parts; // row tiles of a key head; parts of a walk at most
 };
-ChunkPlan plan_of(const CacheDims &d, int T) {
+ChunkPlan plan_of(const CacheDims &d, int T, bool eight) {
   ChunkPlan p{};
   const int64_t rows = (int64_t)T * (d.Z / d.Zkv), heads = (int64_t)d.B * d.Zkv;
-  p.few = d.dtype != RSA_BF16 || rows <= 32;
+  p.few = d.dtype != RSA_BF16 || rows <= (d.A == 128 || (d.A == 256 && eight) ? 32 : 16);
   if (p.few) return p;
   p.qb = 1; const int64_t large = heads * ((rows + 255) / 256), slots = (int64_t)d.width * d.page;
   p.rw = rows <= 64 ? 2 : 4;
@@ -752,14 +755,18 @@ size_t part_rows(const CacheDims &d, const ChunkPlan &p) { return (size_t)p.part
 }  // namespace
 
 size_t chunk_workspace_bytes(const CacheDims &d, int T) {
-  const ChunkPlan p = plan_of(d, T);
-  if (p.few) return chunk_few_workspace_bytes(d, T);
-  return p.parts == 1 ? 0 : kSorted * sizeof(uint32_t) + part_rows(d, p) * (d.A + 2) * 4;
+  size_t most = 0;  // (of pools in the queries' type and in e4m3)
+  for (const bool eight : {false, true}) {
+    const ChunkPlan p = plan_of(d, T, eight);
+    const size_t n = p.few ? chunk_few_workspace_bytes(d, T) : p.parts == 1 ? 0 : kSorted * sizeof(uint32_t) + part_rows(d, p) * (d.A + 2) * 4;
+    most = n > most ? n : most;
+  }
+  return most;
 }
 
 hipError_t cache_attend_chunk(const CacheDims &d, const CachePools &c, int T, int causal, int pad, const void *Q, const int32_t *table,
                               const int32_t *lengths, const int32_t *counts, void *O, float *LSE, void *ws, hipStream_t st) {
-  const ChunkPlan p = plan_of(d, T);
+  const ChunkPlan p = plan_of(d, T, c.Ks != nullptr);
   if (p.few) return chunk_few(d, c, T, causal, pad, Q, table, lengths, counts, O, LSE, ws, st);
   ChunkArgs a{};
   a.Q = static_cast<const uint16_t *>(Q); a.Kc = c.Kc; a.Vc = c.Vc; a.Ks = c.Ks; a.Vs = c.Vs;

@@ -27,13 +27,15 @@ def numbers(name):
 
 
 @pytest.mark.parametrize("kw,T,few", [
-    (dict(Z=8, Zkv=2), 8, True), (dict(Z=8, Zkv=2), 9, False), (dict(Z=2, Zkv=2), 32, True), (dict(Z=2, Zkv=2), 33, False),
-    (dict(Z=64, Zkv=1), 1, False), (dict(Z=8, Zkv=2, dtype=rsa.RSA_F32), 500, True), (dict(Z=8, Zkv=2, A=256), 8, True), (dict(Z=8, Zkv=2, A=256), 9, False)])
+    (dict(Z=8, Zkv=2), 4, True), (dict(Z=8, Zkv=2), 5, False), (dict(Z=2, Zkv=2, A=192), 16, True), (dict(Z=2, Zkv=2, A=192), 17, False),
+    (dict(Z=2, Zkv=2, A=128), 32, True), (dict(Z=2, Zkv=2, A=128), 33, False), (dict(Z=2, Zkv=2, A=256), 16, True), (dict(Z=2, Zkv=2, A=256), 32, None),
+    (dict(Z=64, Zkv=1), 1, False), (dict(Z=8, Zkv=2, dtype=rsa.RSA_F32), 500, True), (dict(Z=8, Zkv=2, A=256), 9, False)])
 @pytest.mark.parametrize("eight", [False, True])
 def test_few_rows_and_many(rec, kw, T, few, eight):
     d = cache(**kw)
     if eight and d.dtype == rsa.RSA_F32:
         pytest.skip("pools in e4m3 for calls in bf16")
+    few = eight if few is None else few                                              # (heads of 256, 17 to 32 rows)
     names = [k.name for k in chunk(rec, d, T, eight)]
     assert all(("attend_" in n) == few and ("chunk_" in n) != few for n in names), names
     form = numbers(names[0])

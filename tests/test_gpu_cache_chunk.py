@@ -209,7 +209,7 @@ def test_long_and_many(dtype, Z, Zkv, A, page, T, lengths, counts, causal, eight
     call = lambda **k: rsa.cache_attend_chunk(d, Q, *pools, table, i32(lengths), None if counts is None else i32(counts), causal, **kw, **k)
     O, LSE = call(ws=ws)
     rO, rLSE, PV = vectorised_chunk(Q, Kc, Vc, table, lengths, counts, causal)
-    few = dtype == "f32" or T * (Z // Zkv) <= 32
+    few = dtype == "f32" or T * (Z // Zkv) <= 16
     # as in attend_bounds, with |q| |k| of these inputs for the sum of products (powers up to 4 in 8 bits)
     rel = 2 * (A + 4) * F32 * A ** 0.5 * (24 if eight else 6) + 2.0 ** -21 + 2 * max(lengths) * F32
     bound = (rel + (0.0 if dtype == "f32" else 2.0 ** -15 if few else 2.0 ** -8)) * PV + STEP[dtype] * rO.abs()
