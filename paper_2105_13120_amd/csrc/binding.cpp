@@ -14,6 +14,7 @@
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <algorithm>
 #include <array>
 
 #include "rsa.h"
@@ -408,7 +409,8 @@ PyObject *cache_append(Call &c) {
 
 // desc, T, Kc, Vc, table, lengths, counts, K, V, Ks, Vs
 PyObject *cache_read(Call &c) {
-  const rsa_cache_desc &d = *c.cd;
+  rsa_cache_desc d = *c.cd;
+  if (!c.given(7) && !c.given(8)) std::fill_n(d.kv_stride, 3, 0);  // (new results are dense, whatever strides appended tensors have)
   const long long T = PyLong_AsLongLong(c.args[1]);
   if (T == -1 && PyErr_Occurred()) throw Refused{};
   if (T < 1 || T > INT32_MAX) refuse(1, "a number of tokens expected");
@@ -421,7 +423,7 @@ PyObject *cache_read(Call &c) {
   for (int i = 0; i < 2; ++i) {
     if (!c.given(7 + i)) {
       for (int k = 0; k < 3; ++k)
-        if (d.kv_stride[k] != 0) refuse(7 + i, "a result with strides has to be given");
+        if (d.kv_stride[k] != 0) refuse(7 + i, "both results or none expected: a new one would not have the other's strides");
       const auto o = c.tensor(2).options().dtype(type_of(d.dtype));
       out[i] = at::empty(shape, o);
     } else {

@@ -389,7 +389,8 @@ def cache_append(desc, K, V, Kc, Vc, table, lengths, counts=None, first=None, in
 
 def cache_read(desc, T, Kc, Vc, table, lengths, counts=None, K=None, V=None, Ks=None, Vs=None):
     """rsa_cache_read: the slots lengths - counts .. lengths of every sequence (counts None: T) as K, V (B, Zkv, T, A), zero where they
-    are not held.  Rows behind a sequence's count are left as they are; in a new tensor they are zero."""
+    are not held, with the descriptor's strides of K where they are given, else dense.  Rows behind a sequence's count are left as they
+    are; in a new tensor they are zero."""
     return _done(_native().cache_read(desc, T, Kc, Vc, table, lengths, counts, K, V, Ks, Vs))
 
 

@@ -209,7 +209,7 @@ def test_numbers_of_tokens_and_strides():
         rsa.cache_attend_chunk(d, x["Q"][:, :, 0], *pools, **s)
     wide = torch.zeros(2, 3, 2, 64, dtype=BF).transpose(1, 2)                         # tokens with their heads side by side
     d = rsa.make_cache_desc(x["Kc"], x["table"], 4, K=wide)
-    for kw in (dict(), dict(K=wide), dict(V=wide), dict(K=wide, V=x["V"])):           # new tensors would not have these strides
+    for kw in (dict(K=wide), dict(V=wide), dict(K=wide, V=x["V"])):                   # a new tensor would not have these strides
         with pytest.raises(ValueError, match="argument"):
             rsa.cache_read(d, 3, *pools, **kw, **s)
     d, _ = tensors()

@@ -284,3 +284,30 @@ def test_captured_and_replayed_with_other_lengths(shape):
         got = [x.clone() for x in (qr, O, LSE, rk, rv)]
         step()
         assert all(torch.equal(x, y) for x, y in zip(got, (qr, O, LSE, rk, rv)))
+
+
+@pytest.mark.parametrize("eight", [False, True])
+def test_appended_slices_and_new_dense_results_by_one_descriptor(eight):
+    """Keys and values as slices of one projection output, appended and read back by the same descriptor: results that are given have its
+    strides, new ones are dense."""
+    rng = np.random.default_rng(51)
+    B, Z, Zkv, T, A, page = 2, 4, 2, 33, 64, 16
+    x = normal(rng, (B, T, Z + 2 * Zkv, A), "bf16").cuda().permute(0, 2, 1, 3)
+    Q, K, V = x[:, :Z], x[:, Z:Z + Zkv], x[:, Z + Zkv:]
+    table = torch.arange(6, dtype=torch.int32, device="cuda").reshape(B, 3)
+    dt = torch.float8_e4m3fn if eight else torch.bfloat16
+    Kc, Vc = (torch.zeros(6, Zkv, page, A, dtype=torch.uint8 if eight else dt, device="cuda").view(dt) for _ in range(2))
+    s = {k: torch.zeros(6, Zkv, page, dtype=torch.uint8, device="cuda") for k in ("Ks", "Vs")} if eight else {}
+    n = torch.tensor([T, 20], dtype=torch.int32, device="cuda")
+    d = rsa.make_cache_desc(Kc, table, Z, Q=Q, K=K)
+    rsa.cache_append(d, K, V, Kc, Vc, table, n, n, **s)
+    k, v = rsa.cache_read(d, T, Kc, Vc, table, n, n, **s)
+    assert k.is_contiguous() and v.is_contiguous() and k.shape == (B, Zkv, T, A)
+    ref = rsa.cache_read(rsa.make_cache_desc(Kc, table, Z), T, Kc, Vc, table, n, n, **s)
+    assert torch.equal(k, ref[0]) and torch.equal(v, ref[1]) and (k[1, :, 20:] == 0).all()
+    if not eight:
+        assert torch.equal(k[0], K[0]) and torch.equal(v[1, :, :20], V[1, :, :20])
+    y = torch.full_like(x, 7.0)
+    rsa.cache_read(d, T, Kc, Vc, table, n, n, K=y[:, Z:Z + Zkv], V=y[:, Z + Zkv:], **s)
+    assert torch.equal(y[0, Z:Z + Zkv], k[0]) and torch.equal(y[1, Z + Zkv:, :20], v[1, :, :20])
+    assert (y[:, :Z] == 7).all() and (y[1, Z:, 20:] == 7).all()
