@@ -1,16 +1,16 @@
 // Attention of several new tokens per sequence to the paged cache (rsa_cache_attend_chunk), bf16, pools in bf16 or e4m3.
 //
 // The rows of a key head are (token, query head) pairs, token by token with the group's heads side by side, so that all of them share
-// the tiles of keys and values: a work-group owns 32 QB RW rows (RW waves) and walks the slots in tiles of 64, one pass with the
-// running maximum and sum:
+// the tiles of keys and values: a work-group owns 32 QB rows for each of its RW waves, or KS of them, and walks the slots in tiles of 64, one pass
+// with the running maximum and sum:
 //   S^T = K Q^T      A operand: rows of the K tile from LDS, B operand: Q^T in registers
 //   softmax on S^T   lane l owns row l % 32, so maximum and sum are in-lane but for one exchange of the halves
 //   O^T += V^T P^T   A operand: V^T by transpose reads, B operand: P^T straight from the accumulators, rounded to bf16
-// P is rounded once, to 2^-9 of itself, which for many keys errs as much as the stored O's own rounding does (three parts of P, as the kernels for few rows
-// have them, would triple half of the matrix work, which is what bounds this kernel).
+// P is rounded once, by 2^-8 of itself at most, which for many keys errs as much as the stored O's own rounding does (three parts of P, as the kernels for
+// few rows have them, would triple half of the matrix work).
 // Tiles come into LDS by direct loads from wherever their slots' pages are, a slot per lane looked up one tile further ahead; pools in
 // e4m3 come through registers, where what they stand for is formed exactly in bf16, once for all rows of the work-group.
-// Bound by the matrix cores: 2048 tokens of 65536 slots, 32 query, 8 key heads of 128, run at 1.07 to 1.13 PFLOP/s from one GPU to another, where
+// Bound by the matrix cores, busy in 55 % of the cycles, and the vector ALU, busy with softmax in 44 %: 2048 tokens of 65536 slots, 32 query, 8 key heads of 128, run at 1.07 to 1.13 PFLOP/s from one GPU to another, where
 // a product of two 8192 x 8192 matrices by the library does 1.23; prompts of up to 2048 tokens at 0.58, of which a work-group's start and end, when
 // the matrix cores wait, take a third.
 // Tried: work-groups that stay and ask for the next item's first tile ahead (1954 -> 2172 us, prompts 126 -> 142); loads a tile and a half ahead with two
@@ -176,7 +176,6 @@ __global__ void __launch_bounds__(64 * RW, AH <= 2 || RW == 8 ? 2 : 1) chunk_ker
   constexpr bool RAW = EIGHT && RW == 8 && AH > 2;
   // (two buffers, each an object of its own, so that the compiler sees that loads into one miss the reads of the other)
   __shared__ __attribute__((aligned(16))) unsigned char K0[AH][kTileBytes], K1[AH][kTileBytes], V0[AH][kTileBytes], V1[AH][kTileBytes];
-
   __shared__ float2 shared_ends[KS == 2 ? BM : 1];
 
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
