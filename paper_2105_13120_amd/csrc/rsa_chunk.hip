@@ -694,6 +694,7 @@ __global__ void __launch_bounds__(256) chunk_join_kernel(ChunkArgs a, int BM) {
 struct ChunkPlan {
   bool few;         // by 16 or 32 rows at a time, from memory to the operands (rsa_cache.hip)
   int qb, rw;       // 32-row blocks of a wave, waves of different rows
+  int rows;         // of a work-group, 32 qb rw: the row tiles, the parts' places and their join go by it
   int tiles, parts; // row tiles of a key head; parts of a walk at most
 };
 ChunkPlan plan_of(const CacheDims &d, int T, bool eight) {
@@ -704,13 +705,14 @@ ChunkPlan plan_of(const CacheDims &d, int T, bool eight) {
   p.qb = 1; const int64_t large = heads * ((rows + 255) / 256), slots = (int64_t)d.width * d.page;
   p.rw = rows <= 64 ? 2 : 4;
   if (d.A >= 192 ? rows > 128 : d.A == 128 && (large >= 512 || (large >= 256 && slots >= 4 * (int64_t)T))) p.rw = 8;
-  if (d.A == 64 && large >= 512) p.qb = 2;
-  p.tiles = (int)((rows + 32 * p.qb * p.rw - 1) / (32 * p.qb * p.rw));
+  if (d.A == 64 && p.rw == 4 && large >= 512) p.qb = 2;  // (two waves' rows are not enough for 64 a wave)
+  p.rows = 32 * p.qb * p.rw;
+  p.tiles = (int)((rows + p.rows - 1) / p.rows);
   // Parts.  None where the walks are short for a full chip, where one sequence alone fills two rounds of places (one or two work-groups on a
   // CU), where the only one fills its rounds; else up to eight rounds of them, eight tiles and more a part, results within 512 MB.
   const int64_t wgs = heads * p.tiles, walk = (slots + kTileKeys - 1) / kTileKeys;
   const int64_t places = p.rw == 8 || d.A > 128 ? kCUs : 2 * kCUs;
-  const int64_t room = (512LL << 20) / (wgs * 32 * p.qb * p.rw * (d.A + 2) * 4), want = (8 * places + wgs - 1) / wgs;
+  const int64_t room = (512LL << 20) / (wgs * p.rows * (d.A + 2) * 4), want = (8 * places + wgs - 1) / wgs;
   const int64_t most = std::min<int64_t>(std::min<int64_t>(walk / 8, room), 32), rounds = (wgs + places - 1) / places;
   const bool whole = d.B > kSorted || (wgs >= places && walk < 64) || wgs / d.B >= 2 * places || (d.B == 1 && wgs * 20 >= rounds * places * 17);
   p.parts = whole ? 1 : (int)(want < most ? want : most > 1 ? most : 1);
@@ -718,16 +720,18 @@ ChunkPlan plan_of(const CacheDims &d, int T, bool eight) {
 }
 
 template <int AH, int QB, int RW, int KS>
-void launch_chunk(const ChunkArgs &a, const ChunkPlan &p, hipStream_t st) {
+hipError_t launch_chunk(const ChunkArgs &a, const ChunkPlan &p, hipStream_t st) {
+  if (p.rows != 32 * QB * RW / KS) return hipErrorInvalidConfiguration;  // (not the plan's form)
   // (128 rows of heads of 256 in bf16: see plan_of)
   constexpr bool apart = AH == 4 && RW == 8 && KS == 2;
   const unsigned grid = (unsigned)(a.by_heads.d * p.tiles * p.parts);
   if (a.Ks) chunk_kernel<AH, QB, RW, KS, true><<<grid, 64 * RW, 0, st>>>(a);
   else if constexpr (apart) chunk_kernel<AH, QB, 4, 1, false><<<grid, 256, 0, st>>>(a);
   else chunk_kernel<AH, QB, RW, KS, false><<<grid, 64 * RW, 0, st>>>(a);
+  return hipSuccess;
 }
 template <int AH>
-void launch_chunk(const ChunkArgs &a, const ChunkPlan &p, hipStream_t st) {
+hipError_t launch_chunk(const ChunkArgs &a, const ChunkPlan &p, hipStream_t st) {
   if constexpr (AH > 2) {
     if (p.rw == 4) return launch_chunk<AH, 1, 8, 2>(a, p, st);
   }
@@ -738,19 +742,21 @@ void launch_chunk(const ChunkArgs &a, const ChunkPlan &p, hipStream_t st) {
   if constexpr (AH >= 2) {
     if (p.rw == 8) return launch_chunk<AH, 1, 8, 1>(a, p, st);
   }
-  if constexpr (AH <= 2) launch_chunk<AH, 1, 4, 1>(a, p, st);
+  if constexpr (AH <= 2) return launch_chunk<AH, 1, 4, 1>(a, p, st);
+  return hipErrorInvalidConfiguration;
 }
 template <int AH>
-void launch_all(const ChunkArgs &a, const ChunkPlan &p, hipStream_t st) {
-  launch_chunk<AH>(a, p, st);
-  const int BM = 32 * p.qb * p.rw;
-  if (p.parts > 1) chunk_join_kernel<AH><<<(unsigned)(a.by_heads.d * a.tiles * (BM / 32)), 256, 0, st>>>(a, BM);
+hipError_t launch_all(const ChunkArgs &a, const ChunkPlan &p, hipStream_t st) {
+  const hipError_t e = launch_chunk<AH>(a, p, st);
+  if (e != hipSuccess) return e;
+  if (p.parts > 1) chunk_join_kernel<AH><<<(unsigned)(a.by_heads.d * a.tiles * (p.rows / 32)), 256, 0, st>>>(a, p.rows);
+  return hipGetLastError();
 }
 
 }  // namespace
 
 namespace {
-size_t part_rows(const CacheDims &d, const ChunkPlan &p) { return (size_t)p.parts * d.B * d.Zkv * p.tiles * 32 * p.qb * p.rw; }
+size_t part_rows(const CacheDims &d, const ChunkPlan &p) { return (size_t)p.parts * d.B * d.Zkv * p.tiles * p.rows; }
 }  // namespace
 
 size_t chunk_workspace_bytes(const CacheDims &d, int T) {
@@ -782,12 +788,11 @@ hipError_t cache_attend_chunk(const CacheDims &d, const CachePools &c, int T, in
     a.part_ml = a.part_o + part_rows(d, p) * d.A;
   }
   switch (d.A) {
-    case 64: launch_all<1>(a, p, st); break;
-    case 128: launch_all<2>(a, p, st); break;
-    case 192: launch_all<3>(a, p, st); break;
-    default: launch_all<4>(a, p, st);
+    case 64: return launch_all<1>(a, p, st);
+    case 128: return launch_all<2>(a, p, st);
+    case 192: return launch_all<3>(a, p, st);
+    default: return launch_all<4>(a, p, st);
   }
-  return hipGetLastError();
 }
 
 }  // namespace rsa
