@@ -16,7 +16,8 @@
 // Tried: work-groups that stay and ask for the next item's first tile ahead (1954 -> 2172 us, prompts 126 -> 142); loads a tile and a half ahead with two
 // barriers (3 to 9 % slower but for short walks).
 // Slots that are not seen: a score is -inf, and a value is cleared in LDS, since 0 times what lies there could be NaN.  Where rows of a
-// work-group see different slots of a tile, infinite and NaN values are taken out likewise and given to the rows that see them.
+// work-group see different slots of a tile, infinite and NaN values are taken out likewise and given to the rows that see them.  What such a
+// row has is infinite from then on, whatever its sums so far weigh beside later ones (Weight).
 #include "rsa_cache_tokens.h"
 #include "rsa_fused_tile.h"
 #include "rsa_kernels.h"
@@ -52,6 +53,14 @@ __device__ __forceinline__ uint32_t slots_of(const ChunkArgs &a, int length) {
   const int most = a.width * (int)a.by_page.d;
   return (uint32_t)(length < 0 ? 0 : length < most ? length : most);
 }
+
+// 2^x, x <= 0, as two factors that are not 0: an infinity times 0 were NaN, where a row had seen no key yet (x = -inf) or none near the largest score.
+// From -126 on, below which exp2 gives 0, the second is 1; finite numbers times both become less than 2^-124 at x <= -252.
+struct Weight {
+  float a, b;
+  __device__ __forceinline__ explicit Weight(float x)
+      : a(__builtin_amdgcn_exp2f(fmaxf(x, -126.f))), b(__builtin_amdgcn_exp2f(fminf(fmaxf(x + 126.f, -126.f), 0.f))) {}
+};
 
 // What a call's work-groups take: a row tile of a key head of a sequence and, where its walk is divided, one of its parts.
 struct Item {
@@ -483,14 +492,14 @@ __global__ void __launch_bounds__(64 * RW, AH <= 2 || RW == 8 ? 2 : 1) chunk_ker
           // (a row that has seen no key yet keeps mc = 0)
           const float mn = fmaxf(m[qb], tm[qb]);
           const bool any = mn > -INFINITY;
-          const float alpha = any ? __builtin_amdgcn_exp2f((m[qb] - mn) * a.cl2) : 1.0f;
+          const Weight w(any ? (m[qb] - mn) * a.cl2 : 0.f);
           m[qb] = mn;
           mc[qb] = any ? mn * a.cl2 : 0.f;
-          l[qb] *= alpha;
+          l[qb] = l[qb] * w.a * w.b;
 #pragma unroll
           for (int db = 0; db < 2 * AH; ++db)
 #pragma unroll
-            for (int v = 0; v < 16; ++v) o[db][qb][v] *= alpha;
+            for (int v = 0; v < 16; ++v) o[db][qb][v] = o[db][qb][v] * w.a * w.b;
         }
       }
       // ---- P^T = exp2(S^T cl2 - m cl2), packed to bf16 as the B operand
@@ -550,8 +559,9 @@ __global__ void __launch_bounds__(64 * RW, AH <= 2 || RW == 8 ? 2 : 1) chunk_ker
     __syncthreads();
     if (share == 1) return;
     const float2 x = *ends;
-    const float M = fmaxf(top, x.x), w0 = top > -INFINITY ? __builtin_amdgcn_exp2f(top - M) : 0.f, w1 = x.x > -INFINITY ? __builtin_amdgcn_exp2f(x.x - M) : 0.f;
     const bool one = top > -INFINITY, two = x.x > -INFINITY;
+    const float M = fmaxf(top, x.x);
+    const Weight w0(top - M), w1(x.x - M);  // (of a share that has seen keys)
 #pragma unroll
     for (int db = 0; db < 2 * AH; ++db)
 #pragma unroll
@@ -559,11 +569,11 @@ __global__ void __launch_bounds__(64 * RW, AH <= 2 || RW == 8 ? 2 : 1) chunk_ker
         const f32x4 y = reinterpret_cast<const f32x4 *>(other)[(db * 4 + g) * 64 + lane];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const float z = one ? o[db][0][g * 4 + e] * w0 : 0.f;
-          o[db][0][g * 4 + e] = two ? fmaf(w1, y[e], z) : z;
+          const float z = one ? o[db][0][g * 4 + e] * w0.a * w0.b : 0.f;
+          o[db][0][g * 4 + e] = two ? fmaf(w1.a, y[e] * w1.b, z) : z;
         }
       }
-    l[0] = half == 0 ? (one ? lt * w0 : 0.f) + (two ? x.y * w1 : 0.f) : 0.f;
+    l[0] = half == 0 ? (one ? lt * w0.a * w0.b : 0.f) + (two ? x.y * w1.a * w1.b : 0.f) : 0.f;
     mc[0] = one || two ? M : 0.f;
   }
 
@@ -645,12 +655,12 @@ __global__ void __launch_bounds__(256) chunk_join_kernel(ChunkArgs a, int BM) {
     f32x4 y[2 * AH];
 #pragma unroll
     for (int db = 0; db < 2 * AH; ++db) y[db] = po[s * step * (A / 4) + db * 256];
-    const float w = x.x > -INFINITY ? __builtin_amdgcn_exp2f(x.x - M) : 0.f;
-    sum = x.x > -INFINITY ? fmaf(w, x.y, sum) : sum;
+    const Weight w(x.x - M);
+    sum = x.x > -INFINITY ? fmaf(w.a, x.y * w.b, sum) : sum;
 #pragma unroll
     for (int db = 0; db < 2 * AH; ++db)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) o[db][e] = x.x > -INFINITY ? fmaf(w, y[db][e], o[db][e]) : o[db][e];
+      for (int e = 0; e < 4; ++e) o[db][e] = x.x > -INFINITY ? fmaf(w.a, y[db][e] * w.b, o[db][e]) : o[db][e];
   }
   const bool there = row < have;
   const float inv = sum != 0.f ? 1.0f / sum : 0.f;
