@@ -693,7 +693,9 @@ __global__ void __launch_bounds__(256) chunk_join_kernel(ChunkArgs a, int BM) {
 // 4 x 16 key heads of 256, 82 -> 85 and 112 -> 97), and of 128 where these work-groups fill the chip twice, or
 // once with walks of about one length (the same 512 -> 501, 64k slots 2145 -> 1973, 8 x 512 of 8192 572 -> 541, in e4m3 578 -> 527; but 2048 of
 // 2048 57 -> 65, 512 of 8192 84 -> 97, 4 x 1024 of 1024, 16 key heads, 36 -> 43).  Heads of 64 take 64 rows a wave where these fill the chip (eight
-// waves of 32: 307 -> 341).
+// waves of 32: 307 -> 341).  Up to 128 rows of a key head half of such a work-group would have none of its own (32 and 64 sequences of 4096, 8 key heads, 4 query heads
+// each, us, with and without, bf16 and e4m3: 16 tokens, heads of 128, 164 -> 114 and 157 -> 88; 24 tokens, heads of 128, 324 -> 249 and 308 -> 213, of 64
+// 196 -> 133 and 214 -> 150).
 // Fewer rows leave waves without any, or CUs with few waves.  Two waves then share 32 rows, each with half of a tile's keys, and are joined at the end: up to
 // 64 rows on four waves (16 tokens of each of 16 sequences of 4096, 4 query heads a key head, us, before and with it, bf16 and e4m3: heads of 64
 // 37 -> 34, 39 -> 32, of 128 68 -> 65, 58 -> 46, of 192 114 -> 101, 115 -> 86, of 256 146 -> 127, 198 -> 127), up to 128 of long heads on eight (32 tokens:
@@ -712,10 +714,10 @@ ChunkPlan plan_of(const CacheDims &d, int T, bool eight) {
   const int64_t rows = (int64_t)T * (d.Z / d.Zkv), heads = (int64_t)d.B * d.Zkv;
   p.few = d.dtype != RSA_BF16 || rows <= (d.A == 128 || (d.A == 256 && eight) ? 32 : 16);
   if (p.few) return p;
-  p.qb = 1; const int64_t large = heads * ((rows + 255) / 256), slots = (int64_t)d.width * d.page;
+  p.qb = 1; const int64_t large = rows > 128 ? heads * ((rows + 255) / 256) : 0, slots = (int64_t)d.width * d.page;
   p.rw = rows <= 64 ? 2 : 4;
   if (d.A >= 192 ? rows > 128 : d.A == 128 && (large >= 512 || (large >= 256 && slots >= 4 * (int64_t)T))) p.rw = 8;
-  if (d.A == 64 && p.rw == 4 && large >= 512) p.qb = 2;  // (two waves' rows are not enough for 64 a wave)
+  if (d.A == 64 && large >= 512) p.qb = 2;
   p.rows = 32 * p.qb * p.rw;
   p.tiles = (int)((rows + p.rows - 1) / p.rows);
   // Parts.  None where the walks are short for a full chip, where one sequence alone fills two rounds of places (one or two work-groups on a

@@ -30,3 +30,15 @@ def test_a_work_groups_rows(rec, A, B, Zkv, group, T, slots, eight):  # noqa: F8
         return
     assert len(k) == 2 and k[1].grid == (heads * tiles * rows // 32, 1, 1)
     assert need >= 64 * 4 + parts * heads * tiles * rows * (A + 2) * 4
+
+
+@pytest.mark.parametrize("A", [64, 128])
+@pytest.mark.parametrize("B,Zkv", [(1, 2), (32, 8), (64, 8), (64, 16), (128, 16)])
+@pytest.mark.parametrize("slots", [128, 8192])
+@pytest.mark.parametrize("eight", [False, True])
+def test_few_rows_have_no_larger_work_groups_however_many_heads_there_are(rec, A, B, Zkv, slots, eight):  # noqa: F811
+    d = cache(A=A, B=B, Z=Zkv * 4, Zkv=Zkv, page=1, width=slots, pages=B * slots)
+    for T in (9, 16):
+        assert numbers(chunk(rec, d, T, eight)[0].name) == [A // 64, 1, 4, 2, eight]
+    for T in (17, 32):
+        assert numbers(chunk(rec, d, T, eight)[0].name) == [A // 64, 1, 4, 1, eight]
