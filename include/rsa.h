@@ -399,8 +399,8 @@ int rsa_cache_read(const rsa_cache_desc *d, int32_t T, int32_t pad, const void *
  * is that of slot lengths[b] - counts[b] + t and sees the slots that are held up to its own or, without `causal`, all that are held (a rank
  * whose share of the cache lies in front of the tokens).  A row that sees no key gets O = 0 and LSE = -inf; rows of tokens that are not there
  * are left as they are or, by the bits of pad, get these as well: 1 in O, 2 in LSE.  Pool memory outside the slots that a row
- * sees does not reach its result, whatever it holds: not one of an infinite or NaN key or value either.  Ks, Vs as in rsa_cache_read.  fp32, and bf16 up to 16 rows of a key head (T Z/Zkv), as rsa_cache_attend;
- * beyond that (heads of 128: beyond 32) P is rounded to bf16 once, as in rsa_forward.  T * Z must be below 2^31, B * Z * T * A at most 2^34.  ws:
+ * sees does not reach its result, whatever it holds: not one of an infinite or NaN key or value either.  Ks, Vs as in rsa_cache_read.  fp32, and bf16 up to 32 rows of a key head (T Z/Zkv), as rsa_cache_attend;
+ * beyond that P is rounded to bf16 once, as in rsa_forward.  T * Z must be below 2^31, B * Z * T * A at most 2^34.  ws:
  * rsa_cache_chunk_workspace_bytes(d, T) bytes, as for rsa_cache_attend.
  * Results of shares are joined by rsa_cache_join with Z * T for Z: rows are rows. */
 size_t rsa_cache_chunk_workspace_bytes(const rsa_cache_desc *d, int32_t T);

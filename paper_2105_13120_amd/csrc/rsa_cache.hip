@@ -305,11 +305,6 @@ __device__ __forceinline__ float xrow_max(float x) {
   return fmaxf(__builtin_bit_cast(float, a), __builtin_bit_cast(float, b));
 }
 
-// The eight bits of x that a bf16 number has, cut off behind.
-__device__ __forceinline__ float first_bits(float x) {
-  return __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, x) & 0xffff0000u);
-}
-
 __device__ __forceinline__ uint32_t length_of(const AttendArgs &args, int b) {
   const int n = args.lengths[b], most = args.width * (int)args.by_page.d;
   return (uint32_t)(n < 0 ? 0 : n < most ? n : most);
@@ -644,28 +639,19 @@ struct Attend : ChunkRows<KIND, NQ> {
   }
   __device__ __forceinline__ void products(const f32x4 (&p)[NQ][KT], uint32_t seen) {
     if constexpr (kHalf) {
-      // The matrix core takes bf16: a probability goes to it as three, its first eight bits, the next eight and the rest, all 24 of
-      // it (as two, 2^-16 of it is lost, which shows where values cancel.  Long walks from HBM take the same, whose matrix cores wait for
-      // memory; one of 200 slots 5.2 and 5.3 us, 16 of 8192 from the infinity cache with 32 queries a key head 21.3 and 22.3).  No part is
-      // 0 where the probability is not (exp2 gives none below 2^-126): times an infinite value that were NaN.  The later ones are at
-      // least the smallest number that bf16 has, 2^-133, which the matrix cores take as it is: less than 2^-24 of a probability of 2^-108.
+      // Probabilities as three numbers each (as two, 2^-16 of one is lost, which shows where values cancel.  Long walks from HBM take the same,
+      // whose matrix cores wait for memory; one of 200 slots 5.2 and 5.3 us, 16 of 8192 from the infinity cache with 32 queries a key head 21.3 and 22.3).
       bf16x8 pb[NQ][3];
 #pragma unroll
       for (int x = 0; x < NQ; ++x) {
         u32x4 w[3];
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-          float part[3][2];
+          const f32x4 y = p[x][k >> 1 ? KT - 1 : 0];
+          uint32_t parts[3];
+          three_parts(y[2 * (k & 1)], y[2 * (k & 1) + 1], parts);
 #pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            const float y = p[x][k >> 1 ? KT - 1 : 0][2 * (k & 1) + e], r = y - first_bits(y);
-            part[0][e] = y;
-            part[1][e] = __builtin_amdgcn_fmed3f(r, 0x1p-133f, y);
-            part[2][e] = __builtin_amdgcn_fmed3f(r - first_bits(r), 0x1p-133f, y);
-          }
-#pragma unroll
-          for (int i = 0; i < 3; ++i)
-            w[i][k] = __builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, part[i][1]), __builtin_bit_cast(uint32_t, part[i][0]), 0x07060302u);
+          for (int i = 0; i < 3; ++i) w[i][k] = parts[i];
         }
 #pragma unroll
         for (int i = 0; i < 3; ++i) pb[x][i] = __builtin_bit_cast(bf16x8, w[i]);

@@ -114,6 +114,28 @@ inline uint32_t token_grid(TokenArgs &a, int B, int T, const int32_t *counts, in
   return (uint32_t)(items < most ? items : most);
 }
 
+// The eight bits of x that a bf16 number has, cut off behind.
+__device__ __forceinline__ float first_bits(float x) {
+  return __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, x) & 0xffff0000u);
+}
+// The matrix core takes bf16: a probability goes to it as three, its first eight bits, the next eight and the rest, all 24 of it; here
+// of two probabilities.  No part is 0 where the probability is not (exp2 gives none below 2^-126): times an infinite value that were
+// NaN.  The later ones are at least the smallest number that bf16 has, 2^-133, which the matrix cores take as it is: less than 2^-24 of a
+// probability of 2^-108.
+__device__ __forceinline__ void three_parts(float a, float b, uint32_t (&w)[3]) {
+  const float y[2] = {a, b};
+  float part[3][2];
+#pragma unroll
+  for (int e = 0; e < 2; ++e) {
+    const float r = y[e] - first_bits(y[e]);
+    part[0][e] = y[e];
+    part[1][e] = __builtin_amdgcn_fmed3f(r, 0x1p-133f, y[e]);
+    part[2][e] = __builtin_amdgcn_fmed3f(r - first_bits(r), 0x1p-133f, y[e]);
+  }
+#pragma unroll
+  for (int i = 0; i < 3; ++i) w[i] = __builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, part[i][1]), __builtin_bit_cast(uint32_t, part[i][0]), 0x07060302u);
+}
+
 // Elements in e4m3 times a power of two (a float, of which only the exponent counts), as bf16, exactly: two of a dword's, eight.
 __device__ __forceinline__ uint32_t widened2(uint32_t x, float power, bool hi) {
   return hi ? __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, power, true))

@@ -6,8 +6,9 @@
 //   S^T = K Q^T      A operand: rows of the K tile from LDS, B operand: Q^T in registers
 //   softmax on S^T   lane l owns row l % 32, so maximum and sum are in-lane but for one exchange of the halves
 //   O^T += V^T P^T   A operand: V^T by transpose reads, B operand: P^T straight from the accumulators, rounded to bf16
-// P is rounded once, by 2^-8 of itself at most, which for many keys errs as much as the stored O's own rounding does (three parts of P, as the kernels for
-// few rows have them, would triple half of the matrix work).
+// Up to 32 rows of a key head P goes to the matrix cores whole, as three bf16 numbers.  Beyond, it is rounded once, by 2^-8 of itself at most, as in
+// rsa_forward: results err by 2.0 to 2.4e-3 of their RMS, where the rounding of the stored O alone errs by 1.6 to 1.7e-3 (three parts would triple half of the
+// matrix work, which bounds these calls: up to 64 rows, where it bounds them least, 3 to 30 % more time).
 // Tiles come into LDS by direct loads from wherever their slots' pages are, a slot per lane looked up one tile further ahead; pools in
 // e4m3 come through registers, where what they stand for is formed exactly in bf16, once for all rows of the work-group.
 // Bound by the matrix cores, busy in 55 % of the cycles, and the vector ALU, busy with softmax in 44 %: 2048 tokens of 65536 slots, 32 query, 8 key heads of 128, run at 1.07 to 1.13 PFLOP/s from one GPU to another, where
@@ -175,20 +176,24 @@ struct Layout {
   }
 };
 
-// KS: the waves that share a row block's rows, each with its part of a tile's keys
+// KS: the waves that share a row block's rows, two each with half of a tile's keys; four of them for half of the result's columns, too, since
+// probabilities go to the matrix cores with all their bits there, in three parts
 template <int AH, int QB, int RW, int KS, bool EIGHT>
 __global__ void __launch_bounds__(64 * RW, AH <= 2 || RW == 8 ? 2 : 1) chunk_kernel(ChunkArgs a) {
   constexpr int A = 64 * AH, R = 32 * QB, ROWS = RW / KS, BM = R * ROWS, THREADS = 64 * RW;
-  constexpr int KB = KS == 2 || (RW == 8 && (AH == 4 || (AH == 3 && EIGHT))) ? 1 : 2;
+  constexpr int PARTS = KS == 4 ? 3 : 1, COLS = KS == 4 ? 2 : 1, DB = 2 * AH / COLS;  // DB: a wave's blocks of 32 columns
+  constexpr bool SHARED = KS > 1;                                                    // keys
+  constexpr int KB = SHARED || (RW == 8 && (AH == 4 || (AH == 3 && EIGHT))) ? 1 : 2;
   // Long heads' pools in e4m3 wait in LDS (K1, V1) as they are, since registers have no room for them, and are widened into K0 and V0 when their turn
   // comes (2048 tokens of 16384 slots, us: heads of 192 963 -> 764, of 256 1872 -> 1197)
   constexpr bool RAW = EIGHT && RW == 8 && AH > 2;
   // (two buffers, each an object of its own, so that the compiler sees that loads into one miss the reads of the other)
   __shared__ __attribute__((aligned(16))) unsigned char K0[AH][kTileBytes], K1[AH][kTileBytes], V0[AH][kTileBytes], V1[AH][kTileBytes];
-  __shared__ float2 shared_ends[KS == 2 ? BM : 1];
+  __shared__ float2 shared_ends[SHARED ? BM : 1];
 
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int col = lane & 31, half = lane >> 5, block = wave & (ROWS - 1), share = wave / ROWS;
+  const int col = lane & 31, half = lane >> 5, block = wave & (ROWS - 1), share = wave / ROWS & 1;
+  const int side = COLS == 2 ? wave >> 1 : 0;  // its blocks of columns: one of each 64
   // The lane as a number of its own, from which a tile's addresses are worked out anew where registers are scarce (kept over the walk they
   // would be spilled, and a reload waits for the next tile's loads: heads of 256, 2048 tokens of 16384 slots 1117 -> 1083 us, 1024 of 1024 99 -> 85)
   const auto anew = [&]() __attribute__((always_inline)) {
@@ -326,13 +331,13 @@ __global__ void __launch_bounds__(64 * RW, AH <= 2 || RW == 8 ? 2 : 1) chunk_ker
     }
   };
 
-  f32x16 o[2 * AH][QB];
+  f32x16 o[DB][QB];
   float m[QB], mc[QB], l[QB];
 #pragma unroll
   for (int qb = 0; qb < QB; ++qb) {
     m[qb] = -INFINITY; mc[qb] = 0.f; l[qb] = 0.f;
 #pragma unroll
-    for (int db = 0; db < 2 * AH; ++db)
+    for (int db = 0; db < DB; ++db)
 #pragma unroll
       for (int v = 0; v < 16; ++v) o[db][qb][v] = 0.f;
   }
@@ -357,7 +362,14 @@ __global__ void __launch_bounds__(64 * RW, AH <= 2 || RW == 8 ? 2 : 1) chunk_ker
 
   // one tile: start the loads of the next one into (Kn, Vn), compute on (Kt, Vt)
   const auto stage = [&](auto &Kt, auto &Vt, auto &Kn, auto &Vn) __attribute__((always_inline)) {
-    const TileLanes tl(anew());
+    TileLanes tl(anew());
+    if constexpr (COLS == 2) {
+#pragma unroll
+      for (int e = 0; e < 2; ++e) tl.cols_off[0][e] = side ? tl.cols_off[1][e] : tl.cols_off[0][e];
+    }
+    const auto columns = [&](int db, int row) __attribute__((always_inline)) {
+      return COLS == 2 ? tl.read_cols(Vt[db], row, 0) : tl.read_cols(Vt[db >> 1], row, db & 1);
+    };
     now = next;
     const bool more = t + 1 < end;
     if constexpr (RAW) {  // (a lane reads what it has asked for itself)
@@ -402,14 +414,14 @@ __global__ void __launch_bounds__(64 * RW, AH <= 2 || RW == 8 ? 2 : 1) chunk_ker
         for (int qb = 0; qb < QB; ++qb) {
           const uint64_t sees = lim[qb] > k0 ? now.seen & (lim[qb] - k0 < 64 ? (1ull << (lim[qb] - k0)) - 1 : ~0ull) : 0ull;
 #pragma unroll
-          for (int db = 0; db < 2 * AH; ++db) {
+          for (int db = 0; db < DB; ++db) {
             f32x16 n;
 #pragma unroll
             for (int v = 0; v < 16; ++v) n[v] = 0.f;
 #pragma unroll
             for (int kk = 0; kk < 4; ++kk) {
               __builtin_amdgcn_sched_barrier(0);
-              const u32x4 va = __builtin_bit_cast(u32x4, tl.read_cols(Vt[db >> 1], kk * 16, db & 1));
+              const u32x4 va = __builtin_bit_cast(u32x4, columns(db, kk * 16));
               const uint32_t bits = (uint32_t)(sees >> (kk * 16 + half * 4));
               u32x4 w, ones;
 #pragma unroll
@@ -445,8 +457,8 @@ __global__ void __launch_bounds__(64 * RW, AH <= 2 || RW == 8 ? 2 : 1) chunk_ker
 
     // ---- by blocks of 32 keys: both at once or, where the accumulators leave no room for both's scores, one after the other
 #pragma unroll
-    for (int k0th = 0; k0th < 2 / KS; k0th += KB) {
-      const int k1 = KS == 2 ? share : k0th;
+    for (int k0th = 0; k0th < (SHARED ? 1 : 2); k0th += KB) {
+      const int k1 = SHARED ? share : k0th;
       // ---- S^T = K Q^T
       f32x16 s[KB][QB];
       float tm[QB];
@@ -497,13 +509,13 @@ __global__ void __launch_bounds__(64 * RW, AH <= 2 || RW == 8 ? 2 : 1) chunk_ker
           mc[qb] = any ? mn * a.cl2 : 0.f;
           l[qb] = l[qb] * w.a * w.b;
 #pragma unroll
-          for (int db = 0; db < 2 * AH; ++db)
+          for (int db = 0; db < DB; ++db)
 #pragma unroll
             for (int v = 0; v < 16; ++v) o[db][qb][v] = o[db][qb][v] * w.a * w.b;
         }
       }
       // ---- P^T = exp2(S^T cl2 - m cl2), packed to bf16 as the B operand
-      bf16x8 pf[QB][2 * KB];
+      bf16x8 pf[QB][2 * KB][PARTS];
 #pragma unroll
       for (int qb = 0; qb < QB; ++qb)
 #pragma unroll
@@ -516,19 +528,33 @@ __global__ void __launch_bounds__(64 * RW, AH <= 2 || RW == 8 ? 2 : 1) chunk_ker
           }
 #pragma unroll
           for (int u = 0; u < 2; ++u) {
-            const u32x4 w = {pack_bf16(p[u * 8 + 0], p[u * 8 + 1]), pack_bf16(p[u * 8 + 2], p[u * 8 + 3]),
-                             pack_bf16(p[u * 8 + 4], p[u * 8 + 5]), pack_bf16(p[u * 8 + 6], p[u * 8 + 7])};
-            pf[qb][kb * 2 + u] = __builtin_bit_cast(bf16x8, w);
+            u32x4 w[PARTS];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              const float x = p[u * 8 + 2 * k], y = p[u * 8 + 2 * k + 1];
+              if constexpr (PARTS == 3) {
+                uint32_t parts[3];
+                three_parts(x, y, parts);
+#pragma unroll
+                for (int i = 0; i < 3; ++i) w[i][k] = parts[i];
+              } else {
+                w[0][k] = pack_bf16(x, y);
+              }
+            }
+#pragma unroll
+            for (int i = 0; i < PARTS; ++i) pf[qb][kb * 2 + u][i] = __builtin_bit_cast(bf16x8, w[i]);
           }
         }
       // ---- O^T += V^T P^T
 #pragma unroll
-      for (int db = 0; db < 2 * AH; ++db)
+      for (int db = 0; db < DB; ++db)
 #pragma unroll
         for (int kk = 0; kk < 2 * KB; ++kk) {
-          const bf16x8 va = tl.read_cols(Vt[db >> 1], (k1 * 2 + kk) * 16, db & 1);
+          const bf16x8 va = columns(db, (k1 * 2 + kk) * 16);
 #pragma unroll
-          for (int qb = 0; qb < QB; ++qb) o[db][qb] = mfma_32x32x16(va, pf[qb][kk], o[db][qb]);
+          for (int qb = 0; qb < QB; ++qb)
+#pragma unroll
+            for (int i = PARTS - 1; i >= 0; --i) o[db][qb] = mfma_32x32x16(va, pf[qb][kk][i], o[db][qb]);
         }
     }
     if (EIGHT && !RAW && more) store8(next, Kn, Vn);
@@ -544,17 +570,18 @@ __global__ void __launch_bounds__(64 * RW, AH <= 2 || RW == 8 ? 2 : 1) chunk_ker
     }
   }
 
-  if constexpr (KS == 2) {  // the shares of a block's rows together, as parts are
-    float *other = reinterpret_cast<float *>(block == 0 ? K0[0] : block == 1 ? K1[0] : block == 2 ? V0[0] : V1[0]);
+  const int own = COLS == 2 ? side : block & 3;  // the wave's buffer
+  if constexpr (SHARED) {  // the shares of a block's rows together, as parts are
+    float *other = reinterpret_cast<float *>(own == 0 ? K0[0] : own == 1 ? K1[0] : own == 2 ? V0[0] : V1[0]);
     float2 *ends = shared_ends + block * R + col;
     float lt = xhalf_sum(l[0]), top = lt != 0.f ? mc[0] : -INFINITY;
     if (share == 1) {
 #pragma unroll
-      for (int db = 0; db < 2 * AH; ++db)
+      for (int db = 0; db < DB; ++db)
 #pragma unroll
         for (int g = 0; g < 4; ++g)
           reinterpret_cast<f32x4 *>(other)[(db * 4 + g) * 64 + lane] = f32x4{o[db][0][g * 4 + 0], o[db][0][g * 4 + 1], o[db][0][g * 4 + 2], o[db][0][g * 4 + 3]};
-      if (half == 0) *ends = make_float2(top, lt);
+      if (half == 0 && side == 0) *ends = make_float2(top, lt);
     }
     __syncthreads();
     if (share == 1) return;
@@ -563,7 +590,7 @@ __global__ void __launch_bounds__(64 * RW, AH <= 2 || RW == 8 ? 2 : 1) chunk_ker
     const float M = fmaxf(top, x.x);
     const Weight w0(top - M), w1(x.x - M);  // (of a share that has seen keys)
 #pragma unroll
-    for (int db = 0; db < 2 * AH; ++db)
+    for (int db = 0; db < DB; ++db)
 #pragma unroll
       for (int g = 0; g < 4; ++g) {
         const f32x4 y = reinterpret_cast<const f32x4 *>(other)[(db * 4 + g) * 64 + lane];
@@ -585,11 +612,11 @@ __global__ void __launch_bounds__(64 * RW, AH <= 2 || RW == 8 ? 2 : 1) chunk_ker
     for (int qb = 0; qb < QB; ++qb) {
       const float lt = xhalf_sum(l[qb]);
 #pragma unroll
-      for (int db = 0; db < 2 * AH; ++db)
+      for (int db = 0; db < DB; ++db)
 #pragma unroll
         for (int g = 0; g < 4; ++g)
-          po[((qb * 2 * AH + db) * 4 + g) * 64] = f32x4{o[db][qb][g * 4 + 0], o[db][qb][g * 4 + 1], o[db][qb][g * 4 + 2], o[db][qb][g * 4 + 3]};
-      if (half == 0) ml[qb * 32] = make_float2(lt != 0.f ? mc[qb] : -INFINITY, lt);
+          po[((qb * 2 * AH + (COLS == 2 ? 2 * db + side : db)) * 4 + g) * 64] = f32x4{o[db][qb][g * 4 + 0], o[db][qb][g * 4 + 1], o[db][qb][g * 4 + 2], o[db][qb][g * 4 + 3]};
+      if (half == 0 && side == 0) ml[qb * 32] = make_float2(lt != 0.f ? mc[qb] : -INFINITY, lt);
     }
     return;
   }
@@ -602,20 +629,20 @@ __global__ void __launch_bounds__(64 * RW, AH <= 2 || RW == 8 ? 2 : 1) chunk_ker
     const float lt = xhalf_sum(l[qb]);
     inv[qb] = lt != 0.f ? 1.0f / lt : 0.f;
     const int row = row0 + block * R + qb * 32 + col;
-    if (half == 0 && (row < rows || ((a.pad & 2) && row < rows_all))) {
+    if (half == 0 && side == 0 && (row < rows || ((a.pad & 2) && row < rows_all))) {
       const int token = (int)a.by_group((uint32_t)row), z = (int)h * group + row - token * group;
       a.LSE[((int64_t)b * a.Z + z) * a.T + token] = lt != 0.f && row < rows ? (mc[qb] + __builtin_amdgcn_logf(lt)) * kLn2 : -INFINITY;
     }
   }
-  unsigned char *ot = ((block & 3) == 0 ? K0[0] : (block & 3) == 1 ? K1[0] : (block & 3) == 2 ? V0[0] : V1[0]) + (block >> 2) * 32 * 128;
+  unsigned char *ot = (own == 0 ? K0[0] : own == 1 ? K1[0] : own == 2 ? V0[0] : V1[0]) + (block >> 2) * 32 * 128;
 #pragma unroll
   for (int ah = 0; ah < AH; ++ah) {
 #pragma unroll
-    for (int qb = 0; qb < QB; ++qb) stage_block_T(ot, qb * 32, o[2 * ah][qb], o[2 * ah + 1][qb], inv[qb], lane);
+    for (int qb = 0; qb < QB; ++qb) stage_block_T(ot, qb * 32, o[COLS == 2 ? ah : 2 * ah][qb], o[COLS == 2 ? ah : 2 * ah + 1][qb], inv[qb], lane);
 #pragma unroll
     for (int it = 0; it < R / 8; ++it) {
       const int r = it * 8 + (lane >> 3), cc = lane & 7, row = row0 + block * R + r;
-      if (row < rows || ((a.pad & 1) && row < rows_all)) {
+      if ((COLS == 1 || cc >> 2 == side) && (row < rows || ((a.pad & 1) && row < rows_all))) {
         const int token = (int)a.by_group((uint32_t)row), z = (int)h * group + row - token * group;
         *reinterpret_cast<u32x4 *>(a.O + (int64_t)b * a.os[0] + (int64_t)z * a.os[1] + (int64_t)token * a.os[2] + ah * 64 + cc * 8) =
             row < rows ? *reinterpret_cast<const u32x4 *>(ot + tile_off(r, cc)) : u32x4{0, 0, 0, 0};
@@ -700,9 +727,12 @@ __global__ void __launch_bounds__(256) chunk_join_kernel(ChunkArgs a, int BM) {
 // 64 rows on four waves (16 tokens of each of 16 sequences of 4096, 4 query heads a key head, us, before and with it, bf16 and e4m3: heads of 64
 // 37 -> 34, 39 -> 32, of 128 68 -> 65, 58 -> 46, of 192 114 -> 101, 115 -> 86, of 256 146 -> 127, 198 -> 127), up to 128 of long heads on eight (32 tokens:
 // heads of 192 118 -> 107, 115 -> 98, of 256 in e4m3 195 -> 165; in bf16 these spill, 148 -> 181, and take four waves, one a row block).
-// Up to 16 rows go straight from memory to the operands; up to 32 in heads of 128 and, in e4m3, of 256, where the others' ways of 32 rows are slower (8 tokens
-// of each of 16 sequences of 4096, 4 query heads a key head, us, so and by tiles in LDS, bf16 and e4m3: heads of 64 47 and 34, 42 and 32, of 128 66 and
-// 64, 47 and 45, but of 64 sequences of 1024 67 and 84, 47 and 77; of 192 140 and 98, 86 and 85, of 256 173 and 124, 96 and 127).
+// Up to 32 rows four waves share them, two by two each half of the columns besides (P's three parts on all columns by two waves: heads of 64 36 -> 40 us, in e4m3
+// 36 -> 40, of 192 95 -> 108, 83 -> 106, of 256 121 -> 136).
+// Up to 16 rows go straight from memory to the operands; up to 32 in heads of 128 and, in e4m3, of 256 (8 tokens of each of 16 sequences of 4096, of 64 of 1024, 4
+// query heads a key head, 30 of one of 65536, 16 heads, us, so and by tiles in LDS, in bf16 heads of 64 47 and 36, 60 and 30, 68 and 69, of 128 66 and 64, 68 and 58,
+// 111 and 123, of 192 140 and 95, 136 and 92, 230 and 156, of 256 173 and 121, 199 and 120, 289 and 198; in e4m3 of 64 42 and 36, 54 and 29, 58 and 68, of 128 48 and 49, 48
+// and 46, 75 and 96, of 192 86 and 83, 84 and 80, 142 and 142, of 256 99 and 107, 119 and 106, 167 and 188; the smallest calls, one tile of one sequence, 6 to 11 and 7 to 14).
 struct ChunkPlan {
   bool few;         // by 16 or 32 rows at a time, from memory to the operands (rsa_cache.hip)
   int qb, rw;       // 32-row blocks of a wave, waves of different rows
@@ -715,7 +745,7 @@ ChunkPlan plan_of(const CacheDims &d, int T, bool eight) {
   p.few = d.dtype != RSA_BF16 || rows <= (d.A == 128 || (d.A == 256 && eight) ? 32 : 16);
   if (p.few) return p;
   p.qb = 1; const int64_t large = rows > 128 ? heads * ((rows + 255) / 256) : 0, slots = (int64_t)d.width * d.page;
-  p.rw = rows <= 64 ? 2 : 4;
+  p.rw = rows <= 32 ? 1 : rows <= 64 ? 2 : 4;
   if (d.A >= 192 ? rows > 128 : d.A == 128 && (large >= 512 || (large >= 256 && slots >= 4 * (int64_t)T))) p.rw = 8;
   if (d.A == 64 && large >= 512) p.qb = 2;
   p.rows = 32 * p.qb * p.rw;
@@ -736,10 +766,17 @@ hipError_t launch_chunk(const ChunkArgs &a, const ChunkPlan &p, hipStream_t st) 
   if (p.rows != 32 * QB * RW / KS) return hipErrorInvalidConfiguration;  // (not the plan's form)
   // (128 rows of heads of 256 in bf16: see plan_of)
   constexpr bool apart = AH == 4 && RW == 8 && KS == 2;
+  // (up to 32 rows of heads of 256 in e4m3: by the kernels for few)
+  constexpr bool eight = !(AH == 4 && KS == 4);
   const unsigned grid = (unsigned)(a.by_heads.d * p.tiles * p.parts);
-  if (a.Ks) chunk_kernel<AH, QB, RW, KS, true><<<grid, 64 * RW, 0, st>>>(a);
-  else if constexpr (apart) chunk_kernel<AH, QB, 4, 1, false><<<grid, 256, 0, st>>>(a);
-  else chunk_kernel<AH, QB, RW, KS, false><<<grid, 64 * RW, 0, st>>>(a);
+  if (a.Ks) {
+    if constexpr (eight) chunk_kernel<AH, QB, RW, KS, true><<<grid, 64 * RW, 0, st>>>(a);
+    else return hipErrorInvalidConfiguration;
+  } else if constexpr (apart) {
+    chunk_kernel<AH, QB, 4, 1, false><<<grid, 256, 0, st>>>(a);
+  } else {
+    chunk_kernel<AH, QB, RW, KS, false><<<grid, 64 * RW, 0, st>>>(a);
+  }
   return hipSuccess;
 }
 template <int AH>
@@ -749,6 +786,9 @@ hipError_t launch_chunk(const ChunkArgs &a, const ChunkPlan &p, hipStream_t st) 
   }
   if constexpr (AH == 1) {
     if (p.qb == 2) return launch_chunk<AH, 2, 4, 1>(a, p, st);
+  }
+  if constexpr (AH != 2) {  // (of heads of 128 the kernels for few take up to 32 rows)
+    if (p.rw == 1) return launch_chunk<AH, 1, 4, 4>(a, p, st);
   }
   if (p.rw == 2) return launch_chunk<AH, 1, 4, 2>(a, p, st);
   if constexpr (AH >= 2) {
