@@ -728,8 +728,9 @@ struct Attend : ChunkRows<KIND, NQ> {
     if constexpr (kRows) {  // (counts and lengths come while the first tile does; one that no row sees adds nothing)
       begin(b);
       const int first = tile * NQ * 16, last = (first + NQ * 16 < this->rows ? first + NQ * 16 : this->rows) - 1;
+      if (last < first) return;  // (all of tokens that are not there)
       this->least = limit_of(first, len);
-      const uint32_t most = (limit_of(last < first ? first : last, len) + kKeys - 1) / kKeys;
+      const uint32_t most = (limit_of(last, len) + kKeys - 1) / kKeys;
       end = end < most ? end : most;
 #pragma unroll
       for (int x = 0; x < NQ; ++x) {
@@ -854,7 +855,13 @@ __global__ __launch_bounds__((64 * Attend<T, A, NQ, KIND>::kWaves), (Attend<T, A
   At at(args, lds);
   const uint32_t head = args.by_tiles(blockIdx.x), b = head / (uint32_t)args.Zkv, h = head - b * args.Zkv;
   uint32_t tile = blockIdx.x - head * args.by_tiles.d;
-  if constexpr (KIND & kChunk) tile = args.by_tiles.d - 1 - tile;  // (the longest walks first)
+  // A chunk's last tiles, of the longest walks, first, but every head's from another tile on: the XCDs take work-groups in turn, and with tiles in the same
+  // order for all heads one of them had all that there are of few tokens, or all the longest (fp32, us: 32 of up to 512 tokens of each of 80 sequences of 8192, 4
+  // heads of 64, 2973 -> 504; prompts, 8 x 2048 263 -> 221, 80 x 512 213 -> 147).
+  if constexpr (KIND & kChunk) {
+    const uint32_t n = args.by_tiles.d, turn = head - args.by_tiles(head) * n;
+    tile = tile + turn < n ? n - 1 - tile - turn : 2 * n - 1 - tile - turn;
+  }
   const uint32_t len = length_of(args, b);
   at.walk(b, h, tile, len, 0, (len + At::kKeys - 1) / At::kKeys);
   at.finish(b, h, tile, nullptr);
