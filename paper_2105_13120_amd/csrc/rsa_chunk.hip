@@ -11,7 +11,7 @@
 // matrix work, which bounds these calls: up to 64 rows, where it bounds them least, 3 to 30 % more time).
 // Tiles come into LDS by direct loads from wherever their slots' pages are, a slot per lane looked up one tile further ahead; pools in
 // e4m3 come through registers, where what they stand for is formed exactly in bf16, once for all rows of the work-group.
-// Bound by the matrix cores, busy in 55 % of the cycles, and the vector ALU, busy with softmax in 44 %: 2048 tokens of 65536 slots, 32 query, 8 key heads of 128, run at 1.07 to 1.13 PFLOP/s from one GPU to another, where
+// Bound by the matrix cores, busy in 54 % of the cycles, and the vector ALU, busy with softmax in 43 %: 2048 tokens of 65536 slots, 32 query, 8 key heads of 128, run at 1.07 to 1.13 PFLOP/s from one GPU to another, where
 // a product of two 8192 x 8192 matrices by the library does 1.23; prompts of up to 2048 tokens at 0.58, of which a work-group's start and end, when
 // the matrix cores wait, take a third.
 // Tried: work-groups that stay and ask for the next item's first tile ahead (1954 -> 2172 us, prompts 126 -> 142); loads a tile and a half ahead with two
