@@ -9,9 +9,9 @@ from paper_2105_13120_amd import rsa
 pytestmark = pytest.mark.gpu
 
 INF = float("inf")
-# A, sequences, query and key heads, tokens: two waves that share 32 rows (of up to 64, of up to 128), waves of their own, 256 rows a work-group
+# A, sequences, query and key heads, tokens: four waves that share 32 rows, two (of up to 64, of up to 128), waves of their own, 256 rows a work-group
 # (of 64 rows a wave, of eight waves), and few rows
-FORMS = [(64, 1, 2, 2, 40), (64, 1, 4, 2, 40), (64, 1, 2, 1, 200), (64, 16, 32, 8, 200),
+FORMS = [(64, 2, 2, 2, 30), (64, 1, 4, 2, 9), (192, 1, 2, 2, 30), (256, 1, 2, 2, 32), (64, 1, 2, 2, 40), (64, 1, 4, 2, 40), (64, 1, 2, 1, 200), (64, 16, 32, 8, 200),
          (128, 1, 2, 2, 40), (128, 1, 4, 2, 40), (128, 1, 2, 1, 200), (128, 8, 32, 8, 500),
          (192, 1, 2, 2, 40), (192, 1, 4, 2, 40), (192, 1, 2, 1, 200),
          (256, 1, 2, 2, 40), (256, 1, 4, 2, 40), (256, 1, 2, 1, 200), (64, 2, 2, 2, 7), (128, 2, 2, 2, 30), (256, 2, 2, 2, 9)]
